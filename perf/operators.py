@@ -236,11 +236,12 @@ def _mix(x):
 
 
 def _block_exponents(m, v):
-    """Scale byte of every block: 2^(byte - 127) brings the block's largest |m| to at most 448, its largest v below 2."""
+    """Scale byte of every block: 2^(byte - 127) brings the block's largest |m| to at most 448, its largest v to at most
+    31/16, the largest code's value (so that no rounding of v is cut off)."""
     top = torch.where(torch.isfinite(m), m.abs(), torch.zeros_like(m)).view(-1, BLOCK).amax(1).view(torch.int32)
     em = ((top >> 23) + ((top & 0x7FFFFF) > 0x600000).int() - 8).clamp(min=1)
     top = torch.where(torch.isfinite(v), v, torch.zeros_like(v)).view(-1, BLOCK).amax(1).view(torch.int32)
-    return em, (top >> 23).clamp(min=1, max=253)
+    return em, ((top >> 23) + ((top & 0x7FFFFF) > 0x780000).int()).clamp(min=1, max=254)
 
 
 def _code_m(m, em):
@@ -252,7 +253,7 @@ def _code_m(m, em):
 def _code_v(v, ev, bits19):
     """Second moment in an unsigned float of 4 exponent and 4 mantissa bits, rounded up with the probability of the
     remainder by 19 random bits; only an exact zero is coded 0."""
-    inv = ((254 - ev) << 23).view(torch.float32).view(-1, 1)
+    inv = ((254 - ev) << 23).clamp(min=1 << 22).view(torch.float32).view(-1, 1)  # (2^-127 is no normal number)
     s = v.view(-1, BLOCK) * inv
     fine = torch.isfinite(s)
     c = ((torch.where(fine, s, torch.zeros_like(s)).view(torch.int32) + bits19) >> 19) - 1792
@@ -470,8 +471,10 @@ def _exact_adamw(s):
     step = torch.exp2(torch.floor(torch.log2(x.abs())).clamp(min=-6.0) - 3)
     mq = torch.where(x == 0, x, torch.round(x / step) * step) * torch.exp2(k)
     # second moment: steps of 1/16 of a power of two, up with the probability of the remainder, kept within 255 codes
-    k = torch.floor(torch.log2(v.amax(1, keepdim=True)))
-    k = torch.where(torch.isfinite(k), k, torch.full_like(k, -126.0)).clamp(-126.0, 126.0)
+    top = v.amax(1, keepdim=True)
+    k = torch.floor(torch.log2(top))
+    k = k + (top * torch.exp2(-k) > 1.9375)
+    k = torch.where(torch.isfinite(k), k, torch.full_like(k, -126.0)).clamp(-126.0, 127.0)
     x = v * torch.exp2(-k)
     e = torch.floor(torch.log2(x))
     place = torch.where(x > 0, 16 * (e + 15) + 16 * (x * torch.exp2(-e) - 1), torch.zeros_like(x))
