@@ -388,6 +388,161 @@ sl_status sl_compress_tensor_static(const float* theta_sync, const float* theta_
                                     uint8_t* payload, int64_t rows, int64_t cols, int32_t k, float beta,
                                     void* cuda_stream);
 
+/* ================================================================================================
+ * The inner phase (Alg. 1, the worker's H local AdamW steps on theta_r between two outer steps): the operators of a
+ * decoder's training step that stream memory, on the same flat buffers and tensor tables.  Same rules as above: device
+ * pointers unless marked host, caller-owned buffers, work enqueued on `cuda_stream`, no host synchronisation outside
+ * the create / destroy calls, no CPU implementation.  Activations and parameters are fp32 or bfloat16; all arithmetic
+ * is fp32 (sums over a whole table fp64), every result rounded once, to nearest even, when it is stored.
+ * ================================================================================================ */
+typedef enum { SL_F32 = 0, SL_BF16 = 1 } sl_dtype;
+
+/* --- AdamW over a tensor table, gradient clipping by the global norm included.
+ * With g the gradient, t the step counted from 1, wd the tensor's decay:
+ *     n  = grad_scale * sqrt(sum g^2)  over all elements of the table, fp64
+ *     c  = grad_scale * (max_norm > 0 ? min(1, max_norm / (n + 1e-6)) : 1)
+ *     g' = c g;   m = beta1 m + (1 - beta1) g';   v = beta2 v + (1 - beta2) g'^2
+ *     theta = theta - theta * (lr * wd) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * With skip_nonfinite, a step whose n is infinite or NaN leaves theta, m, v and the copy as they were.
+ *
+ * state_bits = 32: m, v are flat fp32 buffers of the table's layout, scales is NULL.
+ * state_bits = 8 : m, v are flat uint8 buffers of the table's layout and `scales` holds 2 x blocks bytes (the m scales,
+ *   then the v scales), blocks of 128 consecutive elements of one tensor, numbered tensor after tensor (the last one of
+ *   a tensor may be short).  An element's value is code value * 2^(scale byte - 127):
+ *     m: float8 e4m3 (bias 7, no infinities, 0x7F / 0xFF = NaN), nearest even; the scale is the smallest power of two
+ *        that brings the block's largest finite |m| to 448 or less.
+ *     v: unsigned, 4 exponent and 4 mantissa bits: code c > 0 stands for 2^(floor(c / 16) - 15) * (1 + (c mod 16) / 16), 0
+ *        for 0; the scale brings the block's largest finite v into (31/32, 31/16].  v is rounded up with the probability of its
+ *        remainder (19 bits of a hash of `seed` and the element's offset, so a step can be repeated): with beta2 near 1 a
+ *        rounding to nearest would hold v where it is.  A positive v never becomes 0: it would lose its denominator.
+ *     A non-finite m is coded NaN, a non-finite v as 255.  All zero bytes stand for m = v = 0, the state to begin with.
+ *   The update itself uses the new m and v before they are rounded.
+ *   theta (param_dtype), grad (grad_dtype): flat buffers.  copy: NULL, or a flat bfloat16 buffer that receives the updated
+ *   theta rounded to nearest (the working copy beside fp32 master parameters; needs param_dtype = SL_F32).
+ *   norm: NULL, or one fp32 that receives n.  Only elements of the table are read or written.
+ * The context owns its tile table (32 bytes per 4096 elements) and 16 KB for the norm; calls on one context must not
+ * overlap on the device.  The element ranges of the table must not overlap; offsets are multiples of 4.
+ * sl_adamw_read_state / _write_state: 8-bit state to and from fp32 buffers of the same layout (checkpoints, a change of
+ * state_bits); writing rounds as a step does.
+ * Errors: INVALID_ARG (NULL, step < 1, beta outside [0, 1), eps / max_norm / decay negative or not finite, a copy with bfloat16
+ * parameters, the same buffer twice), ALIGNMENT (a pointer not 16-byte aligned, offset % 4), UNSUPPORTED (state_bits, dtypes;
+ * read / write_state on a 32-bit context), TOO_LARGE, NOMEM, CUDA. */
+typedef struct {
+    int32_t param_dtype, grad_dtype; /* sl_dtype */
+    int32_t state_bits;              /* 32 or 8 */
+    int32_t skip_nonfinite;          /* 0 or 1 */
+    double beta1, beta2, eps;
+    double max_norm;                 /* 0: no clipping */
+} sl_adamw_config;
+typedef struct sl_adamw sl_adamw;
+sl_status sl_adamw_create(const sl_adamw_config* cfg, const sl_tensor_desc* tensors, const float* weight_decay, int32_t n_tensors,
+                          sl_adamw** out); /* tensors, weight_decay: host arrays of n_tensors */
+sl_status sl_adamw_destroy(sl_adamw* ctx);
+sl_status sl_adamw_sizes(const sl_adamw* ctx, int64_t* flat_elems, int64_t* blocks);
+sl_status sl_adamw_step(sl_adamw* ctx, void* theta, const void* grad, void* m, void* v, uint8_t* scales, uint16_t* copy, float* norm,
+                        int64_t step, double lr, double grad_scale, uint32_t seed, void* cuda_stream);
+sl_status sl_adamw_read_state(sl_adamw* ctx, const uint8_t* m, const uint8_t* v, const uint8_t* scales, float* m_out, float* v_out,
+                              void* cuda_stream);
+sl_status sl_adamw_write_state(sl_adamw* ctx, const float* m_in, const float* v_in, uint8_t* m, uint8_t* v, uint8_t* scales,
+                               uint32_t seed, void* cuda_stream);
+
+/* --- Residual update and norms around a block, row by row (a row = one token, `cols` wide):
+ *     z = branch * rb * branch_weight,  rb = 1 / sqrt(mean(branch^2) + eps)      (branch_weight NULL: z = branch)
+ *     y = x + alpha * gate * z                                                    (branch NULL: y = x, not written)
+ *     h = y * r * weight,               r  = 1 / sqrt(mean(y^2) + eps)            (weight NULL: 1; h NULL: no norm)
+ * h is formed from y before y is rounded.  gate: none, one value per column, per row, or per element.
+ * x, branch, y, h, their gradients and a row or element gate are `dtype`; the weights, a column gate and their gradients
+ * `weight_dtype` (fp32, or bfloat16 with bfloat16 activations).  Every matrix has its own row stride in elements (>= cols;
+ * 0 means cols); a row gate is one value per row, its stride 1 (0) or more.  y may be x and h may be branch.
+ * Backward, from dy (gradient of y from elsewhere, NULL: none) and dh (NULL: none), with the forward pass's y, rstd (needed with dh)
+ * and branch_rstd:
+ *     dx = dy + r (dh weight - yhat mean(dh weight yhat)),  yhat = y r
+ *     dgate = alpha dx z, summed over what the gate is shared by;  dz = alpha gate dx
+ *     dbranch = rb (dz branch_weight - bhat mean(dz branch_weight bhat)),  bhat = branch rb       (branch_weight NULL: dz)
+ *     dweight = sum_rows dh yhat;  dbranch_weight = sum_rows dz bhat
+ * Outputs are overwritten; dx, dbranch, dweight, dbranch_weight, dgate may be NULL; dx may be dy, dbranch may be dh or
+ * branch.  Column sums are added in a fixed order (results repeat bit for bit).  workspace: sl_norm_workspace_bytes().
+ * rows = 0 is allowed (sums become 0).  cols <= 16384.
+ * Errors: INVALID_ARG, ALIGNMENT (a pointer off its element size), UNSUPPORTED (dtypes), TOO_LARGE (cols), NOMEM, CUDA. */
+enum { SL_GATE_NONE = 0, SL_GATE_COLUMN = 1, SL_GATE_ROW = 2, SL_GATE_FULL = 3 };
+typedef struct {
+    int64_t rows, cols;
+    int32_t dtype, weight_dtype; /* sl_dtype */
+    int32_t gate_kind;
+    float alpha, eps;
+    int64_t ld_x, ld_branch, ld_gate, ld_y, ld_h; /* backward: y (and dx by ld_x, dbranch by ld_branch, dgate by ld_gate) */
+    int64_t ld_dy, ld_dh;
+} sl_norm_desc;
+sl_status sl_norm_forward(const sl_norm_desc* d, const void* x, const void* branch, const void* branch_weight, const void* gate,
+                          const void* weight, void* y, void* h, float* branch_rstd, float* rstd, void* cuda_stream);
+sl_status sl_norm_workspace_bytes(const sl_norm_desc* d, size_t* bytes);
+sl_status sl_norm_backward(const sl_norm_desc* d, const void* dy, const void* dh, const void* y, const void* branch,
+                           const void* branch_weight, const void* gate, const void* weight, const float* branch_rstd, const float* rstd,
+                           void* dx, void* dbranch, void* dweight, void* dbranch_weight, void* dgate, void* workspace,
+                           size_t workspace_bytes, void* cuda_stream);
+
+/* --- Rotary positions.  Pair i of the first rot_dim values of a head, (a, b) = (x[i], x[i + rot_dim / 2]) (half layout) or
+ * (x[2 i], x[2 i + 1]) (interleaved), becomes magnitude * (a cos - b sin, b cos + a sin) at angle = position * f_i; the
+ * rest of the head is passed through.  f_i = base^(-2 i / rot_dim), stretched for contexts longer than the trained one:
+ *     SL_ROPE_LINEAR    f / factor
+ *     SL_ROPE_BASE      base * factor^(rot_dim / (rot_dim - 2)) in place of base (slowest pair stretched by factor, fastest kept)
+ *     SL_ROPE_BY_PARTS  f (k + (1 - k) / factor), k = clamp((turns - low_turns) / (high_turns - low_turns), 0, 1),
+ *                       turns = original_length f / (2 pi)
+ * The context holds f_i / (2 pi) as 64-bit fractions of a turn, so position * f is reduced exactly: positions of any
+ * size (also negative) keep the full fp32 accuracy of sine and cosine.
+ * inverse != 0 turns by the negative angle: the backward pass (gradients of q and k in, gradients of their inputs out).
+ * q and k (k.in NULL: none) are [batch, seq, heads, head_dim] with strides in elements for batch, token and head and a
+ * unit stride inside a head; `out` may equal `in` with equal strides (in place), else the two must not overlap.
+ * positions: int32 or int64 (position_bits 32 / 64) by batch and token stride (a stride of 0 shares one row), or NULL: first + token.
+ * Errors: INVALID_ARG, ALIGNMENT (a pointer off its element size), UNSUPPORTED (dtype), TOO_LARGE, CUDA. */
+enum { SL_ROPE_HALF = 0, SL_ROPE_INTERLEAVED = 1 };
+enum { SL_ROPE_PLAIN = 0, SL_ROPE_LINEAR = 1, SL_ROPE_BASE = 2, SL_ROPE_BY_PARTS = 3 };
+typedef struct {
+    int32_t rot_dim; /* even, 2..1024 */
+    int32_t layout, scaling;
+    double base, factor, original_length, low_turns, high_turns, magnitude;
+} sl_rotary_config;
+typedef struct {
+    const void* in;
+    void* out;
+    int64_t heads;
+    int64_t in_batch, in_token, in_head, out_batch, out_token, out_head;
+} sl_rotary_heads;
+typedef struct {
+    int32_t dtype, position_bits, inverse;
+    int64_t batch, seq, head_dim;
+    int64_t first, pos_batch, pos_token;
+} sl_rotary_desc;
+typedef struct sl_rotary sl_rotary;
+sl_status sl_rotary_create(const sl_rotary_config* cfg, sl_rotary** out);
+sl_status sl_rotary_destroy(sl_rotary* ctx);
+sl_status sl_rotary_apply(sl_rotary* ctx, const sl_rotary_desc* d, const sl_rotary_heads* q, const sl_rotary_heads* k,
+                          const void* positions, void* cuda_stream);
+
+/* --- Next-token loss and its gradient with respect to the logits, in one call.  Per row with target t != ignore_index:
+ *     lse = log sum_j exp(x_j);   loss = lse - (1 - smoothing) x_t - smoothing mean_j x_j + z lse^2
+ *     grad_j = w (p_j (1 + 2 z lse) - (1 - smoothing) [j = t] - smoothing / vocab),   p_j = exp(x_j - lse)
+ * with w = scale / (number of rows that count) when mean != 0, else scale.  Ignored rows have loss 0 and gradient 0 (their lse
+ * is still written).  total = w * sum of the losses; 0 when no row counts.  A logit of -inf has p = 0 (a masked vocabulary
+ * entry; with smoothing > 0 it makes the loss infinite, as the formula says); a row of nothing but -inf has lse = -inf, gradient 0
+ * and loss +inf; NaN or +inf in a row give NaN.  A target outside [0, vocab) that is not ignore_index gives its row (and the
+ * total) a NaN loss and a gradient of 0 (the row counts).
+ * grad: NULL (loss only), or rows of `dtype` by ld_grad; grad may be logits itself (then ld_grad = ld_logits).
+ * row_loss (rows fp32) is required; lse, total may be NULL.  targets: int32 or int64 (target_bits).  rows = 0 is allowed.
+ * workspace: sl_loss_workspace_bytes(), 16-byte aligned, contents need not be kept; calls that share it must not overlap.
+ * Errors: INVALID_ARG, ALIGNMENT, UNSUPPORTED (dtype, target_bits), TOO_LARGE (vocab > 2^30), NOMEM, CUDA. */
+typedef struct {
+    int64_t rows, vocab;
+    int32_t dtype, target_bits;
+    int64_t ld_logits, ld_grad; /* 0: vocab */
+    int64_t ignore_index;
+    float smoothing, z, scale;
+    int32_t mean;
+} sl_loss_desc;
+size_t sl_loss_workspace_bytes(void);
+sl_status sl_token_loss(const sl_loss_desc* d, const void* logits, const void* targets, void* grad, float* row_loss, float* lse,
+                        float* total, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 const char* sl_strerror(sl_status s);
 const char* sl_last_cuda_error(void); /* text of the last CUDA error seen by this thread */
 

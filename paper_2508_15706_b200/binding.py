@@ -21,6 +21,10 @@ EXPORTS = (
     "sl_outer_step", "sl_outer_step_host", "sl_validate_payload", "sl_read_stats", "sl_strerror",
     "sl_last_cuda_error", "sl_diloco_step", "sl_coded_payload_capacity", "sl_encode_payload", "sl_decode_payload", "sl_set_tile_copies", "sl_device_status", "sl_static_scratch_bytes", "sl_compress_tensor_static", "sl_set_ef_deferred", "sl_ef_pending", "sl_ef_flush", "sl_profile_enable", "sl_profile_read", "sl_profile_name", "sl_lom_step", "sl_diloco_topk_step", "sl_lom_topk_step", "sl_streaming_due",
     "sl_compress_bf16", "sl_aggregate_apply_bf16", "sl_outer_step_bf16", "sl_aggregate_apply_coded", "sl_ef_flush_bf16",
+    # the inner phase (wrapped in inner.py)
+    "sl_adamw_create", "sl_adamw_destroy", "sl_adamw_sizes", "sl_adamw_step", "sl_adamw_read_state", "sl_adamw_write_state",
+    "sl_norm_forward", "sl_norm_workspace_bytes", "sl_norm_backward", "sl_rotary_create", "sl_rotary_destroy", "sl_rotary_apply",
+    "sl_loss_workspace_bytes", "sl_token_loss",
 )
 PROFILE_SLOTS = 9
 

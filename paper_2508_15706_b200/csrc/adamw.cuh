@@ -1,0 +1,404 @@
+// AdamW over a tensor table: global gradient norm, then one pass over parameters, gradients and moments.
+// Part of libsparseloco (inner.cu).
+//
+// Bound: HBM.  A step reads theta, g, m, v once and writes theta, m, v once (28 bytes per element with 32-bit moments and
+// fp32 gradients, 16 with 8-bit ones), plus the pass over g that the norm needs before anything can be updated.  The
+// update kernel walks the table from its end to its beginning: the part of g that the norm pass read last is still in
+// the 126 MB L2 and is not fetched again.
+#pragma once
+#include <cuda_fp8.h>
+
+#include "inner_common.cuh"
+
+namespace {
+
+constexpr int kAdamTile = 4096;   // elements of one tensor that a CTA updates
+constexpr int kAdamThreads = 256;
+constexpr int kAdamVec = 8;       // consecutive elements of a thread
+constexpr int kAdamBlock = 128;   // elements under one scale of an 8-bit moment: 16 threads
+constexpr int kAdamMaxParts = 2048;
+
+struct AdamTile {
+    long long base;    // element offset in the flat buffers
+    long long block0;  // first scale block
+    int len;
+    int tensor;
+    long long pad;
+};
+static_assert(sizeof(AdamTile) == 32, "AdamTile layout");
+
+struct AdamClip {  // what the norm pass leaves for the update
+    float coef;
+    int ok;
+    unsigned ticket;  // CTAs that are done; the last one puts it back to 0
+    int pad;
+};
+
+// 32-bit integer hash, Chris Wellons' published two-multiplication mix: bijective, every input bit reaches every output bit.
+__device__ __forceinline__ unsigned mix32(unsigned x) {
+    x ^= x >> 16;
+    x *= 0x7FEB352Du;
+    x ^= x >> 15;
+    x *= 0x846CA68Bu;
+    return x ^ (x >> 16);
+}
+// 19 random bits of element `i` under `seed`
+__device__ __forceinline__ unsigned hash_key(unsigned seed, unsigned long long i) {
+    return mix32(seed) ^ mix32((unsigned)(i >> 32) * 0x9E3779B9u);
+}
+__device__ __forceinline__ unsigned lot19(unsigned key, unsigned long long i) { return mix32((unsigned)i ^ key) >> 13; }
+
+__device__ __forceinline__ float finite_abs(float x) {
+    const float a = fabsf(x);
+    return a <= 3.402823466e38f ? a : 0.0f;  // false for NaN too
+}
+__device__ __forceinline__ float pow2_byte(int byte) { return __uint_as_float((unsigned)byte << 23); }  // 2^(byte - 127), byte 1..254
+__device__ __forceinline__ float inv_pow2_byte(int byte) {  // 2^(127 - byte), byte 1..254 (2^-127 is no normal number)
+    const unsigned b = (unsigned)(254 - byte) << 23;
+    return __uint_as_float(b > (1u << 22) ? b : 1u << 22);
+}
+__device__ __forceinline__ int scale_byte_m(float top) {
+    const unsigned b = __float_as_uint(top);
+    const int e = (int)(b >> 23) + ((b & 0x7FFFFFu) > 0x600000u) - 8;  // 1.75 * 2^8 = 448 is the largest e4m3
+    return e < 1 ? 1 : e;
+}
+__device__ __forceinline__ int scale_byte_v(float top) {
+    const unsigned b = __float_as_uint(top);
+    const int e = (int)(b >> 23) + ((b & 0x7FFFFFu) > 0x780000u);  // at most 31/16, the largest code's value: rounding up is never cut off
+    return e < 1 ? 1 : (e > 254 ? 254 : e);
+}
+__device__ __forceinline__ unsigned code_v(float v, float inv, unsigned lot) {
+    const float s = v * inv;  // a power of two: exact
+    if (s == 0.0f) return 0u;
+    if (!(s <= 3.402823466e38f)) return 255u;
+    const int c = (int)((__float_as_uint(s) + lot) >> 19) - 1792;  // the exponent and the first 4 mantissa bits
+    return (unsigned)(c < 1 ? 1 : (c > 255 ? 255 : c));
+}
+__device__ __forceinline__ float value_v(unsigned c) { return c ? __uint_as_float((c + 1792u) << 19) : 0.0f; }
+__device__ __forceinline__ unsigned code_m2(float a, float b) {
+    unsigned c = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+    if (!(fabsf(a) <= 3.402823466e38f)) c |= 0x007Fu;  // no infinity in the format: NaN
+    if (!(fabsf(b) <= 3.402823466e38f)) c |= 0x7F00u;
+    return c;
+}
+__device__ __forceinline__ float2 value_m2(unsigned c) {
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)c, __NV_E4M3);
+    return __half22float2(__half2(h));
+}
+
+// 8 elements at p; A8: p is aligned to 8 elements, else to 4 only.
+template <class T, bool A8>
+__device__ __forceinline__ void load8(const T* p, float (&f)[kAdamVec]) {
+    if (A8) {
+        Pack<T, 8> a;
+        a.load_stream(p);
+        a.get(f);
+    } else {
+        Pack<T, 4> a, b;
+        a.load_stream(p);
+        b.load_stream(p + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = widen(a.v[i]), f[i + 4] = widen(b.v[i]);
+    }
+}
+template <class T, bool A8>
+__device__ __forceinline__ void store8(T* p, const float (&f)[kAdamVec]) {
+    if (A8) {
+        Pack<T, 8> a;
+        a.set(f);
+        a.store_stream(p);
+    } else {
+        Pack<T, 4> a, b;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a.v[i] = narrow<T>(f[i]), b.v[i] = narrow<T>(f[i + 4]);
+        a.store_stream(p);
+        b.store_stream(p + 4);
+    }
+}
+template <class T, bool A8>
+__device__ __forceinline__ void load_some(const T* p, int n, float (&f)[kAdamVec]) {
+    if (n >= kAdamVec) {
+        load8<T, A8>(p, f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kAdamVec; ++i) f[i] = i < n ? widen(p[i]) : 0.0f;
+    }
+}
+template <class T, bool A8>
+__device__ __forceinline__ void store_some(T* p, int n, const float (&f)[kAdamVec]) {
+    if (n >= kAdamVec) {
+        store8<T, A8>(p, f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kAdamVec; ++i)
+            if (i < n) p[i] = narrow<T>(f[i]);
+    }
+}
+// 8 code bytes as two words
+template <bool A8>
+__device__ __forceinline__ uint2 load_codes(const uint8_t* p, int n) {
+    uint2 w = make_uint2(0u, 0u);
+    if (n >= kAdamVec) {
+        if (A8) {
+            w = __ldcs(reinterpret_cast<const uint2*>(p));
+        } else {
+            w.x = __ldcs(reinterpret_cast<const unsigned*>(p));
+            w.y = __ldcs(reinterpret_cast<const unsigned*>(p) + 1);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kAdamVec; ++i)
+            if (i < n) (i < 4 ? w.x : w.y) |= (unsigned)p[i] << (8 * (i & 3));
+    }
+    return w;
+}
+template <bool A8>
+__device__ __forceinline__ void store_codes(uint8_t* p, int n, uint2 w) {
+    if (n >= kAdamVec) {
+        if (A8) {
+            __stcs(reinterpret_cast<uint2*>(p), w);
+        } else {
+            __stcs(reinterpret_cast<unsigned*>(p), w.x);
+            __stcs(reinterpret_cast<unsigned*>(p) + 1, w.y);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kAdamVec; ++i)
+            if (i < n) p[i] = (uint8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
+    }
+}
+__device__ __forceinline__ void values_m(uint2 w, float scale, float (&m)[kAdamVec]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = value_m2(((i < 2 ? w.x : w.y) >> (16 * (i & 1))) & 0xFFFFu);
+        m[2 * i] = f.x * scale;
+        m[2 * i + 1] = f.y * scale;
+    }
+}
+__device__ __forceinline__ void values_v(uint2 w, float scale, float (&v)[kAdamVec]) {
+#pragma unroll
+    for (int i = 0; i < kAdamVec; ++i) v[i] = value_v(((i < 4 ? w.x : w.y) >> (8 * (i & 3))) & 0xFFu) * scale;
+}
+// Codes of the thread's 8 moments; the 16 threads of a block agree on its scales.  Every lane of the warp takes part.
+__device__ __forceinline__ void encode_moments(const float (&m)[kAdamVec], const float (&v)[kAdamVec], unsigned seed, unsigned long long at,
+                                               uint2& cm, uint2& cv, int& bm, int& bv) {
+    float tm = 0.0f, tv = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kAdamVec; ++i) {
+        tm = fmaxf(tm, finite_abs(m[i]));
+        tv = fmaxf(tv, finite_abs(v[i]));
+    }
+#pragma unroll
+    for (int o = 8; o; o >>= 1) {
+        tm = fmaxf(tm, __shfl_xor_sync(kFullMask, tm, o));
+        tv = fmaxf(tv, __shfl_xor_sync(kFullMask, tv, o));
+    }
+    bm = scale_byte_m(tm);
+    bv = scale_byte_v(tv);
+    const float im = inv_pow2_byte(bm), iv = inv_pow2_byte(bv);
+    cm.x = code_m2(m[0] * im, m[1] * im) | (code_m2(m[2] * im, m[3] * im) << 16);
+    cm.y = code_m2(m[4] * im, m[5] * im) | (code_m2(m[6] * im, m[7] * im) << 16);
+    cv = make_uint2(0u, 0u);
+    // (8 consecutive offsets that begin at a multiple of 4 may cross a multiple of 2^32)
+    const unsigned key0 = hash_key(seed, at), key1 = hash_key(seed, at + 4);
+#pragma unroll
+    for (int i = 0; i < kAdamVec; ++i) {
+        const unsigned c = code_v(v[i], iv, lot19(i < 4 ? key0 : key1, at + (unsigned)i));
+        (i < 4 ? cv.x : cv.y) |= c << (8 * (i & 3));
+    }
+}
+
+// Sum of squares of the gradient in fp64: every CTA leaves one partial sum, the last one to finish adds them in index
+// order and turns the norm into the coefficient of the update.  The assignment of tiles to CTAs is fixed, so is the sum.
+template <class G, bool A8>
+__global__ void __launch_bounds__(kAdamThreads)
+adamw_norm_kernel(const AdamTile* __restrict__ tiles, long long n_tiles, const G* __restrict__ grad, double grad_scale, double max_norm,
+                  double* __restrict__ parts, AdamClip* __restrict__ clip, float* __restrict__ norm_out) {
+    __shared__ double warp_part[kAdamThreads / 32];
+    __shared__ int last;
+    const int tid = threadIdx.x;
+    cudaTriggerProgrammaticLaunchCompletion();  // the update's CTAs may come and load their operands
+    double acc = 0.0;
+    for (long long t = blockIdx.x; t < n_tiles; t += gridDim.x) {
+        const AdamTile tile = tiles[t];
+        const G* g = grad + tile.base;
+#pragma unroll
+        for (int it = 0; it < kAdamTile / (kAdamThreads * kAdamVec); ++it) {
+            const int i = (it * kAdamThreads + tid) * kAdamVec;
+            if (i < tile.len) {
+                float f[kAdamVec];
+                if (i + kAdamVec <= tile.len) {
+                    Pack<G, 4> a, b;
+                    if (A8) {
+                        Pack<G, 8> c;
+                        c.load(g + i);
+                        c.get(f);
+                    } else {
+                        a.load(g + i);
+                        b.load(g + i + 4);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) f[j] = widen(a.v[j]), f[j + 4] = widen(b.v[j]);
+                    }
+                } else {
+                    load_some<G, A8>(g + i, tile.len - i, f);
+                }
+#pragma unroll
+                for (int j = 0; j < kAdamVec; ++j) acc = fma((double)f[j], (double)f[j], acc);
+            }
+        }
+    }
+    acc = warp_sum(acc);
+    if ((tid & 31) == 0) warp_part[tid >> 5] = acc;
+    __syncthreads();
+    if (tid == 0) {
+        double s = 0.0;
+        for (int w = 0; w < kAdamThreads / 32; ++w) s += warp_part[w];
+        parts[blockIdx.x] = s;
+        __threadfence();
+        last = atomicAdd(&clip->ticket, 1u) == gridDim.x - 1;
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    double s = 0.0;
+    for (int p = tid; p < (int)gridDim.x; p += kAdamThreads) s += __ldcg(parts + p);
+    s = warp_sum(s);
+    if ((tid & 31) == 0) warp_part[tid >> 5] = s;
+    __syncthreads();
+    if (tid == 0) {
+        s = 0.0;
+        for (int w = 0; w < kAdamThreads / 32; ++w) s += warp_part[w];
+        const double n = fabs(grad_scale) * sqrt(s);
+        double c = grad_scale;
+        if (max_norm > 0.0) {
+            const double q = max_norm / (n + 1e-6);
+            if (q < 1.0) c *= q;  // (false for NaN: the coefficient stays, the gradient carries the NaN)
+        }
+        clip->coef = (float)c;
+        clip->ok = n <= 1.7976931348623157e308;
+        clip->ticket = 0u;
+        if (norm_out) *norm_out = (float)n;
+    }
+}
+
+struct AdamArgs {
+    void* theta;
+    const void* grad;
+    void* m;
+    void* v;
+    uint8_t* scales;
+    bf16* copy;
+    const AdamClip* clip;  // NULL: no norm pass ran
+    long long blocks;
+    float coef, beta1, omb1, beta2, omb2, eps, inv_sqrt_bc2, step_size, lr;
+    unsigned seed;
+    int skip;
+};
+
+// The moments are formed by single-rounded operations in the order of the formula, so that the 8-bit codes do not depend
+// on how a compiler contracts them.  sqrt and the division are the fast ones (2^-22 relative): theta's own rounding is coarser.
+__device__ __forceinline__ void adamw_element(float& p, float g, float& m, float& v, const AdamArgs& a, float c, float decay) {
+    g = __fmul_rn(g, c);
+    m = __fadd_rn(__fmul_rn(m, a.beta1), __fmul_rn(g, a.omb1));
+    v = __fadd_rn(__fmul_rn(v, a.beta2), __fmul_rn(__fmul_rn(g, g), a.omb2));
+    float r;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+    const float den = fmaf(r, a.inv_sqrt_bc2, a.eps);
+    p = fmaf(-a.step_size, __fdividef(m, den), fmaf(-decay, p, p));
+}
+
+template <class P, class G, int BITS, bool A8>
+__global__ void __launch_bounds__(kAdamThreads)
+adamw_step_kernel(const AdamTile* __restrict__ tiles, const float* __restrict__ weight_decay, const AdamArgs a) {
+    const AdamTile tile = tiles[gridDim.x - 1 - blockIdx.x];  // last tiles first: their gradients are still in L2
+    const int tid = threadIdx.x;
+    P* theta = static_cast<P*>(a.theta) + tile.base;
+    const G* grad = static_cast<const G*>(a.grad) + tile.base;
+    const float decay = a.lr * weight_decay[tile.tensor];
+    constexpr int kIters = kAdamTile / (kAdamThreads * kAdamVec);
+    if (a.clip) cudaGridDependencySynchronize();
+    const float c = a.clip ? a.clip->coef : a.coef;
+    if (a.clip && a.skip && !a.clip->ok) return;
+#pragma unroll 1
+    for (int it = 0; it < kIters; ++it) {
+        const int i = (it * kAdamThreads + tid) * kAdamVec;
+        if ((it * kAdamThreads + (tid & ~31)) * kAdamVec >= tile.len) return;  // whole warps only
+        const int n = tile.len - i;  // elements of this thread (more than 8: 8; below 1: none)
+        float p[kAdamVec], g[kAdamVec], m[kAdamVec], v[kAdamVec];
+        load_some<P, A8>(theta + i, n, p);
+        load_some<G, A8>(grad + i, n, g);
+        if (BITS == 32) {
+            load_some<float, A8>(static_cast<const float*>(a.m) + tile.base + i, n, m);
+            load_some<float, A8>(static_cast<const float*>(a.v) + tile.base + i, n, v);
+        } else {
+            const long long blk = tile.block0 + i / kAdamBlock;
+            const bool has = n > 0;
+            const uint2 wm = load_codes<A8>(static_cast<const uint8_t*>(a.m) + tile.base + i, n);
+            const uint2 wv = load_codes<A8>(static_cast<const uint8_t*>(a.v) + tile.base + i, n);
+            values_m(wm, pow2_byte(has ? a.scales[blk] : 0), m);
+            values_v(wv, pow2_byte(has ? a.scales[a.blocks + blk] : 0), v);
+        }
+#pragma unroll
+        for (int j = 0; j < kAdamVec; ++j) adamw_element(p[j], g[j], m[j], v[j], a, c, decay);
+        store_some<P, A8>(theta + i, n, p);
+        if (a.copy) store_some<bf16, A8>(a.copy + tile.base + i, n, p);
+        if (BITS == 32) {
+            store_some<float, A8>(static_cast<float*>(a.m) + tile.base + i, n, m);
+            store_some<float, A8>(static_cast<float*>(a.v) + tile.base + i, n, v);
+        } else {
+            if (n < kAdamVec) {  // what lies behind the tensor's end has no part in the scale
+#pragma unroll
+                for (int j = 0; j < kAdamVec; ++j)
+                    if (j >= n) m[j] = v[j] = 0.0f;
+            }
+            uint2 cm, cv;
+            int bm, bv;
+            encode_moments(m, v, a.seed, (unsigned long long)(tile.base + i), cm, cv, bm, bv);
+            store_codes<A8>(static_cast<uint8_t*>(a.m) + tile.base + i, n, cm);
+            store_codes<A8>(static_cast<uint8_t*>(a.v) + tile.base + i, n, cv);
+            if (n > 0 && (tid & 15) == 0) {
+                const long long blk = tile.block0 + i / kAdamBlock;
+                a.scales[blk] = (uint8_t)bm;
+                a.scales[a.blocks + blk] = (uint8_t)bv;
+            }
+        }
+    }
+}
+
+// WRITE: fp32 moments -> codes and scales; else codes and scales -> fp32 moments.
+template <bool WRITE, bool A8>
+__global__ void __launch_bounds__(kAdamThreads)
+adamw_state_kernel(const AdamTile* __restrict__ tiles, float* m32, float* v32, uint8_t* m8, uint8_t* v8, uint8_t* scales, long long blocks,
+                   unsigned seed) {
+    const AdamTile tile = tiles[blockIdx.x];
+    const int tid = threadIdx.x;
+    constexpr int kIters = kAdamTile / (kAdamThreads * kAdamVec);
+#pragma unroll
+    for (int it = 0; it < kIters; ++it) {
+        const int i = (it * kAdamThreads + tid) * kAdamVec;
+        if ((it * kAdamThreads + (tid & ~31)) * kAdamVec >= tile.len) return;  // whole warps only
+        const int n = tile.len - i;
+        const long long blk = tile.block0 + i / kAdamBlock;
+        float m[kAdamVec], v[kAdamVec];
+        if (WRITE) {
+            load_some<float, A8>(m32 + tile.base + i, n, m);
+            load_some<float, A8>(v32 + tile.base + i, n, v);
+            uint2 cm, cv;
+            int bm, bv;
+            encode_moments(m, v, seed, (unsigned long long)(tile.base + i), cm, cv, bm, bv);
+            store_codes<A8>(m8 + tile.base + i, n, cm);
+            store_codes<A8>(v8 + tile.base + i, n, cv);
+            if (n > 0 && (tid & 15) == 0) {
+                scales[blk] = (uint8_t)bm;
+                scales[blocks + blk] = (uint8_t)bv;
+            }
+        } else if (n > 0) {
+            values_m(load_codes<A8>(m8 + tile.base + i, n), pow2_byte(scales[blk]), m);
+            values_v(load_codes<A8>(v8 + tile.base + i, n), pow2_byte(scales[blocks + blk]), v);
+            store_some<float, A8>(m32 + tile.base + i, n, m);
+            store_some<float, A8>(v32 + tile.base + i, n, v);
+        }
+    }
+}
+
+}  // namespace

@@ -16,8 +16,6 @@ constexpr unsigned kFull = 0xFFFFFFFFu;
 constexpr int kProfSlots = 9;     // kernels of one outer step
 constexpr int kProfMaxSeq = 256;  // recorded sequences kept between two reads
 
-thread_local char g_cuda_err[256] = "";
-
 // One chunk of one tensor: where its elements live in the flat buffers.
 struct ChunkDesc {
     long long base;    // element offset of in-chunk index 0

@@ -1,0 +1,684 @@
+// The operators of the inner phase (Alg. 1, the worker's local steps) for sm_100a: host side of the C ABI declared in
+// include/sparseloco.h, over the kernels in the .cuh files beside it.
+//   adamw.cuh       AdamW over the tensor table, clipping by the global norm, moments in 32 or 8 bits
+//   block_norm.cuh  residual update and norms around a block, forward and backward
+//   rotary.cuh      rotary positions of queries and keys
+//   token_loss.cuh  next-token loss and its gradient
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+#include <stdio.h>
+#include <string.h>
+
+#include <algorithm>
+#include <new>
+#include <utility>
+#include <vector>
+
+#include "sparseloco.h"
+
+#include "host.cuh"
+#include "inner_common.cuh"
+#include "adamw.cuh"
+#include "block_norm.cuh"
+#include "rotary.cuh"
+#include "token_loss.cuh"
+
+struct sl_adamw {
+    sl_adamw_config cfg;
+    int device, n_sms;
+    bool aligned8;  // every tensor begins on a multiple of 8 elements
+    long long n_tiles, blocks, flat_elems;
+    AdamTile* d_tiles;
+    float* d_decay;
+    double* d_parts;
+    AdamClip* d_clip;
+};
+
+struct sl_rotary {
+    sl_rotary_config cfg;
+    int device;
+    unsigned long long* d_turns;
+};
+
+namespace {
+
+sl_status sm_count(int* n) {
+    int dev = 0;
+    SL_CUDA(cudaGetDevice(&dev));
+    SL_CUDA(cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev));
+    return SL_OK;
+}
+
+inline bool known_dtype(int t) { return t == SL_F32 || t == SL_BF16; }
+inline int dtype_bytes(int t) { return t == SL_F32 ? 4 : 2; }
+inline bool finite_at_least(double x, double low) { return isfinite(x) && x >= low; }
+
+// ---- AdamW
+template <class G>
+sl_status launch_adamw_norm(const sl_adamw* c, const void* grad, double grad_scale, float* norm, cudaStream_t st) {
+    const long long want = c->n_tiles, most = (long long)c->n_sms * 8;
+    const unsigned grid = (unsigned)std::min(std::min(want, most), (long long)kAdamMaxParts);
+    auto kern = c->aligned8 ? adamw_norm_kernel<G, true> : adamw_norm_kernel<G, false>;
+    kern<<<grid, kAdamThreads, 0, st>>>(c->d_tiles, c->n_tiles, static_cast<const G*>(grad), grad_scale, c->cfg.max_norm, c->d_parts, c->d_clip, norm);
+    SL_CUDA(cudaGetLastError());
+    return SL_OK;
+}
+
+template <class P, class G, int BITS>
+sl_status launch_adamw_step(const sl_adamw* c, const AdamArgs& a, cudaStream_t st) {
+    auto kern = c->aligned8 ? adamw_step_kernel<P, G, BITS, true> : adamw_step_kernel<P, G, BITS, false>;
+    cudaLaunchConfig_t lc;
+    memset(&lc, 0, sizeof(lc));
+    lc.gridDim = dim3((unsigned)c->n_tiles);
+    lc.blockDim = dim3(kAdamThreads);
+    lc.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = at;
+    lc.numAttrs = a.clip ? 1 : 0;  // only behind the norm kernel, which waits for what came before it
+    SL_CUDA(cudaLaunchKernelEx(&lc, kern, (const AdamTile*)c->d_tiles, (const float*)c->d_decay, a));
+    return SL_OK;
+}
+
+template <class P, class G>
+sl_status launch_adamw_bits(const sl_adamw* c, const AdamArgs& a, cudaStream_t st) {
+    return c->cfg.state_bits == 32 ? launch_adamw_step<P, G, 32>(c, a, st) : launch_adamw_step<P, G, 8>(c, a, st);
+}
+
+// ---- norms
+struct NormShape {
+    int vec, nv, threads, rows_per_cta;
+};
+
+// A warp takes a narrow row (forward: up to 4 vectors a lane; backward, where a thread's columns carry three sums: one); wider
+// rows are spread over a CTA of at most 512 threads, with as few vectors per thread as that allows.
+NormShape norm_shape(int cols, int vec, bool backward) {
+    NormShape s;
+    s.vec = vec;
+    const int vectors = (cols + vec - 1) / vec;
+    if (vectors <= (backward ? 32 : 128)) {
+        s.threads = 32;
+        s.nv = vectors <= 32 ? 1 : (vectors <= 64 && vec > 1 ? 2 : 4);
+        s.rows_per_cta = backward ? 8 : kNormWarpRows;
+        return s;
+    }
+    const int need = (vectors + kNormMaxThreads - 1) / kNormMaxThreads;
+    if (vec > 1) s.nv = need <= 1 ? 1 : need <= 2 ? 2 : need <= 4 ? 4 : 8;
+    else s.nv = need <= 1 ? 1 : need <= 4 ? 4 : 32;
+    s.threads = ((vectors + s.nv - 1) / s.nv + 31) / 32 * 32;
+    s.rows_per_cta = 1;
+    return s;
+}
+
+template <class T, class W, int VEC, int NV>
+sl_status launch_norm(const NormArgs& a, const NormShape& s, unsigned grid, bool backward, cudaStream_t st) {
+    const dim3 block((unsigned)s.threads, (unsigned)s.rows_per_cta);
+    if (backward) {
+        const size_t smem = s.rows_per_cta > 1 ? sizeof(float) * 3 * (size_t)a.cols : 0;
+        norm_backward_kernel<T, W, VEC, NV><<<grid, block, smem, st>>>(a);
+    } else {
+        norm_forward_kernel<T, W, VEC, NV><<<grid, block, 0, st>>>(a);
+    }
+    SL_CUDA(cudaGetLastError());
+    return SL_OK;
+}
+
+template <class T, class W>
+sl_status launch_norm_shape(const NormArgs& a, const NormShape& s, unsigned grid, bool backward, cudaStream_t st) {
+    constexpr int V = 16 / (int)sizeof(T);
+    if (s.vec == 1) return s.nv == 1 ? launch_norm<T, W, 1, 1>(a, s, grid, backward, st) : s.nv == 4 ? launch_norm<T, W, 1, 4>(a, s, grid, backward, st)
+                                                                                                     : launch_norm<T, W, 1, 32>(a, s, grid, backward, st);
+    if (s.nv == 1) return launch_norm<T, W, V, 1>(a, s, grid, backward, st);
+    if (s.nv == 2) return launch_norm<T, W, V, 2>(a, s, grid, backward, st);
+    if (s.nv == 4) return launch_norm<T, W, V, 4>(a, s, grid, backward, st);
+    return launch_norm<T, W, V, 32 / V>(a, s, grid, backward, st);
+}
+
+sl_status launch_norm_types(const sl_norm_desc* d, const NormArgs& a, const NormShape& s, unsigned grid, bool backward, cudaStream_t st) {
+    if (d->dtype == SL_F32) return launch_norm_shape<float, float>(a, s, grid, backward, st);
+    if (d->weight_dtype == SL_F32) return launch_norm_shape<bf16, float>(a, s, grid, backward, st);
+    return launch_norm_shape<bf16, bf16>(a, s, grid, backward, st);
+}
+
+sl_status norm_check(const sl_norm_desc* d) {
+    if (!d || d->rows < 0 || d->cols < 1 || !isfinite(d->alpha) || !finite_at_least(d->eps, 0.0)) return SL_ERR_INVALID_ARG;
+    if (!known_dtype(d->dtype) || !known_dtype(d->weight_dtype)) return SL_ERR_UNSUPPORTED;
+    if (d->dtype == SL_F32 && d->weight_dtype != SL_F32) return SL_ERR_UNSUPPORTED;
+    if (d->gate_kind < SL_GATE_NONE || d->gate_kind > SL_GATE_FULL) return SL_ERR_INVALID_ARG;
+    if (d->cols > kNormMaxCols || d->rows > 0x7FFFFFFFll) return SL_ERR_TOO_LARGE;
+    const int64_t ld[] = {d->ld_x, d->ld_branch, d->ld_y, d->ld_h, d->ld_dy, d->ld_dh};
+    for (int64_t l : ld)
+        if (l != 0 && l < d->cols) return SL_ERR_INVALID_ARG;
+    if (d->ld_gate < 0 || (d->gate_kind == SL_GATE_FULL && d->ld_gate != 0 && d->ld_gate < d->cols)) return SL_ERR_INVALID_ARG;
+    return SL_OK;
+}
+
+void norm_strides(const sl_norm_desc* d, NormArgs* a) {
+    memset(a, 0, sizeof(*a));
+    a->rows = d->rows;
+    a->cols = (int)d->cols;
+    a->gate_kind = d->gate_kind;
+    a->alpha = d->alpha;
+    a->eps = d->eps;
+    a->inv_cols = 1.0f / (float)d->cols;
+    a->ld_x = d->ld_x ? d->ld_x : d->cols;
+    a->ld_branch = d->ld_branch ? d->ld_branch : d->cols;
+    a->ld_y = d->ld_y ? d->ld_y : d->cols;
+    a->ld_h = d->ld_h ? d->ld_h : d->cols;
+    a->ld_dy = d->ld_dy ? d->ld_dy : d->cols;
+    a->ld_dh = d->ld_dh ? d->ld_dh : d->cols;
+    a->ld_gate = d->ld_gate ? d->ld_gate : (d->gate_kind == SL_GATE_FULL ? d->cols : 1);
+}
+
+// Vectors of 16 bytes need them everywhere: columns, row strides, pointers (weights are read 16 bytes at a time too).
+struct NormAlign {
+    int bytes;
+    bool element, vector;
+    explicit NormAlign(const sl_norm_desc* d) : bytes(dtype_bytes(d->dtype)), element(true), vector(d->cols % (16 / dtype_bytes(d->dtype)) == 0) {}
+    void matrix(const void* p, long long ld) {
+        if (!p) return;
+        element = element && fits(p, bytes);
+        vector = vector && fits(p, 16) && ld % (16 / bytes) == 0;
+    }
+    void vec(const void* p, int b) {
+        if (!p) return;
+        element = element && fits(p, b);
+        vector = vector && fits(p, 16);
+    }
+};
+
+// CTAs of the backward kernel: their column sums are written once and added up afterwards, so not more than stay resident
+unsigned norm_backward_grid(const NormShape& s, long long rows, int n_sms) {
+    const long long want = (rows + s.rows_per_cta - 1) / s.rows_per_cta;
+    const int threads = s.threads * s.rows_per_cta;
+    const long long most = (long long)n_sms * std::max(1, std::min(4, 768 / threads));
+    return (unsigned)std::min(want, most);
+}
+
+// ---- rotary
+template <class T, int VEC>
+sl_status launch_rotary(const RopeArgs& a, bool half, unsigned grid, size_t smem, cudaStream_t st) {
+    if (half) rotary_kernel<T, VEC, true><<<grid, kRopeThreads, smem, st>>>(a);
+    else rotary_kernel<T, VEC, false><<<grid, kRopeThreads, smem, st>>>(a);
+    SL_CUDA(cudaGetLastError());
+    return SL_OK;
+}
+
+bool overlaps_no(const sl_tensor_desc* tensors, int n) {
+    std::vector<std::pair<long long, long long>> span((size_t)n);
+    for (int j = 0; j < n; ++j) span[(size_t)j] = {(long long)tensors[j].offset, (long long)tensors[j].offset + tensors[j].rows * tensors[j].cols};
+    std::sort(span.begin(), span.end());
+    for (int j = 1; j < n; ++j)
+        if (span[(size_t)j].first < span[(size_t)j - 1].second) return false;
+    return true;
+}
+
+void adamw_free(sl_adamw* c) {
+    cudaFree(c->d_tiles);
+    cudaFree(c->d_decay);
+    cudaFree(c->d_parts);
+    cudaFree(c->d_clip);
+    delete c;
+}
+
+sl_status adamw_upload(sl_adamw* c, const std::vector<AdamTile>& tiles, const float* decay, int n) {
+    SL_CUDA(cudaMalloc(&c->d_tiles, tiles.size() * sizeof(AdamTile)));
+    SL_CUDA(cudaMalloc(&c->d_decay, (size_t)n * sizeof(float)));
+    SL_CUDA(cudaMalloc(&c->d_parts, kAdamMaxParts * sizeof(double)));
+    SL_CUDA(cudaMalloc(&c->d_clip, sizeof(AdamClip)));
+    SL_CUDA(cudaMemcpy(c->d_tiles, tiles.data(), tiles.size() * sizeof(AdamTile), cudaMemcpyHostToDevice));
+    SL_CUDA(cudaMemcpy(c->d_decay, decay, (size_t)n * sizeof(float), cudaMemcpyHostToDevice));
+    SL_CUDA(cudaMemset(c->d_clip, 0, sizeof(AdamClip)));
+    SL_CUDA(cudaDeviceSynchronize());
+    return SL_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+sl_status sl_adamw_create(const sl_adamw_config* cfg, const sl_tensor_desc* tensors, const float* weight_decay, int32_t n_tensors, sl_adamw** out) {
+    if (!out) return SL_ERR_INVALID_ARG;
+    *out = nullptr;
+    if (!cfg || !tensors || !weight_decay || n_tensors < 1) return SL_ERR_INVALID_ARG;
+    if (!(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0) || !(cfg->beta2 >= 0.0 && cfg->beta2 < 1.0)) return SL_ERR_INVALID_ARG;
+    if (!finite_at_least(cfg->eps, 0.0) || !finite_at_least(cfg->max_norm, 0.0)) return SL_ERR_INVALID_ARG;
+    if (cfg->skip_nonfinite != 0 && cfg->skip_nonfinite != 1) return SL_ERR_INVALID_ARG;
+    if ((cfg->state_bits != 32 && cfg->state_bits != 8) || !known_dtype(cfg->param_dtype) || !known_dtype(cfg->grad_dtype)) return SL_ERR_UNSUPPORTED;
+    long long total = 0;
+    for (int j = 0; j < n_tensors; ++j) {
+        const sl_tensor_desc& t = tensors[j];
+        if (t.rows < 1 || t.cols < 1 || t.offset < 0 || !finite_at_least(weight_decay[j], 0.0)) return SL_ERR_INVALID_ARG;
+        if (t.rows > (1ll << 40) / t.cols || t.offset > (1ll << 46)) return SL_ERR_TOO_LARGE;
+        if (t.offset % 4 != 0) return SL_ERR_ALIGNMENT;
+        total += (t.rows * t.cols + kAdamTile - 1) / kAdamTile;
+        if (total > 0x7FFFFFFFll) return SL_ERR_TOO_LARGE;
+    }
+    try {
+        if (!overlaps_no(tensors, n_tensors)) return SL_ERR_INVALID_ARG;
+        std::vector<AdamTile> tiles;
+        tiles.reserve((size_t)total);
+        long long blocks = 0, flat = 0;
+        bool a8 = true;
+        for (int j = 0; j < n_tensors; ++j) {
+            const long long n = tensors[j].rows * tensors[j].cols, off = tensors[j].offset;
+            a8 = a8 && off % 8 == 0;
+            flat = std::max(flat, off + n);
+            for (long long i = 0; i < n; i += kAdamTile) {
+                AdamTile t;
+                t.base = off + i;
+                t.block0 = blocks + i / kAdamBlock;
+                t.len = (int)std::min((long long)kAdamTile, n - i);
+                t.tensor = j;
+                t.pad = 0;
+                tiles.push_back(t);
+            }
+            blocks += (n + kAdamBlock - 1) / kAdamBlock;
+        }
+        sl_adamw* c = new (std::nothrow) sl_adamw();
+        if (!c) return SL_ERR_NOMEM;
+        c->cfg = *cfg;
+        c->aligned8 = a8;
+        c->n_tiles = total;
+        c->blocks = blocks;
+        c->flat_elems = flat;
+        sl_status s = SL_OK;
+        const cudaError_t e = cudaGetDevice(&c->device);
+        s = e == cudaSuccess ? sm_count(&c->n_sms) : cuda_fail(e, "cudaGetDevice");
+        if (s == SL_OK) s = adamw_upload(c, tiles, weight_decay, n_tensors);
+        if (s != SL_OK) {
+            adamw_free(c);
+            return s;
+        }
+        *out = c;
+        return SL_OK;
+    } catch (const std::bad_alloc&) {
+        return SL_ERR_NOMEM;
+    }
+}
+
+sl_status sl_adamw_destroy(sl_adamw* c) {
+    if (!c) return SL_ERR_INVALID_ARG;
+    DeviceGuard g(c->device);
+    const cudaError_t e = cudaDeviceSynchronize();
+    adamw_free(c);
+    return e == cudaSuccess ? SL_OK : cuda_fail(e, "cudaDeviceSynchronize");
+}
+
+sl_status sl_adamw_sizes(const sl_adamw* c, int64_t* flat_elems, int64_t* blocks) {
+    if (!c || !flat_elems || !blocks) return SL_ERR_INVALID_ARG;
+    *flat_elems = c->flat_elems;
+    *blocks = c->blocks;
+    return SL_OK;
+}
+
+sl_status sl_adamw_step(sl_adamw* c, void* theta, const void* grad, void* m, void* v, uint8_t* scales, uint16_t* copy, float* norm, int64_t step,
+                        double lr, double grad_scale, uint32_t seed, void* stream) {
+    if (!c || !theta || !grad || !m || !v || step < 1 || !isfinite(lr) || !isfinite(grad_scale)) return SL_ERR_INVALID_ARG;
+    if ((c->cfg.state_bits == 8) != (scales != nullptr)) return SL_ERR_INVALID_ARG;
+    if (copy && c->cfg.param_dtype != SL_F32) return SL_ERR_INVALID_ARG;
+    const void* p[] = {theta, grad, m, v, scales, copy};
+    for (int i = 0; i < 6; ++i)
+        for (int j = 0; j < i; ++j)
+            if (p[i] && p[i] == p[j]) return SL_ERR_INVALID_ARG;
+    for (const void* x : p)
+        if (misaligned(x)) return SL_ERR_ALIGNMENT;
+    if (!fits(norm, 4)) return SL_ERR_ALIGNMENT;
+    DeviceGuard guard(c->device);
+    if (!guard.ok) return SL_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    AdamArgs a;
+    memset(&a, 0, sizeof(a));
+    a.theta = theta;
+    a.grad = grad;
+    a.m = m;
+    a.v = v;
+    a.scales = scales;
+    a.copy = reinterpret_cast<bf16*>(copy);
+    a.blocks = c->blocks;
+    a.coef = (float)grad_scale;
+    a.beta1 = (float)c->cfg.beta1;
+    a.omb1 = (float)(1.0 - c->cfg.beta1);
+    a.beta2 = (float)c->cfg.beta2;
+    a.omb2 = (float)(1.0 - c->cfg.beta2);
+    a.eps = (float)c->cfg.eps;
+    a.inv_sqrt_bc2 = (float)(1.0 / sqrt(1.0 - pow(c->cfg.beta2, (double)step)));
+    a.step_size = (float)(lr / (1.0 - pow(c->cfg.beta1, (double)step)));
+    a.lr = (float)lr;
+    a.seed = seed;
+    a.skip = c->cfg.skip_nonfinite;
+    if (c->cfg.max_norm > 0.0 || c->cfg.skip_nonfinite || norm) {
+        sl_status s = c->cfg.grad_dtype == SL_F32 ? launch_adamw_norm<float>(c, grad, grad_scale, norm, st) : launch_adamw_norm<bf16>(c, grad, grad_scale, norm, st);
+        if (s != SL_OK) return s;
+        a.clip = c->d_clip;
+    }
+    if (c->cfg.param_dtype == SL_F32) return c->cfg.grad_dtype == SL_F32 ? launch_adamw_bits<float, float>(c, a, st) : launch_adamw_bits<float, bf16>(c, a, st);
+    return c->cfg.grad_dtype == SL_F32 ? launch_adamw_bits<bf16, float>(c, a, st) : launch_adamw_bits<bf16, bf16>(c, a, st);
+}
+
+static sl_status adamw_state(sl_adamw* c, bool write, float* m32, float* v32, uint8_t* m8, uint8_t* v8, uint8_t* scales, uint32_t seed, void* stream) {
+    if (!c || !m32 || !v32 || !m8 || !v8 || !scales) return SL_ERR_INVALID_ARG;
+    if (c->cfg.state_bits != 8) return SL_ERR_UNSUPPORTED;
+    const void* p[] = {m32, v32, m8, v8, scales};
+    for (int i = 0; i < 5; ++i) {
+        for (int j = 0; j < i; ++j)
+            if (p[i] == p[j]) return SL_ERR_INVALID_ARG;
+        if (misaligned(p[i])) return SL_ERR_ALIGNMENT;
+    }
+    DeviceGuard guard(c->device);
+    if (!guard.ok) return SL_ERR_CUDA;
+    auto kern = write ? (c->aligned8 ? adamw_state_kernel<true, true> : adamw_state_kernel<true, false>)
+                      : (c->aligned8 ? adamw_state_kernel<false, true> : adamw_state_kernel<false, false>);
+    kern<<<(unsigned)c->n_tiles, kAdamThreads, 0, static_cast<cudaStream_t>(stream)>>>(c->d_tiles, m32, v32, m8, v8, scales, c->blocks, seed);
+    SL_CUDA(cudaGetLastError());
+    return SL_OK;
+}
+
+sl_status sl_adamw_read_state(sl_adamw* c, const uint8_t* m, const uint8_t* v, const uint8_t* scales, float* m_out, float* v_out, void* stream) {
+    return adamw_state(c, false, m_out, v_out, const_cast<uint8_t*>(m), const_cast<uint8_t*>(v), const_cast<uint8_t*>(scales), 0u, stream);
+}
+
+sl_status sl_adamw_write_state(sl_adamw* c, const float* m_in, const float* v_in, uint8_t* m, uint8_t* v, uint8_t* scales, uint32_t seed, void* stream) {
+    return adamw_state(c, true, const_cast<float*>(m_in), const_cast<float*>(v_in), m, v, scales, seed, stream);
+}
+
+sl_status sl_norm_forward(const sl_norm_desc* d, const void* x, const void* branch, const void* branch_weight, const void* gate, const void* weight,
+                          void* y, void* h, float* branch_rstd, float* rstd, void* stream) {
+    sl_status s = norm_check(d);
+    if (s != SL_OK || d->rows == 0) return s;  // (matrices without rows have no address to check)
+    if (!x || (!y && !h) || (branch != nullptr) != (y != nullptr) || (branch_weight && !branch) || (weight && !h)) return SL_ERR_INVALID_ARG;
+    if ((d->gate_kind != SL_GATE_NONE) != (gate != nullptr) || (gate && !branch)) return SL_ERR_INVALID_ARG;
+    NormArgs a;
+    norm_strides(d, &a);
+    a.x = x;
+    a.branch = branch;
+    a.branch_weight = branch_weight;
+    a.gate = gate;
+    a.weight = weight;
+    a.y = y;
+    a.h = h;
+    a.branch_rstd = branch_rstd;
+    a.rstd = rstd;
+    const int wb = dtype_bytes(d->weight_dtype);
+    NormAlign al(d);
+    al.matrix(x, a.ld_x);
+    al.matrix(branch, a.ld_branch);
+    al.matrix(y, a.ld_y);
+    al.matrix(h, a.ld_h);
+    al.vec(branch_weight, wb);
+    al.vec(weight, wb);
+    if (d->gate_kind == SL_GATE_COLUMN) al.vec(gate, wb);
+    else if (d->gate_kind == SL_GATE_FULL) al.matrix(gate, a.ld_gate);
+    else if (!fits(gate, al.bytes)) return SL_ERR_ALIGNMENT;
+    if (!al.element || !fits(branch_rstd, 4) || !fits(rstd, 4)) return SL_ERR_ALIGNMENT;
+    const NormShape sh = norm_shape(a.cols, al.vector ? 16 / al.bytes : 1, false);
+    const unsigned grid = (unsigned)((d->rows + sh.rows_per_cta - 1) / sh.rows_per_cta);
+    return launch_norm_types(d, a, sh, grid, false, static_cast<cudaStream_t>(stream));
+}
+
+sl_status sl_norm_workspace_bytes(const sl_norm_desc* d, size_t* bytes) {
+    sl_status s = norm_check(d);
+    if (s != SL_OK) return s;
+    if (!bytes) return SL_ERR_INVALID_ARG;
+    int n_sms = 0;
+    s = sm_count(&n_sms);
+    if (s != SL_OK) return s;
+    // the larger of the two launch shapes that alignment decides between
+    size_t most = 0;
+    for (int vec : {1, 16 / dtype_bytes(d->dtype)}) {
+        const NormShape sh = norm_shape((int)d->cols, vec, true);
+        most = std::max(most, sizeof(float) * 3 * (size_t)d->cols * norm_backward_grid(sh, d->rows, n_sms));
+    }
+    *bytes = up256(most);
+    return SL_OK;
+}
+
+sl_status sl_norm_backward(const sl_norm_desc* d, const void* dy, const void* dh, const void* y, const void* branch, const void* branch_weight,
+                           const void* gate, const void* weight, const float* branch_rstd, const float* rstd, void* dx, void* dbranch, void* dweight,
+                           void* dbranch_weight, void* dgate, void* workspace, size_t workspace_bytes, void* stream) {
+    sl_status s = norm_check(d);
+    if (s != SL_OK) return s;
+    const bool rows = d->rows > 0;  // (matrices without rows have no address to check)
+    if (rows && ((!dy && !dh) || (dh && (!y || !rstd)) || (branch_weight && (!branch || !branch_rstd)) || (weight && !dh))) return SL_ERR_INVALID_ARG;
+    if (rows && ((d->gate_kind != SL_GATE_NONE) != (gate != nullptr) || (gate && !branch) || (dbranch && !branch))) return SL_ERR_INVALID_ARG;
+    if ((dweight && !weight) || (dbranch_weight && !branch_weight) || (rows && dgate && !gate)) return SL_ERR_INVALID_ARG;
+    if (rows && !dx && !dbranch && !dweight && !dbranch_weight && !dgate) return SL_ERR_INVALID_ARG;
+    NormArgs a;
+    norm_strides(d, &a);
+    a.dy = dy;
+    a.dh = dh;
+    a.x = y;
+    a.branch = branch;
+    a.branch_weight = branch_weight;
+    a.gate = gate;
+    a.weight = weight;
+    a.branch_rstd = const_cast<float*>(branch_rstd);
+    a.rstd = const_cast<float*>(rstd);
+    a.dx = dx;
+    a.dbranch = dbranch;
+    a.dgate = d->gate_kind == SL_GATE_COLUMN ? nullptr : dgate;
+    const int wb = dtype_bytes(d->weight_dtype);
+    NormAlign al(d);
+    al.matrix(dy, a.ld_dy);
+    al.matrix(dh, a.ld_dh);
+    if (dh) al.matrix(y, a.ld_y);
+    al.matrix(branch, a.ld_branch);
+    al.matrix(dx, a.ld_x);
+    al.matrix(dbranch, a.ld_branch);
+    al.vec(branch_weight, wb);
+    al.vec(weight, wb);
+    if (d->gate_kind == SL_GATE_COLUMN) al.vec(gate, wb);
+    else if (d->gate_kind == SL_GATE_FULL) al.matrix(gate, a.ld_gate), al.matrix(dgate, a.ld_gate);
+    else if (!fits(gate, al.bytes) || !fits(dgate, al.bytes)) return SL_ERR_ALIGNMENT;
+    if (!al.element || !fits(branch_rstd, 4) || !fits(rstd, 4) || !fits(dweight, wb) || !fits(dbranch_weight, wb) || misaligned(workspace) ||
+        (d->gate_kind == SL_GATE_COLUMN && !fits(dgate, wb)))
+        return SL_ERR_ALIGNMENT;
+    const bool columns = dweight || dbranch_weight || (d->gate_kind == SL_GATE_COLUMN && dgate);
+    int n_sms = 0;
+    s = sm_count(&n_sms);
+    if (s != SL_OK) return s;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const NormShape sh = norm_shape(a.cols, al.vector ? 16 / al.bytes : 1, true);
+    const unsigned grid = norm_backward_grid(sh, d->rows, n_sms);
+    if (columns) {
+        if (grid && (!workspace || workspace_bytes < sizeof(float) * 3 * (size_t)a.cols * grid)) return SL_ERR_NOMEM;
+        a.part = static_cast<float*>(workspace);
+    }
+    if (grid) {
+        s = launch_norm_types(d, a, sh, grid, true, st);
+        if (s != SL_OK) return s;
+    }
+    if (columns) {
+        const unsigned cg = (unsigned)((3 * a.cols + 31) / 32);
+        void* dg = d->gate_kind == SL_GATE_COLUMN ? dgate : nullptr;
+        if (d->weight_dtype == SL_F32)
+            norm_columns_kernel<float><<<cg, 256, 0, st>>>(a.part, (int)grid, a.cols, (float*)dweight, (float*)dbranch_weight, (float*)dg);
+        else
+            norm_columns_kernel<bf16><<<cg, 256, 0, st>>>(a.part, (int)grid, a.cols, (bf16*)dweight, (bf16*)dbranch_weight, (bf16*)dg);
+        SL_CUDA(cudaGetLastError());
+    }
+    return SL_OK;
+}
+
+sl_status sl_rotary_create(const sl_rotary_config* cfg, sl_rotary** out) {
+    if (!out) return SL_ERR_INVALID_ARG;
+    *out = nullptr;
+    if (!cfg || cfg->rot_dim < 2 || cfg->rot_dim % 2 || cfg->rot_dim > 1024) return SL_ERR_INVALID_ARG;
+    if (cfg->layout != SL_ROPE_HALF && cfg->layout != SL_ROPE_INTERLEAVED) return SL_ERR_INVALID_ARG;
+    if (cfg->scaling < SL_ROPE_PLAIN || cfg->scaling > SL_ROPE_BY_PARTS) return SL_ERR_INVALID_ARG;
+    if (!(isfinite(cfg->base) && cfg->base > 1.0) || !isfinite(cfg->magnitude)) return SL_ERR_INVALID_ARG;
+    if (cfg->scaling != SL_ROPE_PLAIN && !(finite_at_least(cfg->factor, 1.0))) return SL_ERR_INVALID_ARG;
+    if (cfg->scaling == SL_ROPE_BASE && cfg->rot_dim < 4) return SL_ERR_INVALID_ARG;
+    if (cfg->scaling == SL_ROPE_BY_PARTS && !(finite_at_least(cfg->original_length, 1.0) && finite_at_least(cfg->low_turns, 0.0) && isfinite(cfg->high_turns) &&
+                                              cfg->high_turns > cfg->low_turns))
+        return SL_ERR_INVALID_ARG;
+    const int half = cfg->rot_dim / 2;
+    const long double two_pi = 6.283185307179586476925286766559005768L;
+    std::vector<unsigned long long> turns;
+    try {
+        turns.resize((size_t)half);
+    } catch (const std::bad_alloc&) {
+        return SL_ERR_NOMEM;
+    }
+    long double base = cfg->base;
+    if (cfg->scaling == SL_ROPE_BASE) base *= powl((long double)cfg->factor, (long double)cfg->rot_dim / (cfg->rot_dim - 2));
+    for (int i = 0; i < half; ++i) {
+        long double f = powl(base, -2.0L * i / cfg->rot_dim);
+        if (cfg->scaling == SL_ROPE_LINEAR) f /= cfg->factor;
+        if (cfg->scaling == SL_ROPE_BY_PARTS) {
+            long double k = (cfg->original_length * f / two_pi - cfg->low_turns) / ((long double)cfg->high_turns - cfg->low_turns);
+            k = k < 0.0L ? 0.0L : (k > 1.0L ? 1.0L : k);
+            f = f * k + f / cfg->factor * (1.0L - k);
+        }
+        // f <= 1 radian, so below a turn; the fraction keeps 64 bits behind the point
+        turns[(size_t)i] = (unsigned long long)(f / two_pi * 18446744073709551616.0L + 0.5L);
+    }
+    sl_rotary* c = new (std::nothrow) sl_rotary();
+    if (!c) return SL_ERR_NOMEM;
+    c->cfg = *cfg;
+    c->d_turns = nullptr;
+    cudaError_t e = cudaGetDevice(&c->device);
+    if (e == cudaSuccess) e = cudaMalloc(&c->d_turns, turns.size() * sizeof(unsigned long long));
+    if (e == cudaSuccess) e = cudaMemcpy(c->d_turns, turns.data(), turns.size() * sizeof(unsigned long long), cudaMemcpyHostToDevice);
+    if (e != cudaSuccess) {
+        cudaFree(c->d_turns);
+        delete c;
+        return cuda_fail(e, "sl_rotary_create");
+    }
+    *out = c;
+    return SL_OK;
+}
+
+sl_status sl_rotary_destroy(sl_rotary* c) {
+    if (!c) return SL_ERR_INVALID_ARG;
+    DeviceGuard g(c->device);
+    const cudaError_t e = cudaDeviceSynchronize();
+    cudaFree(c->d_turns);
+    delete c;
+    return e == cudaSuccess ? SL_OK : cuda_fail(e, "cudaDeviceSynchronize");
+}
+
+sl_status sl_rotary_apply(sl_rotary* c, const sl_rotary_desc* d, const sl_rotary_heads* q, const sl_rotary_heads* k, const void* positions, void* stream) {
+    if (!c || !d || !q || !q->in || !q->out) return SL_ERR_INVALID_ARG;
+    if (!known_dtype(d->dtype)) return SL_ERR_UNSUPPORTED;
+    if (d->batch < 0 || d->seq < 0 || d->head_dim < c->cfg.rot_dim || q->heads < 1) return SL_ERR_INVALID_ARG;
+    if (positions && d->position_bits != 32 && d->position_bits != 64) return SL_ERR_INVALID_ARG;
+    const sl_rotary_heads none = {nullptr, nullptr, 0, 0, 0, 0, 0, 0, 0};
+    if (!k) k = &none;
+    if ((k->in != nullptr) != (k->out != nullptr) || (k->in != nullptr) != (k->heads != 0) || k->heads < 0) return SL_ERR_INVALID_ARG;
+    if (d->head_dim > 65536 || d->seq > 0x7FFFFFFFll || d->batch > 0x7FFFFFFFll || d->batch * d->seq > 0x7FFFFFFFll || q->heads > 65536 ||
+        k->heads > 65536 || (q->heads + k->heads) * d->head_dim > (1ll << 27))
+        return SL_ERR_TOO_LARGE;
+    const int bytes = dtype_bytes(d->dtype), rot = c->cfg.rot_dim;
+    const bool half = c->cfg.layout == SL_ROPE_HALF;
+    // the widest access that every offset of a turned or copied part is a multiple of
+    int vec = 16 / bytes;
+    const int64_t parts[] = {half ? rot / 2 : rot, d->head_dim - rot};
+    auto divides = [&](int v) {
+        for (int64_t p : parts)
+            if (p % v) return false;
+        for (const sl_rotary_heads* h : {q, k}) {
+            if (!h->in) continue;
+            for (int64_t st : {h->in_batch, h->in_token, h->in_head, h->out_batch, h->out_token, h->out_head})
+                if (st % v) return false;
+            if (!fits(h->in, v * bytes) || !fits(h->out, v * bytes)) return false;
+        }
+        return true;
+    };
+    while (vec > 1 && !divides(vec)) vec /= 2;
+    for (const sl_rotary_heads* h : {q, k})
+        if (!fits(h->in, bytes) || !fits(h->out, bytes)) return SL_ERR_ALIGNMENT;
+    if (positions && !fits(positions, d->position_bits / 8)) return SL_ERR_ALIGNMENT;
+    DeviceGuard guard(c->device);
+    if (!guard.ok) return SL_ERR_CUDA;
+    RopeArgs a;
+    memset(&a, 0, sizeof(a));
+    auto heads = [](const sl_rotary_heads* h) {
+        RopeHeads r = {h->in, h->out, (int)h->heads, h->in_batch, h->in_token, h->in_head, h->out_batch, h->out_token, h->out_head};
+        return r;
+    };
+    a.q = heads(q);
+    a.k = heads(k);
+    a.turns = c->d_turns;
+    a.positions = positions;
+    a.pos_batch = d->pos_batch;
+    a.pos_token = d->pos_token;
+    a.first = d->first;
+    a.rows = d->batch * d->seq;
+    a.position_bits = d->position_bits;
+    a.seq = (int)d->seq;
+    a.head_dim = (int)d->head_dim;
+    a.rot = rot;
+    a.magnitude = (float)c->cfg.magnitude;
+    a.sign = d->inverse ? -1.0f : 1.0f;
+    a.rot_slots = half ? rot / 2 / vec : (vec > 1 ? rot / vec : rot / 2);
+    a.slots = a.rot_slots + (int)(d->head_dim - rot) / vec;
+    if (a.rows == 0) return SL_OK;
+    int n_sms = 0;
+    sl_status s = sm_count(&n_sms);
+    if (s != SL_OK) return s;
+    // more tokens per CTA even out its last round of accesses; few tokens are spread over the SMs first
+    a.tokens = (int)std::max(1ll, std::min(8ll, (long long)(a.rows / (4 * n_sms))));
+    const unsigned grid = (unsigned)((a.rows + a.tokens - 1) / a.tokens);
+    const size_t smem = sizeof(float2) * (size_t)a.tokens * (rot / 2);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (d->dtype == SL_F32)
+        return vec == 4 ? launch_rotary<float, 4>(a, half, grid, smem, st) : vec == 2 ? launch_rotary<float, 2>(a, half, grid, smem, st) : launch_rotary<float, 1>(a, half, grid, smem, st);
+    return vec == 8 ? launch_rotary<bf16, 8>(a, half, grid, smem, st) : vec == 4 ? launch_rotary<bf16, 4>(a, half, grid, smem, st)
+         : vec == 2 ? launch_rotary<bf16, 2>(a, half, grid, smem, st) : launch_rotary<bf16, 1>(a, half, grid, smem, st);
+}
+
+size_t sl_loss_workspace_bytes(void) { return 256; }
+
+sl_status sl_token_loss(const sl_loss_desc* d, const void* logits, const void* targets, void* grad, float* row_loss, float* lse, float* total,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+    if (!d || d->rows < 0 || d->vocab < 1) return SL_ERR_INVALID_ARG;
+    if (!known_dtype(d->dtype) || (d->target_bits != 32 && d->target_bits != 64)) return SL_ERR_UNSUPPORTED;
+    if (d->rows > 0 && (!logits || !targets || !row_loss)) return SL_ERR_INVALID_ARG;
+    if (!(d->smoothing >= 0.0f && d->smoothing <= 1.0f) || !isfinite(d->z) || !isfinite(d->scale)) return SL_ERR_INVALID_ARG;
+    if (d->vocab > (1ll << 30) || d->rows > 0x7FFFFFFFll) return SL_ERR_TOO_LARGE;
+    if ((d->ld_logits != 0 && d->ld_logits < d->vocab) || (d->ld_grad != 0 && d->ld_grad < d->vocab)) return SL_ERR_INVALID_ARG;
+    const int bytes = dtype_bytes(d->dtype);
+    if (!fits(logits, bytes) || !fits(grad, bytes) || !fits(targets, d->target_bits / 8) || !fits(row_loss, 4) || !fits(lse, 4) || !fits(total, 4) ||
+        misaligned(workspace))
+        return SL_ERR_ALIGNMENT;
+    if (!workspace || workspace_bytes < sizeof(LossWork)) return SL_ERR_NOMEM;
+    LossArgs a;
+    memset(&a, 0, sizeof(a));
+    a.rows = d->rows;
+    a.ld_logits = d->ld_logits ? d->ld_logits : d->vocab;
+    a.ld_grad = d->ld_grad ? d->ld_grad : d->vocab;
+    if (grad && grad == logits && a.ld_grad != a.ld_logits) return SL_ERR_INVALID_ARG;
+    a.ignore_index = d->ignore_index;
+    a.vocab = (int)d->vocab;
+    a.target_bits = d->target_bits;
+    a.mean = d->mean;
+    a.smoothing = d->smoothing;
+    a.z = d->z;
+    a.scale = d->scale;
+    a.targets = targets;
+    a.row_loss = row_loss;
+    a.lse = lse;
+    a.total = total;
+    a.work = static_cast<LossWork*>(workspace);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    loss_count_kernel<<<1, 1024, 0, st>>>(a);
+    SL_CUDA(cudaGetLastError());
+    if (d->rows == 0) return SL_OK;
+    // 16-byte accesses from the first boundary of a row on: every row of logits and gradient has to meet it at the same column
+    const bool same = !grad || ((reinterpret_cast<uintptr_t>(logits) - reinterpret_cast<uintptr_t>(grad)) % 16 == 0 && (a.ld_logits - a.ld_grad) * bytes % 16 == 0);
+    const unsigned grid = (unsigned)d->rows;
+    if (d->dtype == SL_F32) {
+        if (same) token_loss_kernel<float, 4><<<grid, kLossThreads, 0, st>>>(a, (const float*)logits, (float*)grad);
+        else token_loss_kernel<float, 1><<<grid, kLossThreads, 0, st>>>(a, (const float*)logits, (float*)grad);
+    } else {
+        if (same) token_loss_kernel<bf16, 8><<<grid, kLossThreads, 0, st>>>(a, (const bf16*)logits, (bf16*)grad);
+        else token_loss_kernel<bf16, 1><<<grid, kLossThreads, 0, st>>>(a, (const bf16*)logits, (bf16*)grad);
+    }
+    SL_CUDA(cudaGetLastError());
+    return SL_OK;
+}
+
+}  // extern "C"

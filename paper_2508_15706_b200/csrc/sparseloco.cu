@@ -1,5 +1,6 @@
 // SparseLoCo outer step for sm_100a: the C ABI declared in include/sparseloco.h (host side, this
-// file) over the kernels in the .cuh files beside it (one translation unit).
+// file) over the kernels in the .cuh files beside it (one translation unit; the operators of the inner phase are
+// another, inner.cu).
 //
 // Kernel sequence of one outer step (all on the caller's stream, no host synchronisation):
 //   ef_select.cuh    ef_select_kernel         pseudo-gradient + error feedback + chunk-wise Top-k
@@ -37,6 +38,7 @@
 #include "sparseloco.h"
 
 #include "common.cuh"
+#include "host.cuh"
 #include "ef_select.cuh"
 #include "quantiser.cuh"
 #include "pack.cuh"
@@ -50,6 +52,8 @@
 // ================================================================================================
 // Host side
 // ================================================================================================
+
+thread_local char sl_cuda_err[256] = "";
 
 struct sl_ctx {
     sl_config cfg;
@@ -119,18 +123,6 @@ TmaEncodeFn tma_encode_fn() {
     return fn;
 }
 
-sl_status cuda_fail(cudaError_t e, const char* what) {
-    snprintf(g_cuda_err, sizeof(g_cuda_err), "%s: %s", what, cudaGetErrorString(e));
-    return SL_ERR_CUDA;
-}
-#define SL_CUDA(call)                                      \
-    do {                                                   \
-        cudaError_t e_ = (call);                           \
-        if (e_ != cudaSuccess) return cuda_fail(e_, #call); \
-    } while (0)
-
-inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
-
 // general-width quantiser (quant_bits 1, 3, 4): its per-unit bin partials and per-tensor tables follow
 // the arrays of the 2-bit path in the workspace
 // (also the 2-bit quantiser at k > 256, which the fused kernels are not laid out for)
@@ -183,8 +175,6 @@ Workspace carve(const sl_ctx* c, int workers) {
     w.tstat = reinterpret_cast<TStat*>(p);
     return w;
 }
-
-inline bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 
 unsigned blocks_for(long long items, int per_block) { return (unsigned)((items + per_block - 1) / per_block); }
 
@@ -594,19 +584,6 @@ sl_status launch_apply_coded(sl_ctx* c, const PayloadPtrs& pl, const size_t* cod
     return SL_OK;
 }
 
-struct DeviceGuard {
-    int prev;
-    bool ok;
-    explicit DeviceGuard(int dev) : prev(-1), ok(false) {
-        if (cudaGetDevice(&prev) != cudaSuccess) return;
-        ok = prev == dev || cudaSetDevice(dev) == cudaSuccess;
-    }
-    ~DeviceGuard() {
-        int cur = -1;
-        if (prev >= 0 && cudaGetDevice(&cur) == cudaSuccess && cur != prev) cudaSetDevice(prev);
-    }
-};
-
 }  // namespace
 
 extern "C" {
@@ -626,7 +603,7 @@ const char* sl_strerror(sl_status s) {
     return "unknown status";
 }
 
-const char* sl_last_cuda_error(void) { return g_cuda_err; }
+const char* sl_last_cuda_error(void) { return sl_cuda_err; }
 
 size_t sl_record_stride(int32_t k) { return k < 1 ? 0 : (size_t)record_stride(k); }
 
