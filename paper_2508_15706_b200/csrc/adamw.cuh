@@ -46,7 +46,7 @@ __device__ __forceinline__ unsigned mix32(unsigned x) {
 __device__ __forceinline__ unsigned hash_key(unsigned seed, unsigned long long i) {
     return mix32(seed) ^ mix32((unsigned)(i >> 32) * 0x9E3779B9u);
 }
-__device__ __forceinline__ unsigned lot19(unsigned key, unsigned long long i) { return mix32((unsigned)i ^ key) >> 13; }
+__device__ __forceinline__ unsigned lot19(unsigned key, unsigned i) { return mix32(i ^ key) >> 13; }
 
 __device__ __forceinline__ float finite_abs(float x) {
     const float a = fabsf(x);
@@ -67,19 +67,22 @@ __device__ __forceinline__ int scale_byte_v(float top) {
     const int e = (int)(b >> 23) + ((b & 0x7FFFFFu) > 0x780000u);  // at most 31/16, the largest code's value: rounding up is never cut off
     return e < 1 ? 1 : (e > 254 ? 254 : e);
 }
-__device__ __forceinline__ unsigned code_v(float v, float inv, unsigned lot) {
-    const float s = v * inv;  // a power of two: exact
-    if (s == 0.0f) return 0u;
-    if (!(s <= 3.402823466e38f)) return 255u;
-    const int c = (int)((__float_as_uint(s) + lot) >> 19) - 1792;  // the exponent and the first 4 mantissa bits
-    return (unsigned)(c < 1 ? 1 : (c > 255 ? 255 : c));
+// Code of a finite v >= 0 in units of its scale, at most 31/16: the exponent and the first 4 mantissa bits after the lot is added
+// below them; what lies under the smallest code becomes it, only 0 becomes 0.
+__device__ __forceinline__ unsigned code_v(float scaled, unsigned lot) {
+    const unsigned b = __float_as_uint(scaled);
+    const int c = (int)(b + lot - (1792u << 19)) >> 19, least = (int)min(b, 1u);
+    return (unsigned)max(c, least);
 }
-__device__ __forceinline__ float value_v(unsigned c) { return c ? __uint_as_float((c + 1792u) << 19) : 0.0f; }
-__device__ __forceinline__ unsigned code_m2(float a, float b) {
-    unsigned c = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
-    if (!(fabsf(a) <= 3.402823466e38f)) c |= 0x007Fu;  // no infinity in the format: NaN
-    if (!(fabsf(b) <= 3.402823466e38f)) c |= 0x7F00u;
-    return c;
+// ... of any value: what is not finite becomes 255
+__device__ __forceinline__ unsigned code_v_any(float scaled, unsigned lot) { return scaled <= 3.402823466e38f ? min(code_v(scaled, lot), 255u) : 255u; }
+__device__ __forceinline__ float value_v(unsigned c) {
+    const float f = __uint_as_float((c << 19) + (1792u << 19));
+    return c ? f : 0.0f;
+}
+__device__ __forceinline__ unsigned code_m2(float a, float b) { return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3); }
+__device__ __forceinline__ unsigned code_m2_any(float a, float b) {  // no infinity in the format: NaN
+    return code_m2(a, b) | (fabsf(a) <= 3.402823466e38f ? 0u : 0x007Fu) | (fabsf(b) <= 3.402823466e38f ? 0u : 0x7F00u);
 }
 __device__ __forceinline__ float2 value_m2(unsigned c) {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)c, __NV_E4M3);
@@ -87,16 +90,17 @@ __device__ __forceinline__ float2 value_m2(unsigned c) {
 }
 
 // 8 elements at p; A8: p is aligned to 8 elements, else to 4 only.
-template <class T, bool A8>
+template <class T, bool A8, bool STREAM = true>
 __device__ __forceinline__ void load8(const T* p, float (&f)[kAdamVec]) {
     if (A8) {
         Pack<T, 8> a;
-        a.load_stream(p);
+        if (STREAM) a.load_stream(p);
+        else a.load(p);
         a.get(f);
     } else {
         Pack<T, 4> a, b;
-        a.load_stream(p);
-        b.load_stream(p + 4);
+        if (STREAM) a.load_stream(p), b.load_stream(p + 4);
+        else a.load(p), b.load(p + 4);
 #pragma unroll
         for (int i = 0; i < 4; ++i) f[i] = widen(a.v[i]), f[i + 4] = widen(b.v[i]);
     }
@@ -182,11 +186,21 @@ __device__ __forceinline__ void values_v(uint2 w, float scale, float (&v)[kAdamV
 // Codes of the thread's 8 moments; the 16 threads of a block agree on its scales.  Every lane of the warp takes part.
 __device__ __forceinline__ void encode_moments(const float (&m)[kAdamVec], const float (&v)[kAdamVec], unsigned seed, unsigned long long at,
                                                uint2& cm, uint2& cv, int& bm, int& bv) {
-    float tm = 0.0f, tv = 0.0f;
+    float tm = 0.0f, tv = 0.0f, odd = 0.0f;  // odd: 0, or NaN where a moment is not finite
 #pragma unroll
     for (int i = 0; i < kAdamVec; ++i) {
-        tm = fmaxf(tm, finite_abs(m[i]));
-        tv = fmaxf(tv, finite_abs(v[i]));
+        tm = fmaxf(tm, fabsf(m[i]));
+        tv = fmaxf(tv, v[i]);
+        odd = fmaf(m[i], 0.0f, fmaf(v[i], 0.0f, odd));
+    }
+    const bool all_finite = __all_sync(kFullMask, odd == 0.0f);
+    if (!all_finite) {
+        tm = tv = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kAdamVec; ++i) {
+            tm = fmaxf(tm, finite_abs(m[i]));
+            tv = fmaxf(tv, finite_abs(v[i]));
+        }
     }
 #pragma unroll
     for (int o = 8; o; o >>= 1) {
@@ -196,16 +210,22 @@ __device__ __forceinline__ void encode_moments(const float (&m)[kAdamVec], const
     bm = scale_byte_m(tm);
     bv = scale_byte_v(tv);
     const float im = inv_pow2_byte(bm), iv = inv_pow2_byte(bv);
-    cm.x = code_m2(m[0] * im, m[1] * im) | (code_m2(m[2] * im, m[3] * im) << 16);
-    cm.y = code_m2(m[4] * im, m[5] * im) | (code_m2(m[6] * im, m[7] * im) << 16);
-    cv = make_uint2(0u, 0u);
     // (8 consecutive offsets that begin at a multiple of 4 may cross a multiple of 2^32)
-    const unsigned key0 = hash_key(seed, at), key1 = hash_key(seed, at + 4);
+    const unsigned low = (unsigned)at, key0 = hash_key(seed, at), key1 = hash_key(seed, at + 4);
+    unsigned c[kAdamVec];
+    if (all_finite && bv < 254) {
+        cm.x = code_m2(m[0] * im, m[1] * im) | (code_m2(m[2] * im, m[3] * im) << 16);
+        cm.y = code_m2(m[4] * im, m[5] * im) | (code_m2(m[6] * im, m[7] * im) << 16);
 #pragma unroll
-    for (int i = 0; i < kAdamVec; ++i) {
-        const unsigned c = code_v(v[i], iv, lot19(i < 4 ? key0 : key1, at + (unsigned)i));
-        (i < 4 ? cv.x : cv.y) |= c << (8 * (i & 3));
+        for (int i = 0; i < kAdamVec; ++i) c[i] = code_v(v[i] * iv, lot19(i < 4 ? key0 : key1, low + (unsigned)i));
+    } else {
+        cm.x = code_m2_any(m[0] * im, m[1] * im) | (code_m2_any(m[2] * im, m[3] * im) << 16);
+        cm.y = code_m2_any(m[4] * im, m[5] * im) | (code_m2_any(m[6] * im, m[7] * im) << 16);
+#pragma unroll
+        for (int i = 0; i < kAdamVec; ++i) c[i] = code_v_any(v[i] * iv, lot19(i < 4 ? key0 : key1, low + (unsigned)i));
     }
+    cv.x = __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
+    cv.y = __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410);
 }
 
 // Sum of squares of the gradient in fp64: every CTA leaves one partial sum, the last one to finish adds them in index
@@ -219,31 +239,31 @@ adamw_norm_kernel(const AdamTile* __restrict__ tiles, long long n_tiles, const G
     const int tid = threadIdx.x;
     cudaTriggerProgrammaticLaunchCompletion();  // the update's CTAs may come and load their operands
     double acc = 0.0;
+    AdamTile next = tiles[blockIdx.x];
     for (long long t = blockIdx.x; t < n_tiles; t += gridDim.x) {
-        const AdamTile tile = tiles[t];
+        const AdamTile tile = next;
+        if (t + gridDim.x < n_tiles) next = tiles[t + gridDim.x];  // known before its loads are due
         const G* g = grad + tile.base;
+        constexpr int kIters = kAdamTile / (kAdamThreads * kAdamVec);
+        float f[kIters][kAdamVec];
+        if (tile.len == kAdamTile) {
 #pragma unroll
-        for (int it = 0; it < kAdamTile / (kAdamThreads * kAdamVec); ++it) {
-            const int i = (it * kAdamThreads + tid) * kAdamVec;
-            if (i < tile.len) {
-                float f[kAdamVec];
-                if (i + kAdamVec <= tile.len) {
-                    Pack<G, 4> a, b;
-                    if (A8) {
-                        Pack<G, 8> c;
-                        c.load(g + i);
-                        c.get(f);
-                    } else {
-                        a.load(g + i);
-                        b.load(g + i + 4);
+            for (int it = 0; it < kIters; ++it) load8<G, A8, false>(g + (it * kAdamThreads + tid) * kAdamVec, f[it]);
+        } else {
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) f[j] = widen(a.v[j]), f[j + 4] = widen(b.v[j]);
-                    }
-                } else {
-                    load_some<G, A8>(g + i, tile.len - i, f);
-                }
+            for (int it = 0; it < kIters; ++it) load_some<G, A8>(g + (it * kAdamThreads + tid) * kAdamVec, tile.len - (it * kAdamThreads + tid) * kAdamVec, f[it]);
+        }
 #pragma unroll
-                for (int j = 0; j < kAdamVec; ++j) acc = fma((double)f[j], (double)f[j], acc);
+        for (int it = 0; it < kIters; ++it) {
+            if (sizeof(G) == 4) {
+#pragma unroll
+                for (int j = 0; j < kAdamVec; ++j) acc = fma((double)f[it][j], (double)f[it][j], acc);
+            } else {
+                // a bfloat16 square is exact in fp32 and four of them lose at most 2^-23 together: one conversion (of 16 per
+                // SM and clock) in place of four
+#pragma unroll
+                for (int j = 0; j < kAdamVec; j += 4)
+                    acc += (double)fmaf(f[it][j], f[it][j], fmaf(f[it][j + 1], f[it][j + 1], fmaf(f[it][j + 2], f[it][j + 2], f[it][j + 3] * f[it][j + 3])));
             }
         }
     }
@@ -307,6 +327,39 @@ __device__ __forceinline__ void adamw_element(float& p, float g, float& m, float
     p = fmaf(-a.step_size, __fdividef(m, den), fmaf(-decay, p, p));
 }
 
+// What a thread reads for its 8 elements.
+template <class P, class G, int BITS, bool A8>
+struct AdamLoads {
+    float p[kAdamVec], g[kAdamVec];
+    float m[BITS == 32 ? kAdamVec : 1], v[BITS == 32 ? kAdamVec : 1];
+    uint2 wm, wv;
+    int bm, bv;
+    __device__ __forceinline__ void load(const P* theta, const G* grad, const AdamArgs& a, const AdamTile& tile, int i) {
+        const int n = tile.len - i;
+        load_some<P, A8>(theta + i, n, p);
+        load_some<G, A8>(grad + i, n, g);
+        if constexpr (BITS == 32) {
+            load_some<float, A8>(static_cast<const float*>(a.m) + tile.base + i, n, m);
+            load_some<float, A8>(static_cast<const float*>(a.v) + tile.base + i, n, v);
+        } else {
+            wm = load_codes<A8>(static_cast<const uint8_t*>(a.m) + tile.base + i, n);
+            wv = load_codes<A8>(static_cast<const uint8_t*>(a.v) + tile.base + i, n);
+            const long long blk = tile.block0 + i / kAdamBlock;
+            bm = n > 0 ? a.scales[blk] : 0;
+            bv = n > 0 ? a.scales[a.blocks + blk] : 0;
+        }
+    }
+    __device__ __forceinline__ void moments(float (&m_)[kAdamVec], float (&v_)[kAdamVec]) const {
+        if constexpr (BITS == 32) {
+#pragma unroll
+            for (int j = 0; j < kAdamVec; ++j) m_[j] = m[j], v_[j] = v[j];
+        } else {
+            values_m(wm, pow2_byte(bm), m_);
+            values_v(wv, pow2_byte(bv), v_);
+        }
+    }
+};
+
 template <class P, class G, int BITS, bool A8>
 __global__ void __launch_bounds__(kAdamThreads)
 adamw_step_kernel(const AdamTile* __restrict__ tiles, const float* __restrict__ weight_decay, const AdamArgs a) {
@@ -316,30 +369,27 @@ adamw_step_kernel(const AdamTile* __restrict__ tiles, const float* __restrict__ 
     const G* grad = static_cast<const G*>(a.grad) + tile.base;
     const float decay = a.lr * weight_decay[tile.tensor];
     constexpr int kIters = kAdamTile / (kAdamThreads * kAdamVec);
+    // everything that does not depend on the norm is fetched first, all iterations at once where that is few registers
+    constexpr int kAhead = BITS == 8 ? kIters : 1;
+    AdamLoads<P, G, BITS, A8> in[kAhead];
+#pragma unroll
+    for (int it = 0; it < kAhead; ++it) in[it].load(theta, grad, a, tile, (it * kAdamThreads + tid) * kAdamVec);
     if (a.clip) cudaGridDependencySynchronize();
-    const float c = a.clip ? a.clip->coef : a.coef;
-    if (a.clip && a.skip && !a.clip->ok) return;
-#pragma unroll 1
+    const float c = a.clip ? __ldcg(&a.clip->coef) : a.coef;
+    if (a.clip && a.skip && !__ldcg(&a.clip->ok)) return;
+#pragma unroll
     for (int it = 0; it < kIters; ++it) {
         const int i = (it * kAdamThreads + tid) * kAdamVec;
         if ((it * kAdamThreads + (tid & ~31)) * kAdamVec >= tile.len) return;  // whole warps only
+        if (it >= kAhead) in[0].load(theta, grad, a, tile, i);
+        const AdamLoads<P, G, BITS, A8>& x = in[it < kAhead ? it : 0];
         const int n = tile.len - i;  // elements of this thread (more than 8: 8; below 1: none)
-        float p[kAdamVec], g[kAdamVec], m[kAdamVec], v[kAdamVec];
-        load_some<P, A8>(theta + i, n, p);
-        load_some<G, A8>(grad + i, n, g);
-        if (BITS == 32) {
-            load_some<float, A8>(static_cast<const float*>(a.m) + tile.base + i, n, m);
-            load_some<float, A8>(static_cast<const float*>(a.v) + tile.base + i, n, v);
-        } else {
-            const long long blk = tile.block0 + i / kAdamBlock;
-            const bool has = n > 0;
-            const uint2 wm = load_codes<A8>(static_cast<const uint8_t*>(a.m) + tile.base + i, n);
-            const uint2 wv = load_codes<A8>(static_cast<const uint8_t*>(a.v) + tile.base + i, n);
-            values_m(wm, pow2_byte(has ? a.scales[blk] : 0), m);
-            values_v(wv, pow2_byte(has ? a.scales[a.blocks + blk] : 0), v);
-        }
+        float p[kAdamVec], m[kAdamVec], v[kAdamVec];
+        x.moments(m, v);
 #pragma unroll
-        for (int j = 0; j < kAdamVec; ++j) adamw_element(p[j], g[j], m[j], v[j], a, c, decay);
+        for (int j = 0; j < kAdamVec; ++j) p[j] = x.p[j];
+#pragma unroll
+        for (int j = 0; j < kAdamVec; ++j) adamw_element(p[j], x.g[j], m[j], v[j], a, c, decay);
         store_some<P, A8>(theta + i, n, p);
         if (a.copy) store_some<bf16, A8>(a.copy + tile.base + i, n, p);
         if (BITS == 32) {
@@ -393,8 +443,9 @@ adamw_state_kernel(const AdamTile* __restrict__ tiles, float* m32, float* v32, u
                 scales[blocks + blk] = (uint8_t)bv;
             }
         } else if (n > 0) {
-            values_m(load_codes<A8>(m8 + tile.base + i, n), pow2_byte(scales[blk]), m);
-            values_v(load_codes<A8>(v8 + tile.base + i, n), pow2_byte(scales[blocks + blk]), v);
+            const uint2 wm = load_codes<A8>(m8 + tile.base + i, n), wv = load_codes<A8>(v8 + tile.base + i, n);
+            values_m(wm, pow2_byte(scales[blk]), m);
+            values_v(wv, pow2_byte(scales[blocks + blk]), v);
             store_some<float, A8>(m32 + tile.base + i, n, m);
             store_some<float, A8>(v32 + tile.base + i, n, v);
         }

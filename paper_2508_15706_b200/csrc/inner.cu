@@ -92,44 +92,65 @@ struct NormShape {
     int vec, nv, threads, rows_per_cta;
 };
 
-// A warp takes a narrow row (forward: up to 4 vectors a lane; backward, where a thread's columns carry three sums: one); wider
-// rows are spread over a CTA of at most 512 threads, with as few vectors per thread as that allows.
+// A warp takes a row of up to 32 vectors; wider rows are spread over a CTA of at most 512 threads, with as few vectors per thread
+// as that allows.  (Single values: four per thread at least.  Forward, two vectors from five warps a row on: a row's sums cost every
+// warp the same, however many columns it has.)
 NormShape norm_shape(int cols, int vec, bool backward) {
     NormShape s;
     s.vec = vec;
     const int vectors = (cols + vec - 1) / vec;
-    if (vectors <= (backward ? 32 : 128)) {
-        s.threads = 32;
-        s.nv = vectors <= 32 ? 1 : (vectors <= 64 && vec > 1 ? 2 : 4);
-        s.rows_per_cta = backward ? 8 : kNormWarpRows;
-        return s;
-    }
     const int need = (vectors + kNormMaxThreads - 1) / kNormMaxThreads;
-    if (vec > 1) s.nv = need <= 1 ? 1 : need <= 2 ? 2 : need <= 4 ? 4 : 8;
-    else s.nv = need <= 1 ? 1 : need <= 4 ? 4 : 32;
+    if (vec >= 4) s.nv = need <= 1 && (backward || vectors <= 128) ? 1 : need <= 2 ? 2 : need <= 4 ? 4 : 8;
+    else if (vec == 2) s.nv = need <= 4 ? 4 : 16;
+    else s.nv = need <= 4 ? 4 : need <= 8 ? 8 : 32;
     s.threads = ((vectors + s.nv - 1) / s.nv + 31) / 32 * 32;
-    s.rows_per_cta = 1;
+    s.rows_per_cta = s.threads == 32 ? kNormWarpRows : 1;
     return s;
+}
+
+// CTAs per SM: the registers of a thread decide (the kernels' launch bounds hold them to this)
+int norm_ctas(const NormShape& s, bool backward) {
+    return std::max(1, std::min(32, 65536 / norm_regs(s.nv * s.vec, backward) / (s.threads * s.rows_per_cta)));
+}
+unsigned norm_grid(const NormShape& s, long long rows, int n_sms, bool backward) {
+    const long long want = (rows + s.rows_per_cta - 1) / s.rows_per_cta;
+    return (unsigned)std::min(want, (long long)n_sms * norm_ctas(s, backward));
+}
+// Rows in a CTA's ring: up to four, as many as the SM's shared memory holds for its CTAs, two at least (one being used, one on its
+// way), but no more than a CTA has rows.
+int norm_stages(const NormShape& s, int arrays, int bytes, long long rows, unsigned grid, bool backward) {
+    const long long one = (long long)s.threads * s.rows_per_cta * s.nv * s.vec * bytes * arrays;
+    const long long fit = 220ll * 1024 / norm_ctas(s, backward) / one;
+    const long long has = (rows + (long long)grid * s.rows_per_cta - 1) / ((long long)grid * s.rows_per_cta) + 1;
+    return (int)std::max(2ll, std::min(std::min(4ll, fit), has));
+}
+
+template <class T, class W, int VEC, int NV, bool FULL>
+sl_status launch_norm_gate(const NormArgs& given, const NormShape& s, unsigned grid, bool backward, cudaStream_t st) {
+    NormArgs a = given;
+    const int arrays = (backward ? 4 : 2) + (FULL ? 1 : 0), threads = s.threads * s.rows_per_cta;
+    a.stages = norm_stages(s, arrays, (int)sizeof(T), a.rows, grid, backward);
+    const bool few = backward ? NV * VEC <= 8 : kNormFew<VEC, NV>;
+    size_t smem = few ? (size_t)threads * NV * VEC * sizeof(T) * arrays * a.stages : 0;
+    if (backward && s.rows_per_cta > 1) smem = std::max(smem, sizeof(float) * 2 * (size_t)a.cols);
+    auto kern = backward ? norm_backward_kernel<T, W, VEC, NV, FULL> : norm_forward_kernel<T, W, VEC, NV, FULL>;
+    if (smem > 47 * 1024) SL_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024));  // (1 KB stays for the sums)
+    kern<<<grid, dim3((unsigned)s.threads, (unsigned)s.rows_per_cta), smem, st>>>(a);
+    SL_CUDA(cudaGetLastError());
+    return SL_OK;
 }
 
 template <class T, class W, int VEC, int NV>
 sl_status launch_norm(const NormArgs& a, const NormShape& s, unsigned grid, bool backward, cudaStream_t st) {
-    const dim3 block((unsigned)s.threads, (unsigned)s.rows_per_cta);
-    if (backward) {
-        const size_t smem = s.rows_per_cta > 1 ? sizeof(float) * 3 * (size_t)a.cols : 0;
-        norm_backward_kernel<T, W, VEC, NV><<<grid, block, smem, st>>>(a);
-    } else {
-        norm_forward_kernel<T, W, VEC, NV><<<grid, block, 0, st>>>(a);
-    }
-    SL_CUDA(cudaGetLastError());
-    return SL_OK;
+    return a.gate_kind == SL_GATE_FULL ? launch_norm_gate<T, W, VEC, NV, true>(a, s, grid, backward, st) : launch_norm_gate<T, W, VEC, NV, false>(a, s, grid, backward, st);
 }
 
 template <class T, class W>
 sl_status launch_norm_shape(const NormArgs& a, const NormShape& s, unsigned grid, bool backward, cudaStream_t st) {
     constexpr int V = 16 / (int)sizeof(T);
-    if (s.vec == 1) return s.nv == 1 ? launch_norm<T, W, 1, 1>(a, s, grid, backward, st) : s.nv == 4 ? launch_norm<T, W, 1, 4>(a, s, grid, backward, st)
+    if (s.vec == 1) return s.nv == 4 ? launch_norm<T, W, 1, 4>(a, s, grid, backward, st) : s.nv == 8 ? launch_norm<T, W, 1, 8>(a, s, grid, backward, st)
                                                                                                      : launch_norm<T, W, 1, 32>(a, s, grid, backward, st);
+    if (s.vec == 2) return s.nv == 4 ? launch_norm<T, W, 2, 4>(a, s, grid, backward, st) : launch_norm<T, W, 2, 16>(a, s, grid, backward, st);
     if (s.nv == 1) return launch_norm<T, W, V, 1>(a, s, grid, backward, st);
     if (s.nv == 2) return launch_norm<T, W, V, 2>(a, s, grid, backward, st);
     if (s.nv == 4) return launch_norm<T, W, V, 4>(a, s, grid, backward, st);
@@ -140,6 +161,23 @@ sl_status launch_norm_types(const sl_norm_desc* d, const NormArgs& a, const Norm
     if (d->dtype == SL_F32) return launch_norm_shape<float, float>(a, s, grid, backward, st);
     if (d->weight_dtype == SL_F32) return launch_norm_shape<bf16, float>(a, s, grid, backward, st);
     return launch_norm_shape<bf16, bf16>(a, s, grid, backward, st);
+}
+
+template <class W>
+sl_status launch_norm_columns(const NormArgs& a, unsigned parts, const void* column_gate, void* dweight, void* dbranch_weight, void* dgate, cudaStream_t st) {
+    cudaLaunchConfig_t lc;
+    memset(&lc, 0, sizeof(lc));
+    lc.gridDim = dim3((unsigned)((2 * a.cols + 31) / 32));
+    lc.blockDim = dim3(1024);
+    lc.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = at;
+    lc.numAttrs = parts ? 1 : 0;  // only behind the backward kernel, which waits for what came before it
+    SL_CUDA(cudaLaunchKernelEx(&lc, norm_columns_kernel<W>, (const float*)a.part, (int)parts, a.cols, static_cast<const W*>(a.branch_weight),
+                               static_cast<const W*>(column_gate), static_cast<W*>(dweight), static_cast<W*>(dbranch_weight), static_cast<W*>(dgate)));
+    return SL_OK;
 }
 
 sl_status norm_check(const sl_norm_desc* d) {
@@ -172,30 +210,25 @@ void norm_strides(const sl_norm_desc* d, NormArgs* a) {
     a->ld_gate = d->ld_gate ? d->ld_gate : (d->gate_kind == SL_GATE_FULL ? d->cols : 1);
 }
 
-// Vectors of 16 bytes need them everywhere: columns, row strides, pointers (weights are read 16 bytes at a time too).
+// The values per access that columns, row strides and pointers of everything allow: 16 bytes, or two values, or one.
 struct NormAlign {
-    int bytes;
-    bool element, vector;
-    explicit NormAlign(const sl_norm_desc* d) : bytes(dtype_bytes(d->dtype)), element(true), vector(d->cols % (16 / dtype_bytes(d->dtype)) == 0) {}
+    int bytes, vec;
+    bool element;
+    explicit NormAlign(const sl_norm_desc* d) : bytes(dtype_bytes(d->dtype)), vec(16 / dtype_bytes(d->dtype)), element(true) { all(d->cols); }
+    void all(long long n) { vec = n % vec == 0 ? vec : n % 2 == 0 ? std::min(vec, 2) : 1; }
     void matrix(const void* p, long long ld) {
         if (!p) return;
         element = element && fits(p, bytes);
-        vector = vector && fits(p, 16) && ld % (16 / bytes) == 0;
+        all(ld);
+        all((long long)(reinterpret_cast<uintptr_t>(p) / (unsigned)bytes));
     }
-    void vec(const void* p, int b) {
+    void vector(const void* p, int b) {  // weights: 16 bytes at a time, or as many values
         if (!p) return;
         element = element && fits(p, b);
-        vector = vector && fits(p, 16);
+        if (vec > 2 && !fits(p, 16)) vec = 2;
+        if (vec == 2 && !fits(p, 2 * b)) vec = 1;
     }
 };
-
-// CTAs of the backward kernel: their column sums are written once and added up afterwards, so not more than stay resident
-unsigned norm_backward_grid(const NormShape& s, long long rows, int n_sms) {
-    const long long want = (rows + s.rows_per_cta - 1) / s.rows_per_cta;
-    const int threads = s.threads * s.rows_per_cta;
-    const long long most = (long long)n_sms * std::max(1, std::min(4, 768 / threads));
-    return (unsigned)std::min(want, most);
-}
 
 // ---- rotary
 template <class T, int VEC>
@@ -204,6 +237,53 @@ sl_status launch_rotary(const RopeArgs& a, bool half, unsigned grid, size_t smem
     else rotary_kernel<T, VEC, false><<<grid, kRopeThreads, smem, st>>>(a);
     SL_CUDA(cudaGetLastError());
     return SL_OK;
+}
+
+// ---- loss
+template <class K, class T>
+sl_status launch_loss_kernel(K kern, const LossArgs& a, const T* logits, T* grad, int threads, int cluster, cudaStream_t st) {
+    cudaLaunchConfig_t lc;
+    memset(&lc, 0, sizeof(lc));
+    lc.gridDim = dim3((unsigned)(a.rows * cluster));
+    lc.blockDim = dim3((unsigned)threads);
+    lc.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // behind the count, which waits for what came before it
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = (unsigned)cluster;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    lc.attrs = at;
+    lc.numAttrs = cluster > 1 ? 2 : 1;
+    SL_CUDA(kern(lc, a, logits, grad, cluster));
+    return SL_OK;
+}
+
+template <class T, int NV>
+sl_status launch_loss_rows(const LossArgs& a, const T* logits, T* grad, int threads, int cluster, cudaStream_t st) {
+    return launch_loss_kernel([](const cudaLaunchConfig_t& lc, const LossArgs& a_, const T* x, T* g, int c) { return cudaLaunchKernelEx(&lc, loss_row_kernel<T, 16 / (int)sizeof(T), NV>, a_, x, g, c); },
+                              a, logits, grad, threads, cluster, st);
+}
+
+template <class T>
+sl_status launch_loss(const LossArgs& a, const T* logits, T* grad, bool same, int n_sms, cudaStream_t st) {
+    constexpr int V = 16 / (int)sizeof(T), kMaxNv = 8;
+    const long long vectors = std::max(1, a.vocab / V);
+    if (!same)
+        return launch_loss_kernel([](const cudaLaunchConfig_t& lc, const LossArgs& a_, const T* x, T* g, int) { return cudaLaunchKernelEx(&lc, loss_stream_kernel<T, 1>, a_, x, g); }, a, logits,
+                                  grad, kLossThreads, 1, st);
+    if (vectors > 8ll * kLossThreads * kMaxNv || a.rows * 8 > 0x7FFFFFFFll)
+        return launch_loss_kernel([](const cudaLaunchConfig_t& lc, const LossArgs& a_, const T* x, T* g, int) { return cudaLaunchKernelEx(&lc, loss_stream_kernel<T, V>, a_, x, g); }, a, logits,
+                                  grad, kLossThreads, 1, st);
+    // as few CTAs as hold the row; more while there are SMs without one and every thread would keep a vector
+    int cluster = 1;
+    while (vectors > (long long)cluster * kLossThreads * kMaxNv) cluster *= 2;
+    while (cluster < 8 && a.rows * cluster < n_sms && vectors >= 2ll * cluster * kLossThreads) cluster *= 2;
+    const long long per = (vectors + cluster - 1) / cluster;
+    const int nv = per <= kLossThreads ? 1 : per <= 2 * kLossThreads ? 2 : per <= 4 * kLossThreads ? 4 : 8;
+    const int threads = (int)((per + nv - 1) / nv + 31) / 32 * 32;
+    return nv == 1 ? launch_loss_rows<T, 1>(a, logits, grad, threads, cluster, st) : nv == 2 ? launch_loss_rows<T, 2>(a, logits, grad, threads, cluster, st)
+         : nv == 4 ? launch_loss_rows<T, 4>(a, logits, grad, threads, cluster, st) : launch_loss_rows<T, 8>(a, logits, grad, threads, cluster, st);
 }
 
 bool overlaps_no(const sl_tensor_desc* tensors, int n) {
@@ -407,14 +487,17 @@ sl_status sl_norm_forward(const sl_norm_desc* d, const void* x, const void* bran
     al.matrix(branch, a.ld_branch);
     al.matrix(y, a.ld_y);
     al.matrix(h, a.ld_h);
-    al.vec(branch_weight, wb);
-    al.vec(weight, wb);
-    if (d->gate_kind == SL_GATE_COLUMN) al.vec(gate, wb);
+    al.vector(branch_weight, wb);
+    al.vector(weight, wb);
+    if (d->gate_kind == SL_GATE_COLUMN) al.vector(gate, wb);
     else if (d->gate_kind == SL_GATE_FULL) al.matrix(gate, a.ld_gate);
     else if (!fits(gate, al.bytes)) return SL_ERR_ALIGNMENT;
     if (!al.element || !fits(branch_rstd, 4) || !fits(rstd, 4)) return SL_ERR_ALIGNMENT;
-    const NormShape sh = norm_shape(a.cols, al.vector ? 16 / al.bytes : 1, false);
-    const unsigned grid = (unsigned)((d->rows + sh.rows_per_cta - 1) / sh.rows_per_cta);
+    const NormShape sh = norm_shape(a.cols, al.vec, false);
+    int n_sms = 0;
+    s = sm_count(&n_sms);
+    if (s != SL_OK) return s;
+    const unsigned grid = norm_grid(sh, d->rows, n_sms, false);
     return launch_norm_types(d, a, sh, grid, false, static_cast<cudaStream_t>(stream));
 }
 
@@ -425,11 +508,11 @@ sl_status sl_norm_workspace_bytes(const sl_norm_desc* d, size_t* bytes) {
     int n_sms = 0;
     s = sm_count(&n_sms);
     if (s != SL_OK) return s;
-    // the larger of the two launch shapes that alignment decides between
+    // the largest of the launch shapes that alignment decides between
     size_t most = 0;
-    for (int vec : {1, 16 / dtype_bytes(d->dtype)}) {
+    for (int vec : {1, 2, 16 / dtype_bytes(d->dtype)}) {
         const NormShape sh = norm_shape((int)d->cols, vec, true);
-        most = std::max(most, sizeof(float) * 3 * (size_t)d->cols * norm_backward_grid(sh, d->rows, n_sms));
+        most = std::max(most, sizeof(float) * 2 * (size_t)d->cols * norm_grid(sh, d->rows, n_sms, true));
     }
     *bytes = up256(most);
     return SL_OK;
@@ -467,9 +550,9 @@ sl_status sl_norm_backward(const sl_norm_desc* d, const void* dy, const void* dh
     al.matrix(branch, a.ld_branch);
     al.matrix(dx, a.ld_x);
     al.matrix(dbranch, a.ld_branch);
-    al.vec(branch_weight, wb);
-    al.vec(weight, wb);
-    if (d->gate_kind == SL_GATE_COLUMN) al.vec(gate, wb);
+    al.vector(branch_weight, wb);
+    al.vector(weight, wb);
+    if (d->gate_kind == SL_GATE_COLUMN) al.vector(gate, wb);
     else if (d->gate_kind == SL_GATE_FULL) al.matrix(gate, a.ld_gate), al.matrix(dgate, a.ld_gate);
     else if (!fits(gate, al.bytes) || !fits(dgate, al.bytes)) return SL_ERR_ALIGNMENT;
     if (!al.element || !fits(branch_rstd, 4) || !fits(rstd, 4) || !fits(dweight, wb) || !fits(dbranch_weight, wb) || misaligned(workspace) ||
@@ -480,10 +563,10 @@ sl_status sl_norm_backward(const sl_norm_desc* d, const void* dy, const void* dh
     s = sm_count(&n_sms);
     if (s != SL_OK) return s;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const NormShape sh = norm_shape(a.cols, al.vector ? 16 / al.bytes : 1, true);
-    const unsigned grid = norm_backward_grid(sh, d->rows, n_sms);
+    const NormShape sh = norm_shape(a.cols, al.vec, true);
+    const unsigned grid = norm_grid(sh, d->rows, n_sms, true);
     if (columns) {
-        if (grid && (!workspace || workspace_bytes < sizeof(float) * 3 * (size_t)a.cols * grid)) return SL_ERR_NOMEM;
+        if (grid && (!workspace || workspace_bytes < sizeof(float) * 2 * (size_t)a.cols * grid)) return SL_ERR_NOMEM;
         a.part = static_cast<float*>(workspace);
     }
     if (grid) {
@@ -491,13 +574,11 @@ sl_status sl_norm_backward(const sl_norm_desc* d, const void* dy, const void* dh
         if (s != SL_OK) return s;
     }
     if (columns) {
-        const unsigned cg = (unsigned)((3 * a.cols + 31) / 32);
         void* dg = d->gate_kind == SL_GATE_COLUMN ? dgate : nullptr;
-        if (d->weight_dtype == SL_F32)
-            norm_columns_kernel<float><<<cg, 256, 0, st>>>(a.part, (int)grid, a.cols, (float*)dweight, (float*)dbranch_weight, (float*)dg);
-        else
-            norm_columns_kernel<bf16><<<cg, 256, 0, st>>>(a.part, (int)grid, a.cols, (bf16*)dweight, (bf16*)dbranch_weight, (bf16*)dg);
-        SL_CUDA(cudaGetLastError());
+        const void* cg = d->gate_kind == SL_GATE_COLUMN ? gate : nullptr;
+        s = d->weight_dtype == SL_F32 ? launch_norm_columns<float>(a, grid, cg, dweight, dbranch_weight, dg, st)
+                                      : launch_norm_columns<bf16>(a, grid, cg, dweight, dbranch_weight, dg, st);
+        if (s != SL_OK) return s;
     }
     return SL_OK;
 }
@@ -669,16 +750,10 @@ sl_status sl_token_loss(const sl_loss_desc* d, const void* logits, const void* t
     if (d->rows == 0) return SL_OK;
     // 16-byte accesses from the first boundary of a row on: every row of logits and gradient has to meet it at the same column
     const bool same = !grad || ((reinterpret_cast<uintptr_t>(logits) - reinterpret_cast<uintptr_t>(grad)) % 16 == 0 && (a.ld_logits - a.ld_grad) * bytes % 16 == 0);
-    const unsigned grid = (unsigned)d->rows;
-    if (d->dtype == SL_F32) {
-        if (same) token_loss_kernel<float, 4><<<grid, kLossThreads, 0, st>>>(a, (const float*)logits, (float*)grad);
-        else token_loss_kernel<float, 1><<<grid, kLossThreads, 0, st>>>(a, (const float*)logits, (float*)grad);
-    } else {
-        if (same) token_loss_kernel<bf16, 8><<<grid, kLossThreads, 0, st>>>(a, (const bf16*)logits, (bf16*)grad);
-        else token_loss_kernel<bf16, 1><<<grid, kLossThreads, 0, st>>>(a, (const bf16*)logits, (bf16*)grad);
-    }
-    SL_CUDA(cudaGetLastError());
-    return SL_OK;
+    int n_sms = 0;
+    sl_status s = sm_count(&n_sms);
+    if (s != SL_OK) return s;
+    return d->dtype == SL_F32 ? launch_loss<float>(a, (const float*)logits, (float*)grad, same, n_sms, st) : launch_loss<bf16>(a, (const bf16*)logits, (bf16*)grad, same, n_sms, st);
 }
 
 }  // extern "C"

@@ -26,80 +26,141 @@ struct RopeArgs {
     float magnitude, sign;
 };
 
-// VEC consecutive values per access.  Half layout: a turning slot is two accesses, rot / 2 apart; interleaved: one access of
-// VEC / 2 pairs (one pair of single values where VEC is 1).  The slots behind them copy what is passed through.
+// One item: a slot of a head of a token.  VEC consecutive values per access.  Half layout: a turning slot is two accesses, rot / 2
+// apart; interleaved: one access of VEC / 2 pairs (one pair of single values where VEC is 1).  The slots behind them copy what is
+// passed through.
+template <class T, int VEC, bool HALF>
+struct RopeItem {
+    Pack<T, VEC> a, b;
+    __device__ __forceinline__ void load(const T* in, int slot, const RopeArgs& r) {
+        if (slot >= r.rot_slots) {
+            a.load(in + r.rot + (slot - r.rot_slots) * VEC);
+        } else if (HALF) {
+            a.load(in + slot * VEC);
+            b.load(in + r.rot / 2 + slot * VEC);
+        } else if (VEC > 1) {
+            a.load(in + slot * VEC);
+        } else {
+            a.v[0] = in[2 * slot];
+            b.v[0] = in[2 * slot + 1];
+        }
+    }
+    // cs: sines and cosines of the slot's first pair; those of the next pair are rot_slots further on (so that neighbouring slots
+    // read neighbouring words)
+    __device__ __forceinline__ void turn_store(T* out, int slot, const RopeArgs& r, const float2* cs, bool in_place) {
+        if (slot >= r.rot_slots) {
+            if (!in_place) a.store(out + r.rot + (slot - r.rot_slots) * VEC);
+        } else if (HALF) {
+            const int c = slot * VEC;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) turn(a.v[j], b.v[j], cs[j * r.rot_slots]);
+            a.store(out + c);
+            b.store(out + r.rot / 2 + c);
+        } else if (VEC > 1) {
+            const int c = slot * VEC;
+#pragma unroll
+            for (int j = 0; j + 1 < VEC; j += 2) turn(a.v[j], a.v[j + 1], cs[(j / 2) * r.rot_slots]);
+            a.store(out + c);
+        } else {
+            turn(a.v[0], b.v[0], cs[0]);
+            out[2 * slot] = a.v[0];
+            out[2 * slot + 1] = b.v[0];
+        }
+    }
+    static __device__ __forceinline__ void turn(T& x, T& y, float2 e) {
+        const float p = widen(x), q = widen(y);
+        x = narrow<T>(fmaf(p, e.x, -q * e.y));
+        y = narrow<T>(fmaf(q, e.x, p * e.y));
+    }
+};
+
+// A thread keeps its slot and walks over the (token, head) pairs of the CTA, a few of them at a time, all loads before the
+// first use; the first batch is on its way while sines and cosines are computed.
 template <class T, int VEC, bool HALF>
 __global__ void __launch_bounds__(kRopeThreads)
 rotary_kernel(const RopeArgs a) {
-    extern __shared__ float2 turn[];  // [tokens][rot / 2]: magnitude * (cos, sin)
-    const int half = a.rot / 2;
+    constexpr int kBatch = HALF && VEC > 1 ? 2 : 4, kPairs = HALF ? VEC : (VEC > 1 ? VEC / 2 : 1);  // pairs of a slot
+    extern __shared__ float2 turn[];  // [tokens][pair of a slot][slot]: magnitude * (cos, sin)
+    const int half = a.rot / 2, heads = a.q.heads + a.k.heads;
     const long long row0 = (long long)blockIdx.x * a.tokens;
     const int n_tok = (int)(a.rows - row0 < a.tokens ? a.rows - row0 : a.tokens);
-    for (int i = threadIdx.x; i < n_tok * half; i += kRopeThreads) {
-        const int t = i / half, f = i - t * half;
-        const long long row = row0 + t, b = row / a.seq, s = row - b * a.seq;
-        long long pos = a.first + s;
-        if (a.positions) {
-            const long long at = b * a.pos_batch + s * a.pos_token;
-            pos = a.position_bits == 64 ? static_cast<const long long*>(a.positions)[at] : (long long)static_cast<const int*>(a.positions)[at];
-        }
-        // position * frequency in turns, modulo 1 by the 64-bit product; as half turns in [-1, 1)
-        const long long phase = (long long)((unsigned long long)pos * a.turns[f]);
-        float sn, cs;
-        sincospif((float)phase * 1.0842021724855044e-19f, &sn, &cs);  // 2^-63
-        turn[i] = make_float2(cs * a.magnitude, sn * a.sign * a.magnitude);
-    }
-    __syncthreads();
-    const int heads = a.q.heads + a.k.heads, per_tok = heads * a.slots;
-    for (int i = threadIdx.x; i < n_tok * per_tok; i += kRopeThreads) {
-        const int t = i / per_tok, u = i - t * per_tok;
-        int h = u / a.slots;
-        const int slot = u - h * a.slots;
-        const bool is_k = h >= a.q.heads;
-        const RopeHeads& x = is_k ? a.k : a.q;
-        if (is_k) h -= a.q.heads;
-        const long long row = row0 + t, b = row / a.seq, s = row - b * a.seq;
-        const T* in = static_cast<const T*>(x.in) + b * x.in_batch + s * x.in_token + h * x.in_head;
-        T* out = static_cast<T*>(x.out) + b * x.out_batch + s * x.out_token + h * x.out_head;
-        const float2* cs = turn + t * half;
-        if (slot < a.rot_slots) {
-            if (HALF) {
-                const int c = slot * VEC;
-                Pack<T, VEC> lo, hi;
-                lo.load(in + c);
-                hi.load(in + half + c);
+    const int span = a.slots < kRopeThreads ? a.slots : kRopeThreads;  // threads of a (token, head) pair
+    const int groups = kRopeThreads / span, group = threadIdx.x / span;
+    const bool works = group < groups;
+    const int pairs = n_tok * heads;
+
+    struct Place {
+        int tok, head;
+    };
+    const int step_tok = groups / heads, step_head = groups - step_tok * heads;
+    auto step = [&](Place& p) {
+        p.tok += step_tok;
+        p.head += step_head;
+        if (p.head >= heads) p.head -= heads, ++p.tok;
+    };
+    const unsigned b0 = (unsigned)row0 / (unsigned)a.seq, s0 = (unsigned)row0 - b0 * (unsigned)a.seq;
+    auto where = [&](int tok, long long& b, long long& s) {  // (tokens per CTA are few)
+        unsigned bb = b0, ss = s0 + (unsigned)tok;
+        while (ss >= (unsigned)a.seq) ss -= (unsigned)a.seq, ++bb;
+        b = bb;
+        s = ss;
+    };
+    auto in_of = [&](const Place& p) {
+        const bool k = p.head >= a.q.heads;
+        const RopeHeads& x = k ? a.k : a.q;
+        long long b, s;
+        where(p.tok, b, s);
+        return static_cast<const T*>(x.in) + b * x.in_batch + s * x.in_token + (long long)(k ? p.head - a.q.heads : p.head) * x.in_head;
+    };
+    auto out_of = [&](const Place& p) {
+        const bool k = p.head >= a.q.heads;
+        const RopeHeads& x = k ? a.k : a.q;
+        long long b, s;
+        where(p.tok, b, s);
+        return static_cast<T*>(x.out) + b * x.out_batch + s * x.out_token + (long long)(k ? p.head - a.q.heads : p.head) * x.out_head;
+    };
+
+    bool ready = false;
+    for (int slot = threadIdx.x - group * span; slot < a.slots || !ready; slot += span) {
+        RopeItem<T, VEC, HALF> item[kBatch];
+        Place at;
+        at.tok = group / heads;
+        at.head = group - at.tok * heads;
+        const bool mine = works && slot < a.slots;
+        for (int pair = group; pair < pairs || !ready; pair += groups * kBatch) {
+            Place p = at;
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    const float p = widen(lo.v[j]), q = widen(hi.v[j]);
-                    const float2 e = cs[c + j];
-                    lo.v[j] = narrow<T>(fmaf(p, e.x, -q * e.y));
-                    hi.v[j] = narrow<T>(fmaf(q, e.x, p * e.y));
-                }
-                lo.store(out + c);
-                hi.store(out + half + c);
-            } else if (VEC > 1) {
-                const int c = slot * VEC;
-                Pack<T, VEC> v;
-                v.load(in + c);
-#pragma unroll
-                for (int j = 0; j + 1 < VEC; j += 2) {
-                    const float p = widen(v.v[j]), q = widen(v.v[j + 1]);
-                    const float2 e = cs[(c + j) / 2];
-                    v.v[j] = narrow<T>(fmaf(p, e.x, -q * e.y));
-                    v.v[j + 1] = narrow<T>(fmaf(q, e.x, p * e.y));
-                }
-                v.store(out + c);
-            } else {
-                const float p = widen(in[2 * slot]), q = widen(in[2 * slot + 1]);
-                const float2 e = cs[slot];
-                out[2 * slot] = narrow<T>(fmaf(p, e.x, -q * e.y));
-                out[2 * slot + 1] = narrow<T>(fmaf(q, e.x, p * e.y));
+            for (int u = 0; u < kBatch; ++u) {
+                if (mine && pair + u * groups < pairs) item[u].load(in_of(p), slot, a);
+                step(p);
             }
-        } else if (in != out) {
-            const int c = a.rot + (slot - a.rot_slots) * VEC;
-            Pack<T, VEC> v;
-            v.load(in + c);
-            v.store(out + c);
+            if (!ready) {
+                for (int i = threadIdx.x; i < n_tok * half; i += kRopeThreads) {
+                    const int t = i / half, f = i - t * half;
+                    long long b, s;
+                    where(t, b, s);
+                    long long pos = a.first + s;
+                    if (a.positions) {
+                        const long long w = b * a.pos_batch + s * a.pos_token;
+                        pos = a.position_bits == 64 ? static_cast<const long long*>(a.positions)[w] : (long long)static_cast<const int*>(a.positions)[w];
+                    }
+                    // position * frequency in turns, modulo 1 by the 64-bit product; as half turns in [-1, 1)
+                    const long long phase = (long long)((unsigned long long)pos * a.turns[f]);
+                    float sn, cs;
+                    sincospif((float)phase * 1.0842021724855044e-19f, &sn, &cs);  // 2^-63
+                    turn[t * half + (f % kPairs) * a.rot_slots + f / kPairs] = make_float2(cs * a.magnitude, sn * a.sign * a.magnitude);
+                }
+                __syncthreads();
+                ready = true;
+            }
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                if (mine && pair + u * groups < pairs) {
+                    const bool k = at.head >= a.q.heads;
+                    item[u].turn_store(out_of(at), slot, a, turn + at.tok * half + slot, (k ? a.k.in : a.q.in) == (k ? a.k.out : a.q.out));
+                }
+                step(at);
+            }
         }
     }
 }

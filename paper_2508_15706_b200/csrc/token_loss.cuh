@@ -1,9 +1,14 @@
 // Next-token loss and its gradient.  Part of libsparseloco (inner.cu).
 //
-// Bound: HBM (logits read once, gradient written once).  A CTA takes a row: one pass with a running maximum and sum, a
-// second one that forms the gradient from the row again, which by then comes from L2 (a row is 64 or 128 KB at a
-// vocabulary of 32000, the rows in flight a fraction of the 126 MB).
+// Bound: HBM (logits read once, gradient written once).  A row stays in the registers of its CTA, or of the CTAs of a cluster where
+// one CTA cannot hold it or there are fewer rows than SMs: one pass for a maximum and a sum of exponentials per thread, one
+// exchange, then the gradient from the same registers.  (The maximum is taken off before the factor log2 e: a row of the type's
+// lowest value would overflow the other way round.)
+// Rows that eight CTAs cannot hold, and gradients that sit elsewhere relative to 16 bytes than their logits, go through a kernel that
+// reads the row twice (the second time from L2).
 #pragma once
+#include <cooperative_groups.h>
+
 #include "inner_common.cuh"
 
 namespace {
@@ -29,10 +34,13 @@ __device__ __forceinline__ long long target_of(const LossArgs& a, long long row)
     return a.target_bits == 64 ? static_cast<const long long*>(a.targets)[row] : (long long)static_cast<const int*>(a.targets)[row];
 }
 
+// The number of rows that count; also puts the ticket back.
 __global__ void __launch_bounds__(1024)
 loss_count_kernel(const LossArgs a) {
     __shared__ int part[32];
+    cudaTriggerProgrammaticLaunchCompletion();  // the rows' CTAs may come and read their logits
     int n = 0;
+#pragma unroll 4
     for (long long r = threadIdx.x; r < a.rows; r += 1024) n += target_of(a, r) != a.ignore_index;
     n = warp_sum(n);
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = n;
@@ -46,26 +54,211 @@ loss_count_kernel(const LossArgs a) {
     }
 }
 
-// Running maximum and sum of exponentials; sum is relative to the maximum.  -inf with 0 = nothing seen.
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ float exp_fast(float x) {  // e^x, 0 for -inf; relative error 2^-22 and the argument's rounding
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x * kLog2e));
+    return y;
+}
+
+// Maximum and sum of exponentials relative to it; -inf with 0 = nothing seen, NaN and +inf end in the sum.
 __device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
     const float top = fmaxf(m, m2);
-    if (top == -INFINITY) {  // nothing but -inf on both sides (or NaN, which the sums carry)
+    if (top == -INFINITY) {
         s += s2;
         return;
     }
-    s = s * expf(m - top) + s2 * expf(m2 - top);
+    s = s * exp_fast(m - top) + s2 * exp_fast(m2 - top);
     m = top;
 }
 
+// What a row comes to, from its maximum, sum and target.
+struct LossRow {
+    float m, s, sum, lse, w;
+    long long target;
+    int valid;
+    bool counts, inside, empty;
+    __device__ __forceinline__ bool has_gradient() const { return counts && inside && !empty; }
+};
+__device__ __forceinline__ void finish_row(const LossArgs& a, LossRow& r) {
+    r.empty = r.m == -INFINITY && r.s == 0.0f;  // every logit is -inf
+    r.lse = r.empty ? -INFINITY : r.m + logf(r.s);
+    cudaGridDependencySynchronize();
+    r.valid = __ldcg(&a.work->valid);
+    r.w = a.mean ? a.scale / (float)(r.valid > 0 ? r.valid : 1) : a.scale;
+}
+__device__ __forceinline__ void write_row(const LossArgs& a, const LossRow& r, long long row, float xt) {
+    float loss = 0.0f;
+    if (r.counts) {
+        if (!r.inside) loss = __int_as_float(0x7FC00000);
+        else if (r.empty) loss = INFINITY;
+        else {
+            loss = r.lse - (1.0f - a.smoothing) * xt + a.z * r.lse * r.lse;
+            if (a.smoothing != 0.0f) loss -= a.smoothing * (r.sum / (float)a.vocab);
+        }
+    }
+    a.row_loss[row] = loss;
+    if (a.lse) a.lse[row] = r.lse;
+}
+// The last of `rows` callers adds the rows' losses in a fixed order: thread by thread, then thread after thread.
+__device__ __forceinline__ void add_rows(const LossArgs& a, const LossRow& r) {
+    __shared__ int last;
+    __shared__ double st[32];
+    if (!a.total) return;
+    if (threadIdx.x == 0) {
+        __threadfence();
+        last = atomicAdd(&a.work->ticket, 1u) == (unsigned)(a.rows - 1);
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    double t = 0.0;
+    for (long long i = threadIdx.x; i < a.rows; i += blockDim.x) t += (double)__ldcg(a.row_loss + i);
+    t = warp_sum(t);
+    if ((threadIdx.x & 31) == 0) st[threadIdx.x >> 5] = t;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        t = 0.0;
+        for (int i = 0; i < (int)(blockDim.x >> 5); ++i) t += st[i];
+        *a.total = r.valid > 0 ? (float)(t * (double)r.w) : 0.0f;
+    }
+}
+
+// A row in registers: NV accesses of VEC values per thread, `cluster` CTAs per row.  The vector body begins at the row's first
+// 16-byte boundary; the values before it belong to the first CTA, those behind it to the last, one per thread.
+template <class T, int VEC, int NV>
+__global__ void __launch_bounds__(kLossThreads, NV * VEC * (int)sizeof(T) <= 128 ? 2 : 1)
+loss_row_kernel(const LossArgs a, const T* logits, T* grad, int cluster) {
+    __shared__ float sm[32], ss[32], sx[32];
+    __shared__ float mine[4];  // this CTA's maximum, sum of exponentials, sum: read by the cluster
+    const int tid = threadIdx.x, threads = blockDim.x;
+    const long long row = blockIdx.x / (unsigned)cluster;
+    const int rank = (int)(blockIdx.x - (unsigned)row * (unsigned)cluster);
+    const T* x = logits + row * a.ld_logits;
+    int head = (int)((16u - (unsigned)(reinterpret_cast<uintptr_t>(x) & 15u)) & 15u) / (int)sizeof(T);
+    if (head > a.vocab) head = a.vocab;
+    const int body = (a.vocab - head) / VEC, tail = head + body * VEC, per = (body + cluster - 1) / cluster;
+    const int begin = rank * per, end = min(body, begin + per);
+    Pack<T, VEC> v[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int at = begin + i * threads + tid;
+        if (at < end) {
+            v[i].load_stream(x + head + at * VEC);
+        } else {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) v[i].v[j] = narrow<T>(-INFINITY);
+        }
+    }
+    // a single value before or behind the body (each at most VEC - 1 of them; both ends may be in one CTA)
+    const int before = rank == 0 && tid < head ? tid : -1, behind = rank == cluster - 1 && tail + tid < a.vocab ? tail + tid : -1;
+    const float first = before >= 0 ? widen(x[before]) : -INFINITY, last_one = behind >= 0 ? widen(x[behind]) : -INFINITY;
+    LossRow r;
+    r.target = target_of(a, row);
+    r.counts = r.target != a.ignore_index;
+    r.inside = r.target >= 0 && r.target < a.vocab;
+    const float xt = r.counts && r.inside ? widen(x[r.target]) : 0.0f;  // (before any gradient takes its place: a barrier follows)
+
+    float m = fmaxf(first, last_one);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) m = fmaxf(m, widen(v[i].v[j]));
+    const float ref = m == -INFINITY ? 0.0f : m;
+    float s = exp_fast(first - ref) + exp_fast(last_one - ref), sum = 0.0f;
+    if (a.smoothing != 0.0f) {
+        sum = (before >= 0 ? first : 0.0f) + (behind >= 0 ? last_one : 0.0f);
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (begin + i * threads + tid < end)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) sum += widen(v[i].v[j]);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        float part = 0.0f;  // (short chains of additions)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) part += exp_fast(widen(v[i].v[j]) - ref);
+        s += part;
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        const float m2 = __shfl_xor_sync(kFullMask, m, o), s2 = __shfl_xor_sync(kFullMask, s, o);
+        join(m, s, m2, s2);
+        sum += __shfl_xor_sync(kFullMask, sum, o);
+    }
+    if ((tid & 31) == 0) sm[tid >> 5] = m, ss[tid >> 5] = s, sx[tid >> 5] = sum;
+    __syncthreads();
+    r.m = sm[0], r.s = ss[0], r.sum = sx[0];
+    for (int w = 1; w < threads / 32; ++w) {
+        join(r.m, r.s, sm[w], ss[w]);
+        r.sum += sx[w];
+    }
+    if (cluster > 1) {
+        namespace cg = cooperative_groups;
+        auto group = cg::this_cluster();
+        if (tid == 0) mine[0] = r.m, mine[1] = r.s, mine[2] = r.sum;
+        group.sync();
+        for (int c = 0; c < cluster; ++c) {  // in the same order in every CTA
+            const float* other = group.map_shared_rank(mine, (unsigned)c);
+            const float m2 = other[0], s2 = other[1], x2 = other[2];
+            if (c == 0) r.m = m2, r.s = s2, r.sum = x2;
+            else join(r.m, r.s, m2, s2), r.sum += x2;
+        }
+        group.sync();  // nobody leaves while its values are read
+    }
+    finish_row(a, r);
+    if (rank == 0 && tid == 0) write_row(a, r, row, xt);
+    if (grad) {
+        T* g = grad + row * a.ld_grad;
+        const bool some = r.has_gradient();
+        const float k = some ? r.w * fmaf(2.0f * a.z, r.lse, 1.0f) / r.s : 0.0f, off = some ? r.w * a.smoothing / (float)a.vocab : 0.0f,
+                    hit = r.w * (1.0f - a.smoothing);
+        const int t = some ? (int)r.target : -1;
+        const int tv = t >= head && t < tail ? (t - head) / VEC : -1, te = t - head - tv * VEC;  // the target's vector and place in it
+        const float top = some ? r.m : 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int at = begin + i * threads + tid;
+            if (at < end) {
+                float f[VEC];
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) f[j] = fmaf(k, exp_fast(widen(v[i].v[j]) - top), -off);
+                if (at == tv) {
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j)
+                        if (j == te) f[j] -= hit;
+                }
+                if (!some) {  // (0 times what overflows or is NaN would not be 0)
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) f[j] = 0.0f;
+                }
+                Pack<T, VEC> o;
+                o.set(f);
+                o.store_stream(g + head + at * VEC);
+            }
+        }
+        auto one = [&](int at, float val) {
+            float d = some ? fmaf(k, exp_fast(val - top), -off) : 0.0f;
+            if (at == t) d -= hit;
+            g[at] = narrow<T>(d);
+        };
+        if (before >= 0) one(before, first);
+        if (behind >= 0) one(behind, last_one);
+    }
+    if (rank == 0) add_rows(a, r);
+}
+
+// The row read twice: a running maximum and sum, then the gradient.
+
 template <class T, int VEC>
 __global__ void __launch_bounds__(kLossThreads)
-token_loss_kernel(const LossArgs a, const T* logits, T* grad) {
+loss_stream_kernel(const LossArgs a, const T* logits, T* grad) {
     __shared__ float sm[32], ss[32], sx[32];
-    __shared__ int last;
     const int tid = threadIdx.x;
     const long long row = blockIdx.x;
     const T* x = logits + row * a.ld_logits;
-    // the vector body begins at the row's first 16-byte boundary
     int head = 0;
     if (VEC > 1) {
         head = (int)((16u - (unsigned)(reinterpret_cast<uintptr_t>(x) & 15u)) & 15u) / (int)sizeof(T);
@@ -73,20 +266,22 @@ token_loss_kernel(const LossArgs a, const T* logits, T* grad) {
     }
     const int body = VEC > 1 ? (a.vocab - head) / VEC : 0;  // vectors
     const int rest = head + body * VEC;                     // scalars from here on
-    const long long target = target_of(a, row);
-    const bool counts = target != a.ignore_index, inside = target >= 0 && target < a.vocab;
+    LossRow r;
+    r.target = target_of(a, row);
+    r.counts = r.target != a.ignore_index;
+    r.inside = r.target >= 0 && r.target < a.vocab;
     float m = -INFINITY, s = 0.0f, sum = 0.0f;
-    auto see = [&](float v) {
-        sum += v;
-        if (v > m) {
-            s = s * expf(m - v) + 1.0f;
-            m = v;
-        } else if (v == -INFINITY) {
-        } else {
-            s += expf(v - m);  // (NaN and +inf end here and stay in the sum)
+    auto rise = [&](float top) {  // the maximum so far goes up to top
+        if (top > m) {
+            s *= exp_fast(m - top);
+            m = top;
         }
     };
-    for (int i = tid; i < head; i += kLossThreads) see(widen(x[i]));
+    auto see = [&](float v) {
+        sum += v;
+        if (v != -INFINITY) s += exp_fast(m == -INFINITY ? v : v - m);  // (NaN and +inf end here and stay in the sum)
+    };
+    for (int i = tid; i < head; i += kLossThreads) rise(widen(x[i])), see(widen(x[i]));
     for (int i = tid; i < body; i += kLossThreads) {
         Pack<T, VEC> p;
         p.load(x + head + i * VEC);
@@ -95,17 +290,11 @@ token_loss_kernel(const LossArgs a, const T* logits, T* grad) {
         float top = f[0];
 #pragma unroll
         for (int j = 1; j < VEC; ++j) top = fmaxf(top, f[j]);
-        if (top > m) {
-            s = s * expf(m - top);
-            m = top;
-        }
+        rise(top);
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            sum += f[j];
-            if (f[j] != -INFINITY) s += expf(f[j] - m);
-        }
+        for (int j = 0; j < VEC; ++j) see(f[j]);
     }
-    for (int i = rest + tid; i < a.vocab; i += kLossThreads) see(widen(x[i]));
+    for (int i = rest + tid; i < a.vocab; i += kLossThreads) rise(widen(x[i])), see(widen(x[i]));
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
         const float m2 = __shfl_xor_sync(kFullMask, m, o), s2 = __shfl_xor_sync(kFullMask, s, o);
@@ -113,81 +302,35 @@ token_loss_kernel(const LossArgs a, const T* logits, T* grad) {
     }
     sum = warp_sum(sum);
     if ((tid & 31) == 0) sm[tid >> 5] = m, ss[tid >> 5] = s, sx[tid >> 5] = sum;
-    const float xt = counts && inside ? widen(x[target]) : 0.0f;  // (read before any thread writes a gradient in its place)
+    const float xt = r.counts && r.inside ? widen(x[r.target]) : 0.0f;  // (read before any thread writes a gradient in its place)
     __syncthreads();
-    m = sm[0], s = ss[0], sum = sx[0];
+    r.m = sm[0], r.s = ss[0], r.sum = sx[0];
     for (int w = 1; w < kLossThreads / 32; ++w) {
-        join(m, s, sm[w], ss[w]);
-        sum += sx[w];
+        join(r.m, r.s, sm[w], ss[w]);
+        r.sum += sx[w];
     }
-    const bool empty = m == -INFINITY && s == 0.0f;  // every logit is -inf
-    const float lse = empty ? -INFINITY : m + logf(s);
-    const int valid = a.work->valid;
-    const float w = a.mean ? a.scale / (float)(valid > 0 ? valid : 1) : a.scale;
-    if (tid == 0) {
-        float loss = 0.0f;
-        if (counts) {
-            if (!inside) loss = __int_as_float(0x7FC00000);
-            else if (empty) loss = INFINITY;
-            else {
-                loss = lse - (1.0f - a.smoothing) * xt + a.z * lse * lse;
-                if (a.smoothing != 0.0f) loss -= a.smoothing * (sum / (float)a.vocab);
-            }
-        }
-        a.row_loss[row] = loss;
-        if (a.lse) a.lse[row] = lse;
-    }
+    finish_row(a, r);
+    if (tid == 0) write_row(a, r, row, xt);
     if (grad) {
         T* g = grad + row * a.ld_grad;
-        if (!counts || !inside || empty) {
-            // zeros; the stores go where the loads went, by the same alignment
-            for (int i = tid; i < head; i += kLossThreads) g[i] = narrow<T>(0.0f);
-            for (int i = tid; i < body; i += kLossThreads) {
-                Pack<T, VEC> p;
+        const bool some = r.has_gradient();
+        const float k = some ? r.w * fmaf(2.0f * a.z, r.lse, 1.0f) / r.s : 0.0f, off = r.w * a.smoothing / (float)a.vocab, hit = r.w * (1.0f - a.smoothing);
+        auto of = [&](float v, int i) {
+            if (!some) return 0.0f;
+            const float d = fmaf(k, exp_fast(v - r.m), -off);
+            return i == (int)r.target ? d - hit : d;
+        };
+        for (int i = tid; i < head; i += kLossThreads) g[i] = narrow<T>(of(widen(x[i]), i));
+        for (int i = tid; i < body; i += kLossThreads) {
+            Pack<T, VEC> p;
+            p.load(x + head + i * VEC);
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) p.v[j] = narrow<T>(0.0f);
-                p.store(g + head + i * VEC);
-            }
-            for (int i = rest + tid; i < a.vocab; i += kLossThreads) g[i] = narrow<T>(0.0f);
-        } else {
-            const float k = w * fmaf(2.0f * a.z, lse, 1.0f) / s, off = w * a.smoothing / (float)a.vocab, hit = w * (1.0f - a.smoothing);
-            const int t = (int)target;
-            auto of = [&](float v, int i) {
-                float d = fmaf(k, expf(v - m), -off);
-                if (i == t) d -= hit;
-                return d;
-            };
-            for (int i = tid; i < head; i += kLossThreads) g[i] = narrow<T>(of(widen(x[i]), i));
-            for (int i = tid; i < body; i += kLossThreads) {
-                Pack<T, VEC> p;
-                p.load(x + head + i * VEC);
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) p.v[j] = narrow<T>(of(widen(p.v[j]), head + i * VEC + j));
-                p.store(g + head + i * VEC);
-            }
-            for (int i = rest + tid; i < a.vocab; i += kLossThreads) g[i] = narrow<T>(of(widen(x[i]), i));
+            for (int j = 0; j < VEC; ++j) p.v[j] = narrow<T>(of(widen(p.v[j]), head + i * VEC + j));
+            p.store(g + head + i * VEC);
         }
+        for (int i = rest + tid; i < a.vocab; i += kLossThreads) g[i] = narrow<T>(of(widen(x[i]), i));
     }
-    // the last CTA adds the rows' losses in their order: thread by thread, then thread after thread
-    if (!a.total) return;
-    if (tid == 0) {
-        __threadfence();
-        last = atomicAdd(&a.work->ticket, 1u) == gridDim.x - 1;
-    }
-    __syncthreads();
-    if (!last) return;
-    __threadfence();
-    double t = 0.0;
-    for (long long r = tid; r < a.rows; r += kLossThreads) t += (double)__ldcg(a.row_loss + r);
-    t = warp_sum(t);
-    __shared__ double st[32];
-    if ((tid & 31) == 0) st[tid >> 5] = t;
-    __syncthreads();
-    if (tid == 0) {
-        t = 0.0;
-        for (int i = 0; i < kLossThreads / 32; ++i) t += st[i];
-        *a.total = valid > 0 ? (float)(t * (double)w) : 0.0f;
-    }
+    add_rows(a, r);
 }
 
 }  // namespace

@@ -13,11 +13,10 @@ from typing import Optional, Sequence
 
 import torch
 
-from .binding import SlError, SL_ERR_INVALID_ARG, _check, _L, _stream, _TensorDesc
+from .binding import SlError, SL_ERR_INVALID_ARG, _check, _L, _TensorDesc
 
 P, I32, I64, F32, F64 = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_double
 DTYPES = {torch.float32: 0, torch.bfloat16: 1}
-GATES = {"none": 0, "column": 1, "row": 2, "full": 3}
 LAYOUTS = {"half": 0, "interleaved": 1}
 SCALINGS = {"none": 0, "linear": 1, "base": 2, "by_parts": 3}
 
@@ -63,35 +62,44 @@ _L.sl_loss_workspace_bytes.restype = C.c_size_t
 _L.sl_token_loss.argtypes = [P] * 8 + [C.c_size_t, P]
 
 
-def _need(ok: bool, what: str) -> None:
-    if not ok:
-        raise SlError(SL_ERR_INVALID_ARG, f"libsparseloco: {what}")
+def _refuse(what: str):
+    raise SlError(SL_ERR_INVALID_ARG, "libsparseloco: " + what)
 
 
 def _dtype(t: torch.dtype) -> int:
-    _need(t in DTYPES, f"{t} is not one of float32, bfloat16")
-    return DTYPES[t]
+    code = DTYPES.get(t)
+    if code is None:
+        _refuse(f"{t} is not one of float32, bfloat16")
+    return code
 
 
-def _ptr(t: Optional[torch.Tensor], dtype=None, numel: Optional[int] = None, what: str = "tensor") -> Optional[int]:
-    """Address of a contiguous tensor on the current device."""
+# The checks below are made on every call of operators that may take a few microseconds, so they ask for each property once
+# and put a message together only when one fails.
+def _here() -> int:
+    return torch._C._cuda_getDevice()
+
+
+def _queue(dev: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(dev)
+
+
+def _ptr(t: Optional[torch.Tensor], dev: int, dtype, numel: int, what: str) -> Optional[int]:
+    """Address of a contiguous tensor of at least `numel` elements on device `dev`."""
     if t is None:
         return None
-    _need(t.is_cuda and t.is_contiguous(), f"{what} must be a contiguous CUDA tensor")
-    _need(dtype is None or t.dtype == dtype, f"{what} must be {dtype}, got {t.dtype}")
-    _need(numel is None or t.numel() >= numel, f"{what} has {t.numel()} elements, {numel} are needed")
+    if t.get_device() != dev or t.dtype is not dtype or not t.is_contiguous() or t.numel() < numel:
+        _refuse(f"{what} must be a contiguous CUDA tensor of {dtype} on device {dev} with at least {numel} elements, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
-def _rows(t: Optional[torch.Tensor], rows: int, cols: int, dtype, what: str):
+def _rows(t: Optional[torch.Tensor], dev: int, rows: int, cols: int, dtype, what: str):
     """(address, row stride) of a [rows, cols] matrix with a unit column stride."""
     if t is None:
         return None, 0
-    _need(t.is_cuda and t.dtype == dtype, f"{what} must be a CUDA tensor of {dtype}")
-    _need(t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols, f"{what} must be [{rows}, {cols}], got {tuple(t.shape)}")
-    _need(t.stride(1) == 1 or cols == 1, f"{what} must have a unit column stride")
-    _need(rows <= 1 or t.stride(0) >= cols, f"{what}: rows overlap")
-    return t.data_ptr(), t.stride(0) if rows > 1 else cols
+    st = t.stride()
+    if t.get_device() != dev or t.dtype is not dtype or t.shape != (rows, cols) or (st[1] != 1 and cols != 1) or (rows > 1 and st[0] < cols):
+        _refuse(f"{what} must be a CUDA tensor [{rows}, {cols}] of {dtype} on device {dev} with unit column stride and rows apart, got {t.dtype} {tuple(t.shape)} strides {st} on {t.device}")
+    return t.data_ptr(), st[0] if rows > 1 else cols
 
 
 class AdamW:
@@ -111,7 +119,8 @@ class AdamW:
             descs[j] = _TensorDesc(rows, cols, off)
             pos = off + rows * cols
         decay = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else [float(w) for w in weight_decay]
-        _need(len(decay) == n, f"{len(decay)} weight decays for {n} tensors")
+        if len(decay) != n:
+            _refuse(f"{len(decay)} weight decays for {n} tensors")
         cfg = _AdamWConfig(_dtype(param_dtype), _dtype(grad_dtype), state_bits, int(skip_nonfinite), betas[0], betas[1], eps, max_norm)
         self._h = P()
         _check(_L.sl_adamw_create(C.byref(cfg), descs, (F32 * n)(*decay), n, C.byref(self._h)))
@@ -138,60 +147,68 @@ class AdamW:
         m, v = (torch.zeros(self.flat_elems, dtype=self._moment, device=self.device) for _ in range(2))
         return m, v, None if self.state_bits == 32 else torch.zeros(2, self.blocks, dtype=torch.uint8, device=self.device)
 
-    def _state(self, m, v, scales):
-        return (_ptr(m, self._moment, self.flat_elems, "m"), _ptr(v, self._moment, self.flat_elems, "v"),
-                _ptr(scales, torch.uint8, 2 * self.blocks, "scales"))
+    def _state(self, dev, m, v, scales):
+        if dev != self.device.index:
+            _refuse(f"this AdamW was made on {self.device}, the current device is {dev}")
+        return (_ptr(m, dev, self._moment, self.flat_elems, "m"), _ptr(v, dev, self._moment, self.flat_elems, "v"), _ptr(scales, dev, torch.uint8, 2 * self.blocks, "scales"))
 
     def step(self, theta, grad, m, v, scales=None, *, step: int, lr: float, grad_scale: float = 1.0, seed: Optional[int] = None, copy=None, norm=None) -> None:
         """One step, in place.  `step` counts from 1; `grad_scale` multiplies the gradient (1 / accumulated micro-batches);
         `copy` receives a bfloat16 copy of the new parameters, `norm` (one fp32) the gradient's norm before clipping;
         `seed` (default: the step) seeds the rounding of an 8-bit second moment."""
-        pm, pv, ps = self._state(m, v, scales)
-        _check(_L.sl_adamw_step(self._h, _ptr(theta, self.param_dtype, self.flat_elems, "theta"), _ptr(grad, self.grad_dtype, self.flat_elems, "grad"), pm, pv, ps,
-                                _ptr(copy, torch.bfloat16, self.flat_elems, "copy"), _ptr(norm, torch.float32, 1, "norm"), step, lr, grad_scale,
-                                (step if seed is None else seed) & 0xFFFFFFFF, _stream()))
+        dev, n = _here(), self.flat_elems
+        pm, pv, ps = self._state(dev, m, v, scales)
+        _check(_L.sl_adamw_step(self._h, _ptr(theta, dev, self.param_dtype, n, "theta"), _ptr(grad, dev, self.grad_dtype, n, "grad"), pm, pv, ps,
+                                _ptr(copy, dev, torch.bfloat16, n, "copy"), _ptr(norm, dev, torch.float32, 1, "norm"), step, lr, grad_scale,
+                                (step if seed is None else seed) & 0xFFFFFFFF, _queue(dev)))
 
     def read_state(self, m, v, scales, m_out, v_out) -> None:
         """8-bit moments as fp32 values, in flat buffers of the same layout."""
-        pm, pv, ps = self._state(m, v, scales)
-        _check(_L.sl_adamw_read_state(self._h, pm, pv, ps, _ptr(m_out, torch.float32, self.flat_elems, "m_out"), _ptr(v_out, torch.float32, self.flat_elems, "v_out"), _stream()))
+        dev, n = _here(), self.flat_elems
+        pm, pv, ps = self._state(dev, m, v, scales)
+        _check(_L.sl_adamw_read_state(self._h, pm, pv, ps, _ptr(m_out, dev, torch.float32, n, "m_out"), _ptr(v_out, dev, torch.float32, n, "v_out"), _queue(dev)))
 
     def write_state(self, m_in, v_in, m, v, scales, *, seed: int = 0) -> None:
         """fp32 moments into the 8-bit form, rounded as a step rounds them."""
-        pm, pv, ps = self._state(m, v, scales)
-        _check(_L.sl_adamw_write_state(self._h, _ptr(m_in, torch.float32, self.flat_elems, "m_in"), _ptr(v_in, torch.float32, self.flat_elems, "v_in"), pm, pv, ps,
-                                       seed & 0xFFFFFFFF, _stream()))
+        dev, n = _here(), self.flat_elems
+        pm, pv, ps = self._state(dev, m, v, scales)
+        _check(_L.sl_adamw_write_state(self._h, _ptr(m_in, dev, torch.float32, n, "m_in"), _ptr(v_in, dev, torch.float32, n, "v_in"), pm, pv, ps, seed & 0xFFFFFFFF, _queue(dev)))
 
 
 # ------------------------------------------------------------------------------------------------------------- norms
-def _gate(gate, rows, cols, act, wt):
+def _gate(gate, dev, rows, cols, act, wt):
     """(kind, address, stride): [cols] = per column, [rows, 1] or (rows != cols) [rows] = per row, [rows, cols] = per element."""
-    if gate is None:
-        return GATES["none"], None, 0
-    if gate.dim() == 1 and gate.shape[0] == cols:
-        return GATES["column"], _ptr(gate, wt, cols, "column gate"), 0
-    _need(gate.is_cuda and gate.dtype == act, f"a row or element gate must be a CUDA tensor of {act}")
-    if gate.dim() == 1 and gate.shape[0] == rows or gate.dim() == 2 and tuple(gate.shape) == (rows, 1) and cols != 1:
-        _need(rows <= 1 or gate.stride(0) >= 1, "a row gate needs a positive stride")
-        return GATES["row"], gate.data_ptr(), gate.stride(0) if rows > 1 else 1
-    ptr, ld = _rows(gate, rows, cols, act, "element gate")
-    return GATES["full"], ptr, ld
+    sh = gate.shape
+    if len(sh) == 1 and sh[0] == cols:
+        return 1, _ptr(gate, dev, wt, cols, "column gate"), 0
+    if sh == (rows,) or (sh == (rows, 1) and cols != 1):
+        st = gate.stride(0)
+        if gate.get_device() != dev or gate.dtype is not act or (rows > 1 and st < 1):
+            _refuse(f"a row gate must be a CUDA tensor of {act} on device {dev} with a positive stride")
+        return 2, gate.data_ptr(), st if rows > 1 else 1
+    return (3, *_rows(gate, dev, rows, cols, act, "element gate"))
 
 
-def _norm_desc(x, weight, branch_weight, gate, alpha, eps):
-    _need(x.dim() == 2, "activations must be [rows, cols]")
+def _norm_desc(x, dev, weight, branch_weight, gate, alpha, eps):
+    if x.dim() != 2:
+        _refuse("activations must be [rows, cols]")
     rows, cols = x.shape
-    wt = next((w.dtype for w in (weight, branch_weight) if w is not None), gate.dtype if gate is not None and gate.dim() == 1 and gate.shape[0] == cols else torch.float32)
-    d = _NormDesc(rows, cols, _dtype(x.dtype), _dtype(wt), 0, alpha, eps)
-    d.gate_kind, g, d.ld_gate = _gate(gate, rows, cols, x.dtype, wt)
-    return d, rows, cols, wt, g
+    act = x.dtype
+    if weight is not None:
+        wt = weight.dtype
+    elif branch_weight is not None:
+        wt = branch_weight.dtype
+    else:
+        wt = gate.dtype if gate is not None and gate.shape == (cols,) else torch.float32
+    kind, g, ld = (0, None, 0) if gate is None else _gate(gate, dev, rows, cols, act, wt)
+    return _NormDesc(rows, cols, _dtype(act), _dtype(wt), kind, alpha, eps, 0, 0, ld), rows, cols, act, wt, g
 
 
 def norm_forward(x, weight=None, *, branch=None, branch_weight=None, gate=None, alpha: float = 1.0, eps: float = 1e-6, norm: bool = True, y=None, h=None, rstd=None, branch_rstd=None):
     """y = x + alpha * gate * norm(branch) (the norm only with `branch_weight`), h = norm(y) * weight (`norm=False`: no h).
     Returns (y, h, rstd, branch_rstd); y is x itself without a branch.  Outputs left out are allocated."""
-    d, rows, cols, wt, g = _norm_desc(x, weight, branch_weight, gate, alpha, eps)
-    act = x.dtype
+    dev = _here()
+    d, rows, cols, act, wt, g = _norm_desc(x, dev, weight, branch_weight, gate, alpha, eps)
     if branch is not None and y is None:
         y = torch.empty(rows, cols, dtype=act, device=x.device)
     if norm and h is None:
@@ -200,12 +217,12 @@ def norm_forward(x, weight=None, *, branch=None, branch_weight=None, gate=None, 
         rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
     if branch_weight is not None and branch_rstd is None:
         branch_rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
-    px, d.ld_x = _rows(x, rows, cols, act, "x")
-    pb, d.ld_branch = _rows(branch, rows, cols, act, "branch")
-    py, d.ld_y = _rows(y, rows, cols, act, "y") if branch is not None else (None, 0)
-    ph, d.ld_h = _rows(h, rows, cols, act, "h") if norm else (None, 0)
-    _check(_L.sl_norm_forward(C.byref(d), px, pb, _ptr(branch_weight, wt, cols, "branch_weight"), g, _ptr(weight, wt, cols, "weight"), py, ph,
-                              _ptr(branch_rstd, torch.float32, rows, "branch_rstd"), _ptr(rstd, torch.float32, rows, "rstd"), _stream()))
+    px, d.ld_x = _rows(x, dev, rows, cols, act, "x")
+    pb, d.ld_branch = _rows(branch, dev, rows, cols, act, "branch")
+    py, d.ld_y = _rows(y, dev, rows, cols, act, "y") if branch is not None else (None, 0)
+    ph, d.ld_h = _rows(h, dev, rows, cols, act, "h") if norm else (None, 0)
+    _check(_L.sl_norm_forward(C.byref(d), px, pb, _ptr(branch_weight, dev, wt, cols, "branch_weight"), g, _ptr(weight, dev, wt, cols, "weight"), py, ph,
+                              _ptr(branch_rstd, dev, torch.float32, rows, "branch_rstd"), _ptr(rstd, dev, torch.float32, rows, "rstd"), _queue(dev)))
     return y if branch is not None else x, h, rstd, branch_rstd
 
 
@@ -220,27 +237,30 @@ def norm_backward(dy, dh, y, weight=None, *, rstd=None, branch=None, branch_weig
                   dbranch_weight=None, dgate=None, workspace=None) -> None:
     """Gradients of `norm_forward`, written into the outputs that are given.  `y`, `rstd`, `branch_rstd` as the forward pass left them;
     dy (gradient that reaches y from elsewhere) or dh may be None."""
-    ref = y if y is not None else dy
-    d, rows, cols, wt, g = _norm_desc(ref, weight, branch_weight, gate, alpha, 0.0)
-    act = ref.dtype
-    pdy, d.ld_dy = _rows(dy, rows, cols, act, "dy")
-    pdh, d.ld_dh = _rows(dh, rows, cols, act, "dh")
-    py, d.ld_y = _rows(y, rows, cols, act, "y")
-    pb, d.ld_branch = _rows(branch, rows, cols, act, "branch")
-    pdx, d.ld_x = _rows(dx, rows, cols, act, "dx")
-    pdb, ld = _rows(dbranch, rows, cols, act, "dbranch")
-    _need(dbranch is None or rows <= 1 or ld == d.ld_branch, "dbranch must have the row stride of branch")
+    dev = _here()
+    d, rows, cols, act, wt, g = _norm_desc(y if y is not None else dy, dev, weight, branch_weight, gate, alpha, 0.0)
+    pdy, d.ld_dy = _rows(dy, dev, rows, cols, act, "dy")
+    pdh, d.ld_dh = _rows(dh, dev, rows, cols, act, "dh")
+    py, d.ld_y = _rows(y, dev, rows, cols, act, "y")
+    pb, ld_b = _rows(branch, dev, rows, cols, act, "branch")
+    d.ld_branch = ld_b
+    pdx, d.ld_x = _rows(dx, dev, rows, cols, act, "dx")
+    pdb, ld = _rows(dbranch, dev, rows, cols, act, "dbranch")
+    if dbranch is not None and ld != ld_b:
+        _refuse("dbranch must have the row stride of branch")
     pdg = None
     if dgate is not None:
-        _need(gate is not None and dgate.shape == gate.shape, "dgate must have the shape of gate")
-        kind, pdg, ld = _gate(dgate, rows, cols, act, wt)
-        _need(kind == d.gate_kind and (ld == d.ld_gate or rows <= 1), "dgate must have the strides of gate")
-    if workspace is None and (dweight is not None or dbranch_weight is not None or (dgate is not None and d.gate_kind == GATES["column"])):
+        if gate is None or dgate.shape != gate.shape:
+            _refuse("dgate must have the shape of gate")
+        kind, pdg, ld = _gate(dgate, dev, rows, cols, act, wt)
+        if ld != d.ld_gate:
+            _refuse("dgate must have the strides of gate")
+    if workspace is None and (dweight is not None or dbranch_weight is not None or (dgate is not None and d.gate_kind == 1)):
         workspace = norm_backward_workspace(rows, cols, dtype=act)
-    _check(_L.sl_norm_backward(C.byref(d), pdy, pdh, py, pb, _ptr(branch_weight, wt, cols, "branch_weight"), g, _ptr(weight, wt, cols, "weight"),
-                               _ptr(branch_rstd, torch.float32, rows, "branch_rstd"), _ptr(rstd, torch.float32, rows, "rstd"), pdx, pdb, _ptr(dweight, wt, cols, "dweight"),
-                               _ptr(dbranch_weight, wt, cols, "dbranch_weight"), pdg, _ptr(workspace, torch.uint8, 0, "workspace"),
-                               0 if workspace is None else workspace.numel(), _stream()))
+    _check(_L.sl_norm_backward(C.byref(d), pdy, pdh, py, pb, _ptr(branch_weight, dev, wt, cols, "branch_weight"), g, _ptr(weight, dev, wt, cols, "weight"),
+                               _ptr(branch_rstd, dev, torch.float32, rows, "branch_rstd"), _ptr(rstd, dev, torch.float32, rows, "rstd"), pdx, pdb, _ptr(dweight, dev, wt, cols, "dweight"),
+                               _ptr(dbranch_weight, dev, wt, cols, "dbranch_weight"), pdg, _ptr(workspace, dev, torch.uint8, 0, "workspace"),
+                               0 if workspace is None else workspace.numel(), _queue(dev)))
 
 
 class _BlockNorm(torch.autograd.Function):
@@ -286,9 +306,11 @@ class Rotary:
 
     def __init__(self, rot_dim: int, *, base: float = 10000.0, layout: str = "half", scaling: str = "none", factor: float = 1.0, original_length: float = 0.0, low_turns: float = 1.0,
                  high_turns: float = 32.0, magnitude: float = 1.0):
-        _need(layout in LAYOUTS and scaling in SCALINGS, f"layout {layout!r} / scaling {scaling!r} unknown")
+        if layout not in LAYOUTS or scaling not in SCALINGS:
+            _refuse(f"layout {layout!r} / scaling {scaling!r} unknown")
         cfg = _RotaryConfig(rot_dim, LAYOUTS[layout], SCALINGS[scaling], base, factor, original_length, low_turns, high_turns, magnitude)
         self._h, self.rot_dim = P(), rot_dim
+        self.device = torch.device("cuda", torch.cuda.current_device())
         _check(_L.sl_rotary_create(C.byref(cfg), C.byref(self._h)))
 
     def close(self) -> None:
@@ -305,31 +327,32 @@ class Rotary:
     def apply(self, q, k=None, positions=None, *, first: int = 0, inverse: bool = False, out_q=None, out_k=None) -> None:
         """Turns q (and k), [batch, seq, heads, head_dim] with any strides but a unit one inside a head: in place, or into
         out_q / out_k.  `positions`: int32 or int64 [seq] or [batch, seq]; None: first + token.  `inverse`: the backward pass."""
-        _need(q.dim() == 4, "q must be [batch, seq, heads, head_dim]")
+        dev = _here()
+        if dev != self.device.index or q.dim() != 4:
+            _refuse(f"q must be [batch, seq, heads, head_dim] on {self.device}, where this Rotary was made, and that the current device")
         batch, seq, _, head_dim = q.shape
-
-        def heads(x, out, what):
-            if x is None:
-                return None
-            out = x if out is None else out
-            _need(x.dim() == 4 and x.shape[0] == batch and x.shape[1] == seq and x.shape[3] == head_dim and out.shape == x.shape, f"{what}: shapes {tuple(x.shape)}, {tuple(out.shape)}")
-            _need(x.is_cuda and out.is_cuda and x.dtype == q.dtype and out.dtype == q.dtype, f"{what} must be CUDA tensors of {q.dtype}")
-            _need(head_dim == 1 or (x.stride(3) == 1 and out.stride(3) == 1), f"{what} must have a unit stride inside a head")
-            return _RotaryHeads(x.data_ptr(), out.data_ptr(), x.shape[2], *x.stride()[:3], *out.stride()[:3])
-
-        hq, hk = heads(q, out_q, "q"), heads(k, out_k, "k")
-        d = _RotaryDesc(_dtype(q.dtype), 64, int(inverse), batch, seq, head_dim, first)
-        pos = None
+        dtype = q.dtype
+        hq = _heads(q, q if out_q is None else out_q, dev, batch, seq, head_dim, dtype, "q")
+        hk = None if k is None else _heads(k, k if out_k is None else out_k, dev, batch, seq, head_dim, dtype, "k")
+        bits, pos, pos_batch, pos_token = 64, None, 0, 0
         if positions is not None:
-            _need(positions.is_cuda and positions.dtype in (torch.int32, torch.int64), "positions must be a CUDA tensor of int32 or int64")
-            _need(tuple(positions.shape) in ((seq,), (batch, seq)), f"positions must be [{seq}] or [{batch}, {seq}], got {tuple(positions.shape)}")
-            d.position_bits = 32 if positions.dtype == torch.int32 else 64
-            d.pos_token = positions.stride(-1)
-            d.pos_batch = positions.stride(0) if positions.dim() == 2 else 0
-            pos = positions.data_ptr()
+            sh, bits = positions.shape, 64 if positions.dtype is torch.int64 else 32 if positions.dtype is torch.int32 else 0
+            if positions.get_device() != dev or not bits or (sh != (batch, seq) and sh != (seq,)):
+                _refuse(f"positions must be a CUDA tensor [{seq}] or [{batch}, {seq}] of int32 or int64, got {positions.dtype} {tuple(sh)}")
+            st = positions.stride()
+            pos, pos_token, pos_batch = positions.data_ptr(), st[-1], st[0] if len(st) == 2 else 0
         if batch * seq == 0:
             return
-        _check(_L.sl_rotary_apply(self._h, C.byref(d), C.byref(hq), C.byref(hk) if hk is not None else None, pos, _stream()))
+        d = _RotaryDesc(_dtype(dtype), bits, inverse, batch, seq, head_dim, first, pos_batch, pos_token)
+        _check(_L.sl_rotary_apply(self._h, C.byref(d), C.byref(hq), None if hk is None else C.byref(hk), pos, _queue(dev)))
+
+
+def _heads(x, out, dev, batch, seq, head_dim, dtype, what):
+    sh, a, b = x.shape, x.stride(), out.stride()
+    if (len(sh) != 4 or sh[0] != batch or sh[1] != seq or sh[3] != head_dim or out.shape != sh or x.get_device() != dev or out.get_device() != dev or x.dtype is not dtype or
+            out.dtype is not dtype or (head_dim > 1 and (a[3] != 1 or b[3] != 1))):
+        _refuse(f"{what} must be CUDA tensors [{batch}, {seq}, heads, {head_dim}] of {dtype} on device {dev} with a unit stride inside a head, got {tuple(sh)} {x.dtype}, {tuple(out.shape)} {out.dtype}")
+    return _RotaryHeads(x.data_ptr(), out.data_ptr(), sh[2], a[0], a[1], a[2], b[0], b[1], b[2])
 
 
 class _Turn(torch.autograd.Function):
@@ -362,19 +385,24 @@ def token_loss(logits, targets, *, grad=None, ignore_index: int = -100, smoothin
                workspace=None):
     """Loss of every row of [rows, vocab] logits and, into `grad` (which may be `logits`), its gradient.  Returns (total, row_loss, lse):
     total = sum of the row losses, divided by the rows that count with `mean`, times `scale`; the gradient is total's."""
-    _need(logits.dim() == 2, "logits must be [rows, vocab]")
+    if logits.dim() != 2:
+        _refuse("logits must be [rows, vocab]")
+    dev = _here()
     rows, vocab = logits.shape
-    _need(targets.is_cuda and targets.is_contiguous() and tuple(targets.shape) == (rows,) and targets.dtype in (torch.int32, torch.int64), f"targets must be [{rows}] int32 or int64, contiguous, on the GPU")
-    d = _LossDesc(rows, vocab, _dtype(logits.dtype), 32 if targets.dtype == torch.int32 else 64, 0, 0, ignore_index, smoothing, z, scale, int(mean))
-    px, d.ld_logits = _rows(logits, rows, vocab, logits.dtype, "logits")
-    pg, d.ld_grad = _rows(grad, rows, vocab, logits.dtype, "grad")
-    dev = logits.device
-    row_loss = torch.empty(rows, device=dev) if row_loss is None else row_loss
-    lse = torch.empty(rows, device=dev) if lse is None else lse
-    total = torch.empty(1, device=dev) if total is None else total
+    act = logits.dtype
+    bits = 64 if targets.dtype is torch.int64 else 32 if targets.dtype is torch.int32 else 0
+    if not bits or targets.shape != (rows,):
+        _refuse(f"targets must be [{rows}] of int32 or int64, got {targets.dtype} {tuple(targets.shape)}")
+    pt = _ptr(targets, dev, targets.dtype, rows, "targets")
+    px, ld_x = _rows(logits, dev, rows, vocab, act, "logits")
+    pg, ld_g = _rows(grad, dev, rows, vocab, act, "grad")
+    row_loss = torch.empty(rows, device=logits.device) if row_loss is None else row_loss
+    lse = torch.empty(rows, device=logits.device) if lse is None else lse
+    total = torch.empty(1, device=logits.device) if total is None else total
     workspace = loss_workspace() if workspace is None else workspace
-    _check(_L.sl_token_loss(C.byref(d), px, targets.data_ptr(), pg, _ptr(row_loss, torch.float32, rows, "row_loss"), _ptr(lse, torch.float32, rows, "lse"),
-                            _ptr(total, torch.float32, 1, "total"), _ptr(workspace, torch.uint8, 0, "workspace"), workspace.numel(), _stream()))
+    d = _LossDesc(rows, vocab, _dtype(act), bits, ld_x, ld_g, ignore_index, smoothing, z, scale, mean)
+    _check(_L.sl_token_loss(C.byref(d), px, pt, pg, _ptr(row_loss, dev, torch.float32, rows, "row_loss"), _ptr(lse, dev, torch.float32, rows, "lse"),
+                            _ptr(total, dev, torch.float32, 1, "total"), _ptr(workspace, dev, torch.uint8, 0, "workspace"), workspace.numel(), _queue(dev)))
     return total, row_loss, lse
 
 
