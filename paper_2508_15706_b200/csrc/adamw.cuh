@@ -42,11 +42,18 @@ __device__ __forceinline__ unsigned mix32(unsigned x) {
     x *= 0x846CA68Bu;
     return x ^ (x >> 16);
 }
-// 19 random bits of element `i` under `seed`
+// 19 random bits of element i under a seed: mix32(i ^ key) >> 13.  Of four elements i, i + 1, .. from a multiple of 4 on, only the two
+// lowest bits differ, which the first shift leaves alone: `lot_base` is common to them.
 __device__ __forceinline__ unsigned hash_key(unsigned seed, unsigned long long i) {
     return mix32(seed) ^ mix32((unsigned)(i >> 32) * 0x9E3779B9u);
 }
-__device__ __forceinline__ unsigned lot19(unsigned key, unsigned i) { return mix32(i ^ key) >> 13; }
+__device__ __forceinline__ unsigned lot_base(unsigned key, unsigned i) { return (i ^ key) ^ ((i ^ key) >> 16); }
+__device__ __forceinline__ unsigned lot19(unsigned base, unsigned j) {  // j: 0..3
+    unsigned x = (base ^ j) * 0x7FEB352Du;
+    x ^= x >> 15;
+    x *= 0x846CA68Bu;
+    return (x ^ (x >> 16)) >> 13;
+}
 
 __device__ __forceinline__ float finite_abs(float x) {
     const float a = fabsf(x);
@@ -101,8 +108,11 @@ __device__ __forceinline__ void load8(const T* p, float (&f)[kAdamVec]) {
         Pack<T, 4> a, b;
         if (STREAM) a.load_stream(p), b.load_stream(p + 4);
         else a.load(p), b.load(p + 4);
+        float x[4], y[4];
+        a.get(x);
+        b.get(y);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = widen(a.v[i]), f[i + 4] = widen(b.v[i]);
+        for (int i = 0; i < 4; ++i) f[i] = x[i], f[i + 4] = y[i];
     }
 }
 template <class T, bool A8>
@@ -113,8 +123,9 @@ __device__ __forceinline__ void store8(T* p, const float (&f)[kAdamVec]) {
         a.store_stream(p);
     } else {
         Pack<T, 4> a, b;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) a.v[i] = narrow<T>(f[i]), b.v[i] = narrow<T>(f[i + 4]);
+        const float x[4] = {f[0], f[1], f[2], f[3]}, y[4] = {f[4], f[5], f[6], f[7]};
+        a.set(x);
+        b.set(y);
         a.store_stream(p);
         b.store_stream(p + 4);
     }
@@ -184,16 +195,19 @@ __device__ __forceinline__ void values_v(uint2 w, float scale, float (&v)[kAdamV
     for (int i = 0; i < kAdamVec; ++i) v[i] = value_v(((i < 4 ? w.x : w.y) >> (8 * (i & 3))) & 0xFFu) * scale;
 }
 // Codes of the thread's 8 moments; the 16 threads of a block agree on its scales.  Every lane of the warp takes part.
+// NAN_V: a v may be NaN though its m is not (never after a step, where both come from one gradient).
+template <bool NAN_V>
 __device__ __forceinline__ void encode_moments(const float (&m)[kAdamVec], const float (&v)[kAdamVec], unsigned seed, unsigned long long at,
                                                uint2& cm, uint2& cv, int& bm, int& bv) {
-    float tm = 0.0f, tv = 0.0f, odd = 0.0f;  // odd: 0, or NaN where a moment is not finite
+    float tm = 0.0f, tv = 0.0f, odd = 0.0f;  // odd: 0, or NaN where an m is not finite
 #pragma unroll
     for (int i = 0; i < kAdamVec; ++i) {
         tm = fmaxf(tm, fabsf(m[i]));
         tv = fmaxf(tv, v[i]);
-        odd = fmaf(m[i], 0.0f, fmaf(v[i], 0.0f, odd));
+        odd = fmaf(m[i], 0.0f, odd);
+        if (NAN_V) odd = fmaf(v[i], 0.0f, odd);
     }
-    const bool all_finite = __all_sync(kFullMask, odd == 0.0f);
+    const bool all_finite = __all_sync(kFullMask, odd == 0.0f && tv <= 3.402823466e38f);
     if (!all_finite) {
         tm = tv = 0.0f;
 #pragma unroll
@@ -211,18 +225,18 @@ __device__ __forceinline__ void encode_moments(const float (&m)[kAdamVec], const
     bv = scale_byte_v(tv);
     const float im = inv_pow2_byte(bm), iv = inv_pow2_byte(bv);
     // (8 consecutive offsets that begin at a multiple of 4 may cross a multiple of 2^32)
-    const unsigned low = (unsigned)at, key0 = hash_key(seed, at), key1 = hash_key(seed, at + 4);
+    const unsigned base0 = lot_base(hash_key(seed, at), (unsigned)at), base1 = lot_base(hash_key(seed, at + 4), (unsigned)at + 4u);
     unsigned c[kAdamVec];
     if (all_finite && bv < 254) {
         cm.x = code_m2(m[0] * im, m[1] * im) | (code_m2(m[2] * im, m[3] * im) << 16);
         cm.y = code_m2(m[4] * im, m[5] * im) | (code_m2(m[6] * im, m[7] * im) << 16);
 #pragma unroll
-        for (int i = 0; i < kAdamVec; ++i) c[i] = code_v(v[i] * iv, lot19(i < 4 ? key0 : key1, low + (unsigned)i));
+        for (int i = 0; i < kAdamVec; ++i) c[i] = code_v(v[i] * iv, lot19(i < 4 ? base0 : base1, (unsigned)(i & 3)));
     } else {
         cm.x = code_m2_any(m[0] * im, m[1] * im) | (code_m2_any(m[2] * im, m[3] * im) << 16);
         cm.y = code_m2_any(m[4] * im, m[5] * im) | (code_m2_any(m[6] * im, m[7] * im) << 16);
 #pragma unroll
-        for (int i = 0; i < kAdamVec; ++i) c[i] = code_v_any(v[i] * iv, lot19(i < 4 ? key0 : key1, low + (unsigned)i));
+        for (int i = 0; i < kAdamVec; ++i) c[i] = code_v_any(v[i] * iv, lot19(i < 4 ? base0 : base1, (unsigned)(i & 3)));
     }
     cv.x = __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
     cv.y = __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410);
@@ -316,15 +330,23 @@ struct AdamArgs {
 };
 
 // The moments are formed by single-rounded operations in the order of the formula, so that the 8-bit codes do not depend
-// on how a compiler contracts them.  sqrt and the division are the fast ones (2^-22 relative): theta's own rounding is coarser.
+// on how a compiler contracts them.  sqrt and reciprocal are the fast ones (2^-22 relative): theta's own rounding is coarser.
+// FLUSH: denormal operands of the two may count as 0, for a denominator of at least eps >= 1e-15 hides a sqrt(v) below 2^-63.
+template <bool FLUSH>
 __device__ __forceinline__ void adamw_element(float& p, float g, float& m, float& v, const AdamArgs& a, float c, float decay) {
     g = __fmul_rn(g, c);
     m = __fadd_rn(__fmul_rn(m, a.beta1), __fmul_rn(g, a.omb1));
     v = __fadd_rn(__fmul_rn(v, a.beta2), __fmul_rn(__fmul_rn(g, g), a.omb2));
-    float r;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
-    const float den = fmaf(r, a.inv_sqrt_bc2, a.eps);
-    p = fmaf(-a.step_size, __fdividef(m, den), fmaf(-decay, p, p));
+    float r, q;
+    if (FLUSH) {
+        asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(q) : "f"(fmaf(r, a.inv_sqrt_bc2, a.eps)));
+        q *= m;
+    } else {
+        asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+        q = __fdividef(m, fmaf(r, a.inv_sqrt_bc2, a.eps));
+    }
+    p = fmaf(-a.step_size, q, fmaf(-decay, p, p));
 }
 
 // What a thread reads for its 8 elements.
@@ -388,8 +410,13 @@ adamw_step_kernel(const AdamTile* __restrict__ tiles, const float* __restrict__ 
         x.moments(m, v);
 #pragma unroll
         for (int j = 0; j < kAdamVec; ++j) p[j] = x.p[j];
+        if (a.eps >= 1e-15f) {
 #pragma unroll
-        for (int j = 0; j < kAdamVec; ++j) adamw_element(p[j], x.g[j], m[j], v[j], a, c, decay);
+            for (int j = 0; j < kAdamVec; ++j) adamw_element<true>(p[j], x.g[j], m[j], v[j], a, c, decay);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kAdamVec; ++j) adamw_element<false>(p[j], x.g[j], m[j], v[j], a, c, decay);
+        }
         store_some<P, A8>(theta + i, n, p);
         if (a.copy) store_some<bf16, A8>(a.copy + tile.base + i, n, p);
         if (BITS == 32) {
@@ -403,7 +430,7 @@ adamw_step_kernel(const AdamTile* __restrict__ tiles, const float* __restrict__ 
             }
             uint2 cm, cv;
             int bm, bv;
-            encode_moments(m, v, a.seed, (unsigned long long)(tile.base + i), cm, cv, bm, bv);
+            encode_moments<false>(m, v, a.seed, (unsigned long long)(tile.base + i), cm, cv, bm, bv);
             store_codes<A8>(static_cast<uint8_t*>(a.m) + tile.base + i, n, cm);
             store_codes<A8>(static_cast<uint8_t*>(a.v) + tile.base + i, n, cv);
             if (n > 0 && (tid & 15) == 0) {
@@ -435,7 +462,7 @@ adamw_state_kernel(const AdamTile* __restrict__ tiles, float* m32, float* v32, u
             load_some<float, A8>(v32 + tile.base + i, n, v);
             uint2 cm, cv;
             int bm, bv;
-            encode_moments(m, v, seed, (unsigned long long)(tile.base + i), cm, cv, bm, bv);
+            encode_moments<true>(m, v, seed, (unsigned long long)(tile.base + i), cm, cv, bm, bv);
             store_codes<A8>(m8 + tile.base + i, n, cm);
             store_codes<A8>(v8 + tile.base + i, n, cv);
             if (n > 0 && (tid & 15) == 0) {

@@ -1,0 +1,283 @@
+// Residual update and norms around a block (sl_norm_forward, sl_norm_backward): host side of the C ABI declared in
+// include/sparseloco.h, over the kernels in block_norm.cuh.
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+#include <string.h>
+
+#include <algorithm>
+
+#include "sparseloco.h"
+
+#include "host.cuh"
+#include "inner_common.cuh"
+#include "block_norm.cuh"
+
+namespace {
+
+struct NormShape {
+    int vec, nv, threads, rows_per_cta;
+};
+
+// A warp takes a row of up to 32 vectors; wider rows are spread over a CTA of at most 512 threads, with as few vectors per thread
+// as that allows.  (Single values: four per thread at least.  Forward, two vectors from five warps a row on: a row's sums cost every
+// warp the same, however many columns it has.)
+NormShape norm_shape(int cols, int vec, bool backward) {
+    NormShape s;
+    s.vec = vec;
+    const int vectors = (cols + vec - 1) / vec;
+    const int need = (vectors + kNormMaxThreads - 1) / kNormMaxThreads;
+    if (vec >= 4) s.nv = need <= 1 && (backward || vectors <= 128) ? 1 : need <= 2 ? 2 : need <= 4 ? 4 : 8;
+    else if (vec == 2) s.nv = need <= 4 ? 4 : 16;
+    else s.nv = need <= 4 ? 4 : need <= 8 ? 8 : 32;
+    s.threads = ((vectors + s.nv - 1) / s.nv + 31) / 32 * 32;
+    s.rows_per_cta = s.threads == 32 ? kNormWarpRows : 1;
+    return s;
+}
+
+// CTAs per SM: the registers of a thread decide (the kernels' launch bounds hold them to this)
+int norm_ctas(const NormShape& s, bool backward) {
+    return std::max(1, std::min(32, 65536 / norm_regs(s.nv * s.vec, backward) / (s.threads * s.rows_per_cta)));
+}
+unsigned norm_grid(const NormShape& s, long long rows, int n_sms, bool backward) {
+    const long long want = (rows + s.rows_per_cta - 1) / s.rows_per_cta;
+    return (unsigned)std::min(want, (long long)n_sms * norm_ctas(s, backward));
+}
+// Rows in a CTA's ring: up to four, as many as the SM's shared memory holds for its CTAs, two at least (one being used, one on its
+// way), but no more than a CTA has rows.
+int norm_stages(const NormShape& s, int arrays, int bytes, long long rows, unsigned grid, bool backward) {
+    const long long one = (long long)s.threads * s.rows_per_cta * s.nv * s.vec * bytes * arrays;
+    const long long fit = 220ll * 1024 / norm_ctas(s, backward) / one;
+    const long long has = (rows + (long long)grid * s.rows_per_cta - 1) / ((long long)grid * s.rows_per_cta) + 1;
+    return (int)std::max(2ll, std::min(std::min(4ll, fit), has));
+}
+
+template <class T, class W, int VEC, int NV, bool FULL>
+sl_status launch_norm_gate(const NormArgs& given, const NormShape& s, unsigned grid, bool backward, cudaStream_t st) {
+    NormArgs a = given;
+    const int arrays = (backward ? 4 : 2) + (FULL ? 1 : 0), threads = s.threads * s.rows_per_cta;
+    a.stages = norm_stages(s, arrays, (int)sizeof(T), a.rows, grid, backward);
+    const bool few = backward ? kNormFewBackward<VEC, NV> : kNormFew<VEC, NV>;
+    size_t smem = few ? (size_t)threads * NV * VEC * sizeof(T) * arrays * a.stages : 0;
+    if (backward && s.rows_per_cta > 1) smem = std::max(smem, sizeof(float) * 2 * (size_t)a.cols);
+    auto kern = backward ? norm_backward_kernel<T, W, VEC, NV, FULL> : norm_forward_kernel<T, W, VEC, NV, FULL>;
+    if (smem > 47 * 1024) SL_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024));  // (1 KB stays for the sums)
+    kern<<<grid, dim3((unsigned)s.threads, (unsigned)s.rows_per_cta), smem, st>>>(a);
+    SL_CUDA(cudaGetLastError());
+    return SL_OK;
+}
+
+template <class T, class W, int VEC, int NV>
+sl_status launch_norm(const NormArgs& a, const NormShape& s, unsigned grid, bool backward, cudaStream_t st) {
+    return a.gate_kind == SL_GATE_FULL ? launch_norm_gate<T, W, VEC, NV, true>(a, s, grid, backward, st) : launch_norm_gate<T, W, VEC, NV, false>(a, s, grid, backward, st);
+}
+
+template <class T, class W>
+sl_status launch_norm_shape(const NormArgs& a, const NormShape& s, unsigned grid, bool backward, cudaStream_t st) {
+    constexpr int V = 16 / (int)sizeof(T);
+    if (s.vec == 1) return s.nv == 4 ? launch_norm<T, W, 1, 4>(a, s, grid, backward, st) : s.nv == 8 ? launch_norm<T, W, 1, 8>(a, s, grid, backward, st)
+                                                                                                     : launch_norm<T, W, 1, 32>(a, s, grid, backward, st);
+    if (s.vec == 2) return s.nv == 4 ? launch_norm<T, W, 2, 4>(a, s, grid, backward, st) : launch_norm<T, W, 2, 16>(a, s, grid, backward, st);
+    if (s.nv == 1) return launch_norm<T, W, V, 1>(a, s, grid, backward, st);
+    if (s.nv == 2) return launch_norm<T, W, V, 2>(a, s, grid, backward, st);
+    if (s.nv == 4) return launch_norm<T, W, V, 4>(a, s, grid, backward, st);
+    return launch_norm<T, W, V, 32 / V>(a, s, grid, backward, st);
+}
+
+sl_status launch_norm_types(const sl_norm_desc* d, const NormArgs& a, const NormShape& s, unsigned grid, bool backward, cudaStream_t st) {
+    if (d->dtype == SL_F32) return launch_norm_shape<float, float>(a, s, grid, backward, st);
+    if (d->weight_dtype == SL_F32) return launch_norm_shape<bf16, float>(a, s, grid, backward, st);
+    return launch_norm_shape<bf16, bf16>(a, s, grid, backward, st);
+}
+
+template <class W>
+sl_status launch_norm_columns(const NormArgs& a, unsigned parts, const void* column_gate, void* dweight, void* dbranch_weight, void* dgate, cudaStream_t st) {
+    cudaLaunchConfig_t lc;
+    memset(&lc, 0, sizeof(lc));
+    lc.gridDim = dim3((unsigned)((2 * a.cols + 31) / 32));
+    lc.blockDim = dim3(1024);
+    lc.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = at;
+    lc.numAttrs = parts ? 1 : 0;  // only behind the backward kernel, which waits for what came before it
+    SL_CUDA(cudaLaunchKernelEx(&lc, norm_columns_kernel<W>, (const float*)a.part, (int)parts, a.cols, static_cast<const W*>(a.branch_weight),
+                               static_cast<const W*>(column_gate), static_cast<W*>(dweight), static_cast<W*>(dbranch_weight), static_cast<W*>(dgate)));
+    return SL_OK;
+}
+
+sl_status norm_check(const sl_norm_desc* d) {
+    if (!d || d->rows < 0 || d->cols < 1 || !isfinite(d->alpha) || !finite_at_least(d->eps, 0.0)) return SL_ERR_INVALID_ARG;
+    if (!known_dtype(d->dtype) || !known_dtype(d->weight_dtype)) return SL_ERR_UNSUPPORTED;
+    if (d->dtype == SL_F32 && d->weight_dtype != SL_F32) return SL_ERR_UNSUPPORTED;
+    if (d->gate_kind < SL_GATE_NONE || d->gate_kind > SL_GATE_FULL) return SL_ERR_INVALID_ARG;
+    if (d->cols > kNormMaxCols || d->rows > 0x7FFFFFFFll) return SL_ERR_TOO_LARGE;
+    const int64_t ld[] = {d->ld_x, d->ld_branch, d->ld_y, d->ld_h, d->ld_dy, d->ld_dh};
+    for (int64_t l : ld)
+        if (l != 0 && l < d->cols) return SL_ERR_INVALID_ARG;
+    if (d->ld_gate < 0 || (d->gate_kind == SL_GATE_FULL && d->ld_gate != 0 && d->ld_gate < d->cols)) return SL_ERR_INVALID_ARG;
+    return SL_OK;
+}
+
+void norm_strides(const sl_norm_desc* d, NormArgs* a) {
+    memset(a, 0, sizeof(*a));
+    a->rows = d->rows;
+    a->cols = (int)d->cols;
+    a->gate_kind = d->gate_kind;
+    a->alpha = d->alpha;
+    a->eps = d->eps;
+    a->inv_cols = 1.0f / (float)d->cols;
+    a->ld_x = d->ld_x ? d->ld_x : d->cols;
+    a->ld_branch = d->ld_branch ? d->ld_branch : d->cols;
+    a->ld_y = d->ld_y ? d->ld_y : d->cols;
+    a->ld_h = d->ld_h ? d->ld_h : d->cols;
+    a->ld_dy = d->ld_dy ? d->ld_dy : d->cols;
+    a->ld_dh = d->ld_dh ? d->ld_dh : d->cols;
+    a->ld_gate = d->ld_gate ? d->ld_gate : (d->gate_kind == SL_GATE_FULL ? d->cols : 1);
+}
+
+// The values per access that columns, row strides and pointers of everything allow: 16 bytes, or two values, or one.
+struct NormAlign {
+    int bytes, vec;
+    bool element;
+    explicit NormAlign(const sl_norm_desc* d) : bytes(dtype_bytes(d->dtype)), vec(16 / dtype_bytes(d->dtype)), element(true) { all(d->cols); }
+    void all(long long n) { vec = n % vec == 0 ? vec : n % 2 == 0 ? std::min(vec, 2) : 1; }
+    void matrix(const void* p, long long ld) {
+        if (!p) return;
+        element = element && fits(p, bytes);
+        all(ld);
+        all((long long)(reinterpret_cast<uintptr_t>(p) / (unsigned)bytes));
+    }
+    void vector(const void* p, int b) {  // weights: 16 bytes at a time, or as many values
+        if (!p) return;
+        element = element && fits(p, b);
+        if (vec > 2 && !fits(p, 16)) vec = 2;
+        if (vec == 2 && !fits(p, 2 * b)) vec = 1;
+    }
+};
+
+}  // namespace
+
+extern "C" {
+
+sl_status sl_norm_forward(const sl_norm_desc* d, const void* x, const void* branch, const void* branch_weight, const void* gate, const void* weight,
+                          void* y, void* h, float* branch_rstd, float* rstd, void* stream) {
+    sl_status s = norm_check(d);
+    if (s != SL_OK || d->rows == 0) return s;  // (matrices without rows have no address to check)
+    if (!x || (!y && !h) || (branch != nullptr) != (y != nullptr) || (branch_weight && !branch) || (weight && !h)) return SL_ERR_INVALID_ARG;
+    if ((d->gate_kind != SL_GATE_NONE) != (gate != nullptr) || (gate && !branch)) return SL_ERR_INVALID_ARG;
+    NormArgs a;
+    norm_strides(d, &a);
+    a.x = x;
+    a.branch = branch;
+    a.branch_weight = branch_weight;
+    a.gate = gate;
+    a.weight = weight;
+    a.y = y;
+    a.h = h;
+    a.branch_rstd = branch_rstd;
+    a.rstd = rstd;
+    const int wb = dtype_bytes(d->weight_dtype);
+    NormAlign al(d);
+    al.matrix(x, a.ld_x);
+    al.matrix(branch, a.ld_branch);
+    al.matrix(y, a.ld_y);
+    al.matrix(h, a.ld_h);
+    al.vector(branch_weight, wb);
+    al.vector(weight, wb);
+    if (d->gate_kind == SL_GATE_COLUMN) al.vector(gate, wb);
+    else if (d->gate_kind == SL_GATE_FULL) al.matrix(gate, a.ld_gate);
+    else if (!fits(gate, al.bytes)) return SL_ERR_ALIGNMENT;
+    if (!al.element || !fits(branch_rstd, 4) || !fits(rstd, 4)) return SL_ERR_ALIGNMENT;
+    const NormShape sh = norm_shape(a.cols, al.vec, false);
+    int n_sms = 0;
+    s = sm_count(&n_sms);
+    if (s != SL_OK) return s;
+    const unsigned grid = norm_grid(sh, d->rows, n_sms, false);
+    return launch_norm_types(d, a, sh, grid, false, static_cast<cudaStream_t>(stream));
+}
+
+sl_status sl_norm_workspace_bytes(const sl_norm_desc* d, size_t* bytes) {
+    sl_status s = norm_check(d);
+    if (s != SL_OK) return s;
+    if (!bytes) return SL_ERR_INVALID_ARG;
+    int n_sms = 0;
+    s = sm_count(&n_sms);
+    if (s != SL_OK) return s;
+    // the largest of the launch shapes that alignment decides between
+    size_t most = 0;
+    for (int vec : {1, 2, 16 / dtype_bytes(d->dtype)}) {
+        const NormShape sh = norm_shape((int)d->cols, vec, true);
+        most = std::max(most, sizeof(float) * 2 * (size_t)d->cols * norm_grid(sh, d->rows, n_sms, true));
+    }
+    *bytes = up256(most);
+    return SL_OK;
+}
+
+sl_status sl_norm_backward(const sl_norm_desc* d, const void* dy, const void* dh, const void* y, const void* branch, const void* branch_weight,
+                           const void* gate, const void* weight, const float* branch_rstd, const float* rstd, void* dx, void* dbranch, void* dweight,
+                           void* dbranch_weight, void* dgate, void* workspace, size_t workspace_bytes, void* stream) {
+    sl_status s = norm_check(d);
+    if (s != SL_OK) return s;
+    const bool rows = d->rows > 0;  // (matrices without rows have no address to check)
+    if (rows && ((!dy && !dh) || (dh && (!y || !rstd)) || (branch_weight && (!branch || !branch_rstd)) || (weight && !dh))) return SL_ERR_INVALID_ARG;
+    if (rows && ((d->gate_kind != SL_GATE_NONE) != (gate != nullptr) || (gate && !branch) || (dbranch && !branch))) return SL_ERR_INVALID_ARG;
+    if ((dweight && !weight) || (dbranch_weight && !branch_weight) || (rows && dgate && !gate)) return SL_ERR_INVALID_ARG;
+    if (rows && !dx && !dbranch && !dweight && !dbranch_weight && !dgate) return SL_ERR_INVALID_ARG;
+    NormArgs a;
+    norm_strides(d, &a);
+    a.dy = dy;
+    a.dh = dh;
+    a.x = y;
+    a.branch = branch;
+    a.branch_weight = branch_weight;
+    a.gate = gate;
+    a.weight = weight;
+    a.branch_rstd = const_cast<float*>(branch_rstd);
+    a.rstd = const_cast<float*>(rstd);
+    a.dx = dx;
+    a.dbranch = dbranch;
+    a.dgate = d->gate_kind == SL_GATE_COLUMN ? nullptr : dgate;
+    const int wb = dtype_bytes(d->weight_dtype);
+    NormAlign al(d);
+    al.matrix(dy, a.ld_dy);
+    al.matrix(dh, a.ld_dh);
+    if (dh) al.matrix(y, a.ld_y);
+    al.matrix(branch, a.ld_branch);
+    al.matrix(dx, a.ld_x);
+    al.matrix(dbranch, a.ld_branch);
+    al.vector(branch_weight, wb);
+    al.vector(weight, wb);
+    if (d->gate_kind == SL_GATE_COLUMN) al.vector(gate, wb);
+    else if (d->gate_kind == SL_GATE_FULL) al.matrix(gate, a.ld_gate), al.matrix(dgate, a.ld_gate);
+    else if (!fits(gate, al.bytes) || !fits(dgate, al.bytes)) return SL_ERR_ALIGNMENT;
+    if (!al.element || !fits(branch_rstd, 4) || !fits(rstd, 4) || !fits(dweight, wb) || !fits(dbranch_weight, wb) || misaligned(workspace) ||
+        (d->gate_kind == SL_GATE_COLUMN && !fits(dgate, wb)))
+        return SL_ERR_ALIGNMENT;
+    const bool columns = dweight || dbranch_weight || (d->gate_kind == SL_GATE_COLUMN && dgate);
+    int n_sms = 0;
+    s = sm_count(&n_sms);
+    if (s != SL_OK) return s;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const NormShape sh = norm_shape(a.cols, al.vec, true);
+    const unsigned grid = norm_grid(sh, d->rows, n_sms, true);
+    if (columns) {
+        if (grid && (!workspace || workspace_bytes < sizeof(float) * 2 * (size_t)a.cols * grid)) return SL_ERR_NOMEM;
+        a.part = static_cast<float*>(workspace);
+    }
+    if (grid) {
+        s = launch_norm_types(d, a, sh, grid, true, st);
+        if (s != SL_OK) return s;
+    }
+    if (columns) {
+        void* dg = d->gate_kind == SL_GATE_COLUMN ? dgate : nullptr;
+        const void* cg = d->gate_kind == SL_GATE_COLUMN ? gate : nullptr;
+        s = d->weight_dtype == SL_F32 ? launch_norm_columns<float>(a, grid, cg, dweight, dbranch_weight, dg, st)
+                                      : launch_norm_columns<bf16>(a, grid, cg, dweight, dbranch_weight, dg, st);
+        if (s != SL_OK) return s;
+    }
+    return SL_OK;
+}
+
+}  // extern "C"

@@ -32,18 +32,27 @@ struct NormArgs {
     float* part;  // [CTAs][2][cols] column sums: of dh yhat, and of alpha dx bhat (times a row or element gate)
 };
 
-// Sum of K values over the threads of a row, the same in all of them: lanes, then (rows wider than a warp) up to 16 warps through
-// `buf` (K * 16 floats; those of absent warps are 0).  `buf` must not be written again before every thread has read it: callers
-// alternate between two.
+// Sum of K (1 or 3) values over the threads of a row, the same in all of them: lanes, then (rows wider than a warp) up to 16 warps
+// through `buf` (K * 16 floats; those of absent warps are 0).  `buf` must not be written again before every thread has read it:
+// callers alternate between two.
 template <int K>
 __device__ __forceinline__ void row_sums(float (&s)[K], float* buf) {
-#pragma unroll
-    for (int k = 0; k < K; ++k) s[k] = warp_sum(s[k]);
-    if (blockDim.x <= 32) return;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (lane == 0) {
+    if (K == 1 || blockDim.x <= 32) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) buf[k * 16 + warp] = s[k];
+        for (int k = 0; k < K; ++k) s[k] = warp_sum(s[k]);
+        if (blockDim.x <= 32) return;
+        if (lane == 0) buf[warp] = s[0];
+    } else {
+        // three sums at once: with every halving of the lanes that share a value, each lane keeps half of the values
+        const bool high = lane & 16, odd = lane & 8;
+        const float p = (high ? s[K - 1] : s[0]) + __shfl_xor_sync(kFullMask, high ? s[0] : s[K - 1], 16);
+        const float q = (high ? 0.0f : s[K / 2]) + __shfl_xor_sync(kFullMask, high ? s[K / 2] : 0.0f, 16);
+        float v = (odd ? q : p) + __shfl_xor_sync(kFullMask, odd ? p : q, 8);
+        v += __shfl_xor_sync(kFullMask, v, 4);
+        v += __shfl_xor_sync(kFullMask, v, 2);
+        v += __shfl_xor_sync(kFullMask, v, 1);
+        if ((lane & 7) == 0 && lane != 24) buf[(high ? 2 : odd ? 1 : 0) * 16 + warp] = v;
     }
     __syncthreads();
     const int mask = blockDim.x > 256 ? 15 : blockDim.x > 128 ? 7 : blockDim.x > 64 ? 3 : 1;
@@ -64,15 +73,21 @@ __device__ __forceinline__ void clear_sums(float* buf, int n) {
 
 __device__ __forceinline__ float reciprocal_root(float x) { return rsqrtf(x); }  // 2 ulp
 
-// The columns of a thread: vector i begins at column (i * blockDim.x + threadIdx.x) * VEC.
+// A thread's columns: `pieces` of at most NV pieces of VEC columns, piece i from column (i * blockDim.x + threadIdx.x) * VEC on.
 template <int VEC>
 __device__ __forceinline__ int norm_column(int i) { return (i * (int)blockDim.x + (int)threadIdx.x) * VEC; }
+template <int VEC, int NV>
+__device__ __forceinline__ int norm_pieces(int cols) {
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) n += norm_column<VEC>(i) < cols;
+    return n;
+}
 
 template <int BYTES>
-__device__ __forceinline__ void copy_async(void* shared, const void* global) {
-    const unsigned at = (unsigned)__cvta_generic_to_shared(shared);
-    if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(global) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(global), "n"(BYTES) : "memory");
+__device__ __forceinline__ void copy_async(unsigned shared, const void* global) {
+    if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(shared), "l"(global) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(shared), "l"(global), "n"(BYTES) : "memory");
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void copy_wait(int behind) {  // all but the `behind` last groups have landed, for this thread
@@ -80,111 +95,132 @@ __device__ __forceinline__ void copy_wait(int behind) {  // all but the `behind`
     else if (behind == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
     else asm volatile("cp.async.wait_group 3;" ::: "memory");
 }
+template <int BYTES>
+__device__ __forceinline__ void shared_load(unsigned at, void* to) {
+    unsigned* w = static_cast<unsigned*>(to);
+    if (BYTES == 16) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at));
+    else if (BYTES == 8) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at));
+    else if (BYTES == 4) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(at));
+    else {
+        unsigned short h;
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(at));
+        *static_cast<unsigned short*>(to) = h;
+    }
+}
 
-// Where a thread finds its pieces of a row.  RING: a ring of rows in shared memory that it fills for itself, asynchronously and
-// rows ahead (a piece is read by the thread that copied it, so nothing is waited for but the copy); places of absent matrices and
-// of columns beyond the row's end are zeroed once.  Else (many columns per thread): global memory.
+// One matrix as a thread sees it.  RING: a ring of rows in shared memory that the thread fills for itself, asynchronously and rows
+// ahead (a piece is read by the thread that copied it, so nothing is waited for but the copy); places of absent matrices and of
+// columns beyond the row's end are zeroed once.  Else (many columns per thread): global memory.
 template <class T, int VEC, int NV, bool RING>
 struct NormMatrix {
     typedef Pack<T, VEC> Piece;
-    const T* ahead;     // the thread's first column in the row to be copied next (null: absent)
-    const T* now;       // ... in the present row (where there is no ring)
-    long long step;     // elements from one of the CTA's rows to the next
-    char* places;       // this thread's first piece of stage 0
-    __device__ __forceinline__ NormMatrix(const void* base, long long ld, long long row, long long stride, char* ring, int array) {
-        ahead = base ? static_cast<const T*>(base) + row * ld + norm_column<VEC>(0) : nullptr;
-        now = ahead;
-        step = stride * ld;
-        places = ring + ((size_t)array * NV * blockDim.x * blockDim.y + threadIdx.y * blockDim.x + threadIdx.x) * sizeof(Piece);
+    const T* row;    // the thread's first column in the row to be copied (RING) or used next; null: absent
+    long long step;  // elements from one of the CTA's rows to the next
+    unsigned place;  // shared address of its first piece in the ring's first row
+    __device__ __forceinline__ NormMatrix(const void* base, long long ld, long long first, long long stride, const char* ring, int array) {
+        row = base ? static_cast<const T*>(base) + first * ld + norm_column<VEC>(0) : nullptr;
+        step = base ? stride * ld : 0;
+        place = (unsigned)__cvta_generic_to_shared(ring) + (unsigned)((array * NV * blockDim.x * blockDim.y + threadIdx.y * blockDim.x + threadIdx.x) * sizeof(Piece));
     }
     static __device__ __forceinline__ int offset(int i) { return i * (int)blockDim.x * VEC; }
-    __device__ __forceinline__ Piece* place(int stage_bytes, int i) const {
-        return reinterpret_cast<Piece*>(places + stage_bytes + i * (int)(blockDim.x * blockDim.y * sizeof(Piece)));
-    }
-    __device__ __forceinline__ void clear(int stages, int stage_bytes, int cols) const {
+    static __device__ __forceinline__ unsigned pitch(int i) { return (unsigned)i * (unsigned)(blockDim.x * blockDim.y * sizeof(Piece)); }
+    __device__ __forceinline__ void clear(int stages, unsigned stage_bytes, int pieces) const {
         for (int s = 0; s < stages; ++s)
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                if (!ahead || norm_column<VEC>(i) >= cols)
+                if (!row || i >= pieces)
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) place(s * stage_bytes, i)->v[j] = narrow<T>(0.0f);
+                    for (int j = 0; j < VEC * (int)sizeof(T); j += 2)
+                        asm volatile("st.shared.u16 [%0], %1;" ::"r"(place + (unsigned)s * stage_bytes + pitch(i) + (unsigned)j), "h"((unsigned short)0) : "memory");
     }
-    __device__ __forceinline__ void fetch(int stage_at, int cols) {
-        if (!ahead) return;
+    __device__ __forceinline__ void fetch(unsigned stage_at, int pieces) {
+        if (!row) return;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            if (norm_column<VEC>(i) < cols) {
-                if constexpr (Piece::kBytes >= 4) copy_async<Piece::kBytes>(place(stage_at, i), ahead + offset(i));
-                else place(stage_at, i)->v[0] = ahead[offset(i)];
+            if (i < pieces) {
+                if constexpr (Piece::kBytes >= 4) {
+                    copy_async<Piece::kBytes>(place + stage_at + pitch(i), row + offset(i));
+                } else {
+                    const unsigned short h = *reinterpret_cast<const unsigned short*>(row + offset(i));
+                    asm volatile("st.shared.u16 [%0], %1;" ::"r"(place + stage_at + pitch(i)), "h"(h) : "memory");
+                }
             }
         }
-        ahead += step;
+        row += step;
     }
-    __device__ __forceinline__ void get(int stage_at, int i, int cols, float (&f)[VEC]) const {
-        Piece t;
-        if constexpr (RING) {
-            t = *place(stage_at, i);
-            t.get(f);
-        } else if (now && norm_column<VEC>(i) < cols) {
-            t.load(now + offset(i));
-            t.get(f);
-        } else {
+    // all of the thread's values as pairs, 0 beyond the row's end or without a matrix
+    __device__ __forceinline__ void get(unsigned stage_at, int pieces, float2 (&f)[NV * VEC / 2]) const {
+        float g[NV * VEC];
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) f[j] = 0.0f;
+        for (int i = 0; i < NV; ++i) {
+            Piece t;
+            if constexpr (RING) {
+                shared_load<Piece::kBytes>(place + stage_at + pitch(i), &t);
+            } else {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) t.v[j] = narrow<T>(0.0f);
+                if (row && i < pieces) t.load(row + offset(i));
+            }
+            float x[VEC];
+            t.get(x);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) g[i * VEC + j] = x[j];
         }
+#pragma unroll
+        for (int i = 0; i < NV * VEC / 2; ++i) f[i] = make_float2(g[2 * i], g[2 * i + 1]);
     }
-    __device__ __forceinline__ void next() { now += now ? step : 0; }
+    __device__ __forceinline__ void next() {
+        if (!RING) row += step;
+    }
 };
 
-// Weights of a thread's columns, 1 where there are none.
+// A row of an output, by the same pieces.
+template <class T, int VEC, int NV>
+__device__ __forceinline__ void norm_store(T* row, int pieces, const float2 (&f)[NV * VEC / 2]) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (i < pieces) {
+            float x[VEC];
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) x[j] = (i * VEC + j) % 2 ? f[(i * VEC + j) / 2].y : f[(i * VEC + j) / 2].x;
+            Pack<T, VEC> t;
+            t.set(x);
+            t.store(row + i * (int)blockDim.x * VEC);
+        }
+    }
+}
+
+// Weights of a thread's columns (times those of `times`), 1 where there are none.
 template <class W, int VEC, int NV>
-struct NormWeights {
-    float f[NV][VEC];
-    __device__ __forceinline__ void set(const void* w, const void* times, int cols) {
+__device__ __forceinline__ void norm_weights(const void* w, const void* times, int pieces, float2 (&f)[NV * VEC / 2]) {
+    float g[NV * VEC];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
+    for (int i = 0; i < NV; ++i) {
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) f[i][j] = 1.0f;
-            const int c = norm_column<VEC>(i);
-            if (c < cols) {
-                Pack<W, VEC> t;
-                if (w) {
-                    t.load(static_cast<const W*>(w) + c);
-                    t.get(f[i]);
-                }
-                if (times) {
-                    t.load(static_cast<const W*>(times) + c);
+        for (int j = 0; j < VEC; ++j) g[i * VEC + j] = 1.0f;
+        if (i < pieces) {
+            Pack<W, VEC> t;
+            if (w) {
+                t.load(static_cast<const W*>(w) + norm_column<VEC>(i));
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) f[i][j] *= widen(t.v[j]);
-                }
+                for (int j = 0; j < VEC; ++j) g[i * VEC + j] = widen(t.v[j]);
+            }
+            if (times) {
+                t.load(static_cast<const W*>(times) + norm_column<VEC>(i));
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) g[i * VEC + j] *= widen(t.v[j]);
             }
         }
     }
-};
-
-// Weights of piece i: kept, or (many columns per thread) fetched again.
-template <class W, int VEC, int NV, bool KEEP>
-__device__ __forceinline__ void norm_weights(const NormWeights<W, VEC, NV>& kept, const void* w, const void* times, int i, int cols, float (&f)[VEC]) {
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) f[j] = KEEP ? kept.f[i][j] : 1.0f;
-    const int c = norm_column<VEC>(i);
-    if (!KEEP && c < cols) {
-        Pack<W, VEC> t;
-        if (w) {
-            t.load(static_cast<const W*>(w) + c);
-            t.get(f);
-        }
-        if (times) {
-            t.load(static_cast<const W*>(times) + c);
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) f[j] *= widen(t.v[j]);
-        }
-    }
+    for (int i = 0; i < NV * VEC / 2; ++i) f[i] = make_float2(g[2 * i], g[2 * i + 1]);
 }
 
 // Few columns per thread: their weights stay in registers and rows come through the ring.
 template <int VEC, int NV>
 constexpr bool kNormFew = NV * VEC <= 16;
+template <int VEC, int NV>
+constexpr bool kNormFewBackward = NV * VEC <= 8;
 
 // T: activations, W: weights; VEC values per access, NV accesses per thread: blockDim.x * VEC * NV >= cols; FULL: a gate per element.
 // blockDim.y rows per CTA, more than one only where blockDim.x is a warp.
@@ -192,6 +228,7 @@ template <class T, class W, int VEC, int NV, bool FULL>
 __global__ void __launch_bounds__(NV* VEC <= 8 ? 1024 : NV * VEC <= 16 ? 640 : kNormMaxThreads)
 norm_forward_kernel(const NormArgs a) {
     constexpr bool kFew = kNormFew<VEC, NV>;
+    constexpr int P = NV * VEC / 2;
     extern __shared__ __align__(16) char ring[];
     __shared__ float sums[2][16];
     clear_sums(sums[0], 32);
@@ -199,96 +236,78 @@ norm_forward_kernel(const NormArgs a) {
     long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y;
     const bool normed = a.branch_weight != nullptr, has_branch = a.branch != nullptr;
     const void* column_gate = a.gate_kind == SL_GATE_COLUMN ? a.gate : nullptr;
-    NormMatrix<T, VEC, NV, kFew> x(a.x, a.ld_x, row, stride, ring, 0), b(a.branch, a.ld_branch, row, stride, ring, 1), g(FULL ? a.gate : nullptr, a.ld_gate, row, stride, ring, 2);
-    const int stage_bytes = (FULL ? 3 : 2) * NV * VEC * (int)(sizeof(T) * blockDim.x * blockDim.y), ring_bytes = a.stages * stage_bytes;
-    if constexpr (kFew) {
-        x.clear(a.stages, stage_bytes, a.cols);
-        b.clear(a.stages, stage_bytes, a.cols);
-        if (FULL) g.clear(a.stages, stage_bytes, a.cols);
-    }
+    const int pieces = norm_pieces<VEC, NV>(a.cols);
+    NormMatrix<T, VEC, NV, kFew> mx(a.x, a.ld_x, row, stride, ring, 0), mb(a.branch, a.ld_branch, row, stride, ring, 1), mg(FULL ? a.gate : nullptr, a.ld_gate, row, stride, ring, 2);
+    const unsigned stage_bytes = (unsigned)((FULL ? 3 : 2) * NV * VEC * sizeof(T) * blockDim.x * blockDim.y), ring_bytes = (unsigned)a.stages * stage_bytes;
     long long coming = row;  // the row to be copied next
-    auto fetch = [&](int stage_at) {
+    auto fetch = [&](unsigned stage_at) {
         if (coming < a.rows) {
-            x.fetch(stage_at, a.cols);
-            b.fetch(stage_at, a.cols);
-            if (FULL) g.fetch(stage_at, a.cols);
+            mx.fetch(stage_at, pieces);
+            mb.fetch(stage_at, pieces);
+            if (FULL) mg.fetch(stage_at, pieces);
         }
         coming += stride;
         copy_commit();
     };
-    if (kFew)
-        for (int k = 0; k < a.stages - 1; ++k) fetch(k * stage_bytes);
-    NormWeights<W, VEC, NV> w, c;
+    if constexpr (kFew) {
+        mx.clear(a.stages, stage_bytes, pieces);
+        mb.clear(a.stages, stage_bytes, pieces);
+        if (FULL) mg.clear(a.stages, stage_bytes, pieces);
+        for (int k = 0; k < a.stages - 1; ++k) fetch((unsigned)k * stage_bytes);
+    }
+    float2 w[P], c[P];
     if (kFew) {
-        w.set(a.weight, nullptr, a.cols);
-        c.set(a.branch_weight, column_gate, a.cols);
+        norm_weights<W, VEC, NV>(a.weight, nullptr, pieces, w);
+        norm_weights<W, VEC, NV>(a.branch_weight, column_gate, pieces, c);
     }
     T* y = static_cast<T*>(a.y) + (a.y ? row * a.ld_y + norm_column<VEC>(0) : 0);
     T* h = static_cast<T*>(a.h) + (a.h ? row * a.ld_h + norm_column<VEC>(0) : 0);
-    for (int at = 0; row < a.rows; row += stride) {
+    for (unsigned at = 0; row < a.rows; row += stride) {
         if (kFew) {
             fetch(at ? at - stage_bytes : ring_bytes - stage_bytes);
             copy_wait(a.stages - 1);
         }
-        float v[NV][VEC];
+        float2 v[P];
         if (has_branch) {
-            float z[NV][VEC], rb = 1.0f;
-#pragma unroll
-            for (int i = 0; i < NV; ++i) b.get(at, i, a.cols, z[i]);
+            float2 z[P];
+            float rb = 1.0f;
+            mb.get(at, pieces, z);
             if (normed) {
-                float s[1] = {0.0f};
+                float2 q = both(0.0f);
 #pragma unroll
-                for (int i = 0; i < NV; ++i)
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) s[0] = fmaf(z[i][j], z[i][j], s[0]);
+                for (int i = 0; i < P; ++i) q = fma2(z[i], z[i], q);
+                float s[1] = {q.x + q.y};
                 row_sums<1>(s, sums[0]);
                 rb = reciprocal_root(fmaf(s[0], a.inv_cols, a.eps));
                 if (a.branch_rstd && threadIdx.x == 0) a.branch_rstd[row] = rb;
             }
             float scale = a.alpha * rb;
             if (a.gate_kind == SL_GATE_ROW) scale *= widen(static_cast<const T*>(a.gate)[row * a.ld_gate]);
+            mx.get(at, pieces, v);
+            float2 g[P];
+            if (FULL) mg.get(at, pieces, g);
+            if (!kFew) norm_weights<W, VEC, NV>(a.branch_weight, column_gate, pieces, c);
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                float gi[VEC], ci[VEC];
-                x.get(at, i, a.cols, v[i]);
-                if (FULL) g.get(at, i, a.cols, gi);
-                norm_weights<W, VEC, NV, kFew>(c, a.branch_weight, column_gate, i, a.cols, ci);
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) v[i][j] = fmaf(FULL ? ci[j] * gi[j] : ci[j], scale * z[i][j], v[i][j]);
-                if (norm_column<VEC>(i) < a.cols) {
-                    Pack<T, VEC> t;
-                    t.set(v[i]);
-                    t.store(y + x.offset(i));
-                }
-            }
+            for (int i = 0; i < P; ++i) v[i] = fma2(mul2(z[i], both(scale)), FULL ? mul2(c[i], g[i]) : c[i], v[i]);
+            norm_store<T, VEC, NV>(y, pieces, v);
             y += stride * a.ld_y;
         } else {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) x.get(at, i, a.cols, v[i]);
+            mx.get(at, pieces, v);
         }
-        at = at + stage_bytes == ring_bytes ? 0 : at + stage_bytes;
-        x.next(), b.next(), g.next();
+        at = at + stage_bytes == ring_bytes ? 0u : at + stage_bytes;
+        mx.next(), mb.next(), mg.next();
         if (!a.h) continue;
-        float s[1] = {0.0f};
+        float2 q = both(0.0f);
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) s[0] = fmaf(v[i][j], v[i][j], s[0]);  // (0 beyond the row's end)
+        for (int i = 0; i < P; ++i) q = fma2(v[i], v[i], q);  // (0 beyond the row's end)
+        float s[1] = {q.x + q.y};
         row_sums<1>(s, sums[1]);
         const float r = reciprocal_root(fmaf(s[0], a.inv_cols, a.eps));
         if (a.rstd && threadIdx.x == 0) a.rstd[row] = r;
+        if (!kFew) norm_weights<W, VEC, NV>(a.weight, nullptr, pieces, w);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            if (norm_column<VEC>(i) < a.cols) {
-                float wi[VEC];
-                norm_weights<W, VEC, NV, kFew>(w, a.weight, nullptr, i, a.cols, wi);
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) wi[j] *= v[i][j] * r;
-                Pack<T, VEC> t;
-                t.set(wi);
-                t.store(h + x.offset(i));
-            }
-        }
+        for (int i = 0; i < P; ++i) v[i] = mul2(mul2(v[i], both(r)), w[i]);
+        norm_store<T, VEC, NV>(h, pieces, v);
         h += stride * a.ld_h;
     }
 }
@@ -298,12 +317,12 @@ norm_forward_kernel(const NormArgs a) {
 //     s0 = sum u yhat;   s1 = sum q (dy + r u);   s2 = sum q yhat
 // give mean(u yhat) = s0 / cols and sum q dx = s1 - r s0 / cols s2, from which both mean(dz branch_weight bhat) and a row gate's
 // gradient follow.  Two column sums serve three gradients: dbranch_weight and a column gate's are the sum of alpha dx bhat times the
-// other one's weight.  The row's pieces are read again for the second half rather than kept: registers decide how many rows are
-// under way.
+// other one's weight.
 template <class T, class W, int VEC, int NV, bool FULL>
 __global__ void __launch_bounds__(NV* VEC <= 8 ? 640 : kNormMaxThreads)
 norm_backward_kernel(const NormArgs a) {
-    constexpr bool kFew = NV * VEC <= 8;
+    constexpr bool kFew = kNormFewBackward<VEC, NV>;
+    constexpr int P = NV * VEC / 2;
     extern __shared__ __align__(16) char ring[];  // afterwards [2][cols] column sums, only where blockDim.y > 1
     __shared__ float sums[2][3 * 16];
     clear_sums(sums[0], 2 * 3 * 16);
@@ -311,24 +330,18 @@ norm_backward_kernel(const NormArgs a) {
     long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y;
     const bool normed = a.branch_weight != nullptr, row_gate = a.gate_kind == SL_GATE_ROW;
     const void* column_gate = a.gate_kind == SL_GATE_COLUMN ? a.gate : nullptr;
+    const int pieces = norm_pieces<VEC, NV>(a.cols);
     NormMatrix<T, VEC, NV, kFew> mdy(a.dy, a.ld_dy, row, stride, ring, 0), mdh(a.dh, a.ld_dh, row, stride, ring, 1), my(a.dh ? a.x : nullptr, a.ld_y, row, stride, ring, 2),
         mb(a.branch, a.ld_branch, row, stride, ring, 3), mg(FULL ? a.gate : nullptr, a.ld_gate, row, stride, ring, 4);
-    const int stage_bytes = (FULL ? 5 : 4) * NV * VEC * (int)(sizeof(T) * blockDim.x * blockDim.y), ring_bytes = a.stages * stage_bytes;
-    if constexpr (kFew) {
-        mdy.clear(a.stages, stage_bytes, a.cols);
-        mdh.clear(a.stages, stage_bytes, a.cols);
-        my.clear(a.stages, stage_bytes, a.cols);
-        mb.clear(a.stages, stage_bytes, a.cols);
-        if (FULL) mg.clear(a.stages, stage_bytes, a.cols);
-    }
+    const unsigned stage_bytes = (unsigned)((FULL ? 5 : 4) * NV * VEC * sizeof(T) * blockDim.x * blockDim.y), ring_bytes = (unsigned)a.stages * stage_bytes;
     long long coming = row;
-    auto fetch = [&](int stage_at) {
+    auto fetch = [&](unsigned stage_at) {
         if (coming < a.rows) {
-            mdy.fetch(stage_at, a.cols);
-            mdh.fetch(stage_at, a.cols);
-            my.fetch(stage_at, a.cols);
-            mb.fetch(stage_at, a.cols);
-            if (FULL) mg.fetch(stage_at, a.cols);
+            mdy.fetch(stage_at, pieces);
+            mdh.fetch(stage_at, pieces);
+            my.fetch(stage_at, pieces);
+            mb.fetch(stage_at, pieces);
+            if (FULL) mg.fetch(stage_at, pieces);
         }
         coming += stride;
         copy_commit();
@@ -339,95 +352,81 @@ norm_backward_kernel(const NormArgs a) {
         if (normed) rb_next = a.branch_rstd[at];
         if (row_gate) rg_next = widen(static_cast<const T*>(a.gate)[at * a.ld_gate]);
     };
-    if (kFew)
-        for (int k = 0; k < a.stages - 1; ++k) fetch(k * stage_bytes);
-    if (row < a.rows) scalars(row);
-    NormWeights<W, VEC, NV> w, c;
-    if (kFew) {
-        w.set(a.weight, nullptr, a.cols);
-        c.set(a.branch_weight, column_gate, a.cols);
+    if constexpr (kFew) {
+        mdy.clear(a.stages, stage_bytes, pieces);
+        mdh.clear(a.stages, stage_bytes, pieces);
+        my.clear(a.stages, stage_bytes, pieces);
+        mb.clear(a.stages, stage_bytes, pieces);
+        if (FULL) mg.clear(a.stages, stage_bytes, pieces);
+        for (int k = 0; k < a.stages - 1; ++k) fetch((unsigned)k * stage_bytes);
     }
-    float acc[2][NV][VEC];
+    if (row < a.rows) scalars(row);
+    float2 w[P], c[P], acc[2][P];
+    if (kFew) {
+        norm_weights<W, VEC, NV>(a.weight, nullptr, pieces, w);
+        norm_weights<W, VEC, NV>(a.branch_weight, column_gate, pieces, c);
+    }
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) acc[0][i][j] = acc[1][i][j] = 0.0f;
+    for (int i = 0; i < P; ++i) acc[0][i] = acc[1][i] = both(0.0f);
     T* dx = static_cast<T*>(a.dx) + (a.dx ? row * a.ld_x + norm_column<VEC>(0) : 0);
     T* dbranch = static_cast<T*>(a.dbranch) + (a.dbranch ? row * a.ld_branch + norm_column<VEC>(0) : 0);
     T* dgate = static_cast<T*>(a.dgate) + (FULL && a.dgate ? row * a.ld_gate + norm_column<VEC>(0) : 0);
     int turn = 0;
-    for (int at = 0; row < a.rows; row += stride, turn ^= 1) {
+    for (unsigned at = 0; row < a.rows; row += stride, turn ^= 1) {
         if (kFew) {
             fetch(at ? at - stage_bytes : ring_bytes - stage_bytes);
             copy_wait(a.stages - 1);
+        } else {
+            norm_weights<W, VEC, NV>(a.weight, nullptr, pieces, w);
+            norm_weights<W, VEC, NV>(a.branch_weight, column_gate, pieces, c);
         }
         const float r = r_next, rb = rb_next, rg = rg_next;
         if (row + stride < a.rows) scalars(row + stride);
-        auto piece = [&](int i, float (&dy)[VEC], float (&dh)[VEC], float (&yh)[VEC], float (&bh)[VEC], float (&g)[VEC], float (&wi)[VEC], float (&ci)[VEC]) {
-            mdy.get(at, i, a.cols, dy);
-            mdh.get(at, i, a.cols, dh);
-            my.get(at, i, a.cols, yh);
-            mb.get(at, i, a.cols, bh);
-            if (FULL) mg.get(at, i, a.cols, g);
-            norm_weights<W, VEC, NV, kFew>(w, a.weight, nullptr, i, a.cols, wi);
-            norm_weights<W, VEC, NV, kFew>(c, a.branch_weight, column_gate, i, a.cols, ci);
+        float2 dy[P], dh[P], yh[P], bh[P], g[P];
+        mdy.get(at, pieces, dy);
+        mdh.get(at, pieces, dh);
+        my.get(at, pieces, yh);
+        mb.get(at, pieces, bh);
+        if (FULL) mg.get(at, pieces, g);
+        float2 t0 = both(0.0f), t1 = t0, t2 = t0;
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                yh[j] *= r;
-                bh[j] *= rb;
-            }
-        };
-        float s[3] = {0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            float dy[VEC], dh[VEC], yh[VEC], bh[VEC], g[VEC], wi[VEC], ci[VEC];
-            piece(i, dy, dh, yh, bh, g, wi, ci);
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                const float u = dh[j] * wi[j], q = FULL ? bh[j] * ci[j] * g[j] : bh[j] * ci[j];
-                s[0] = fmaf(u, yh[j], s[0]);
-                s[1] = fmaf(q, fmaf(r, u, dy[j]), s[1]);
-                s[2] = fmaf(q, yh[j], s[2]);
-            }
+        for (int i = 0; i < P; ++i) {
+            yh[i] = mul2(yh[i], both(r));
+            bh[i] = mul2(bh[i], both(rb));
+            const float2 u = mul2(dh[i], w[i]), q = FULL ? mul2(mul2(bh[i], c[i]), g[i]) : mul2(bh[i], c[i]);
+            t0 = fma2(u, yh[i], t0);
+            t1 = fma2(q, fma2(both(r), u, dy[i]), t1);
+            t2 = fma2(q, yh[i], t2);
         }
+        float s[3] = {t0.x + t0.y, t1.x + t1.y, t2.x + t2.y};
         row_sums<3>(s, sums[turn]);
         const float mean = s[0] * a.inv_cols;
         const float qdx = fmaf(-r * mean, s[2], s[1]);         // sum q dx
         const float bmean = a.alpha * rg * qdx * a.inv_cols;    // mean(dz branch_weight bhat)
         if (row_gate && a.dgate && threadIdx.x == 0) static_cast<T*>(a.dgate)[row * a.ld_gate] = narrow<T>(a.alpha * qdx);
         const float scale = a.alpha * rg, rbm = normed ? rb * bmean : 0.0f;
+        mdy.get(at, pieces, dy);  // (read again rather than kept over the exchange: registers decide how many CTAs are resident)
+        mdh.get(at, pieces, dh);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            if (norm_column<VEC>(i) >= a.cols) continue;
-            float dy[VEC], dh[VEC], yh[VEC], bh[VEC], g[VEC], wi[VEC], ci[VEC];
-            piece(i, dy, dh, yh, bh, g, wi, ci);
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                acc[0][i][j] = fmaf(dh[j], yh[j], acc[0][i][j]);
-                dy[j] = fmaf(r, fmaf(dh[j], wi[j], -yh[j] * mean), dy[j]);     // dx
-                const float up = scale * dy[j], e = FULL ? up * g[j] : up;
-                acc[1][i][j] = fmaf(e, bh[j], acc[1][i][j]);
-                dh[j] = fmaf(rb * e, ci[j], -bh[j] * rbm);                      // dbranch (rb is 1 and rbm 0 without its norm)
-                if (FULL) g[j] = up * bh[j] * ci[j];                            // the element gate's (c is branch_weight then)
+        for (int i = 0; i < P; ++i) {
+            acc[0][i] = fma2(dh[i], yh[i], acc[0][i]);
+            dy[i] = fma2(both(r), fma2(yh[i], both(-mean), mul2(dh[i], w[i])), dy[i]);  // dx
+            float2 e = mul2(dy[i], both(scale));
+            if (FULL) {
+                const float2 up = e;
+                e = mul2(e, g[i]);
+                g[i] = mul2(up, mul2(bh[i], c[i]));                                       // the element gate's (c is branch_weight then)
             }
-            Pack<T, VEC> t;
-            if (a.dx) {
-                t.set(dy);
-                t.store(dx + mdy.offset(i));
-            }
-            if (a.dbranch) {
-                t.set(dh);
-                t.store(dbranch + mdy.offset(i));
-            }
-            if (FULL && a.dgate) {
-                t.set(g);
-                t.store(dgate + mdy.offset(i));
-            }
+            acc[1][i] = fma2(e, bh[i], acc[1][i]);
+            dh[i] = fma2(mul2(e, both(rb)), c[i], mul2(bh[i], both(-rbm)));                // dbranch (rb is 1 and rbm 0 without its norm)
         }
+        if (a.dx) norm_store<T, VEC, NV>(dx, pieces, dy);
+        if (a.dbranch) norm_store<T, VEC, NV>(dbranch, pieces, dh);
+        if (FULL && a.dgate) norm_store<T, VEC, NV>(dgate, pieces, g);
         dx += stride * a.ld_x;
         dbranch += stride * a.ld_branch;
         if (FULL) dgate += stride * a.ld_gate;
-        at = at + stage_bytes == ring_bytes ? 0 : at + stage_bytes;
+        at = at + stage_bytes == ring_bytes ? 0u : at + stage_bytes;
         mdy.next(), mdh.next(), my.next(), mb.next(), mg.next();
     }
     cudaTriggerProgrammaticLaunchCompletion();
@@ -446,7 +445,8 @@ norm_backward_kernel(const NormArgs a) {
 #pragma unroll
                         for (int j = 0; j < VEC; ++j) {
                             const int at = k * a.cols + col + j;
-                            const float sum = t ? colsum[at] + acc[k][i][j] : acc[k][i][j];
+                            const float own = (i * VEC + j) % 2 ? acc[k][(i * VEC + j) / 2].y : acc[k][(i * VEC + j) / 2].x;
+                            const float sum = t ? colsum[at] + own : own;
                             if (t == (int)blockDim.y - 1) part[at] = sum;
                             else colsum[at] = sum;
                         }

@@ -1,6 +1,7 @@
 // Host-side helpers shared by the translation units of libsparseloco.
 #pragma once
 #include <cuda_runtime.h>
+#include <math.h>
 #include <stdint.h>
 #include <stdio.h>
 
@@ -23,6 +24,17 @@ sl_status cuda_fail(cudaError_t e, const char* what) {
 
 inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 inline bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+
+sl_status sm_count(int* n) {
+    int dev = 0;
+    SL_CUDA(cudaGetDevice(&dev));
+    SL_CUDA(cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev));
+    return SL_OK;
+}
+
+inline bool known_dtype(int t) { return t == SL_F32 || t == SL_BF16; }
+inline int dtype_bytes(int t) { return t == SL_F32 ? 4 : 2; }
+inline bool finite_at_least(double x, double low) { return isfinite(x) && x >= low; }
 
 struct DeviceGuard {
     int prev;

@@ -58,15 +58,47 @@ struct Pack {
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) __stcs(reinterpret_cast<Raw*>(p) + i, raw[i]);
     }
+    // (bfloat16 by pairs: a shift and a mask one way, one conversion of two values the other)
     __device__ __forceinline__ void get(float (&f)[N]) const {
+        if constexpr (sizeof(T) == 2 && N % 2 == 0) {
+            const unsigned* w = reinterpret_cast<const unsigned*>(raw);
 #pragma unroll
-        for (int i = 0; i < N; ++i) f[i] = widen(v[i]);
+            for (int i = 0; i < N; i += 2) {
+                f[i] = __uint_as_float(w[i / 2] << 16);
+                f[i + 1] = __uint_as_float(w[i / 2] & 0xFFFF0000u);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) f[i] = widen(v[i]);
+        }
     }
     __device__ __forceinline__ void set(const float (&f)[N]) {
+        if constexpr (sizeof(T) == 2 && N % 2 == 0) {
+            unsigned* w = reinterpret_cast<unsigned*>(raw);
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = narrow<T>(f[i]);
+            for (int i = 0; i < N; i += 2) {
+                const __nv_bfloat162 b = __floats2bfloat162_rn(f[i], f[i + 1]);
+                w[i / 2] = *reinterpret_cast<const unsigned*>(&b);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = narrow<T>(f[i]);
+        }
     }
 };
+
+// Two fp32 operations in one instruction; each half is rounded as the single one is.
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+__device__ __forceinline__ float2 add2(float2 a, float2 b) { return __fadd2_rn(a, b); }
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) { return __fmul2_rn(a, b); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
+
+// 32 bits that hold two bfloat16, the first one low, as floats and back
+__device__ __forceinline__ float2 widen2(unsigned w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
+__device__ __forceinline__ unsigned narrow2(float2 f) {
+    const __nv_bfloat162 b = __floats2bfloat162_rn(f.x, f.y);
+    return *reinterpret_cast<const unsigned*>(&b);
+}
 
 template <class V>
 __device__ __forceinline__ V warp_sum(V x) {

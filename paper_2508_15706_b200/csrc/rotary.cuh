@@ -52,25 +52,43 @@ struct RopeItem {
             if (!in_place) a.store(out + r.rot + (slot - r.rot_slots) * VEC);
         } else if (HALF) {
             const int c = slot * VEC;
+            float x[VEC], y[VEC];
+            a.get(x);
+            b.get(y);
+            if constexpr (VEC > 1) {
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) turn(a.v[j], b.v[j], cs[j * r.rot_slots]);
+                for (int j = 0; j < VEC; j += 2) {
+                    const float2 e = cs[j * r.rot_slots], f = cs[(j + 1) * r.rot_slots];
+                    const float2 co = make_float2(e.x, f.x), si = make_float2(e.y, f.y), p = make_float2(x[j], x[j + 1]), q = make_float2(y[j], y[j + 1]);
+                    const float2 u = fma2(p, co, mul2(q, make_float2(-si.x, -si.y))), v = fma2(q, co, mul2(p, si));
+                    x[j] = u.x, x[j + 1] = u.y, y[j] = v.x, y[j + 1] = v.y;
+                }
+            } else {
+                turn(x[0], y[0], cs[0]);
+            }
+            a.set(x);
+            b.set(y);
             a.store(out + c);
             b.store(out + r.rot / 2 + c);
         } else if (VEC > 1) {
             const int c = slot * VEC;
+            float x[VEC];
+            a.get(x);
 #pragma unroll
-            for (int j = 0; j + 1 < VEC; j += 2) turn(a.v[j], a.v[j + 1], cs[(j / 2) * r.rot_slots]);
+            for (int j = 0; j + 1 < VEC; j += 2) turn(x[j], x[j + 1], cs[(j / 2) * r.rot_slots]);
+            a.set(x);
             a.store(out + c);
         } else {
-            turn(a.v[0], b.v[0], cs[0]);
-            out[2 * slot] = a.v[0];
-            out[2 * slot + 1] = b.v[0];
+            float x = widen(a.v[0]), y = widen(b.v[0]);
+            turn(x, y, cs[0]);
+            out[2 * slot] = narrow<T>(x);
+            out[2 * slot + 1] = narrow<T>(y);
         }
     }
-    static __device__ __forceinline__ void turn(T& x, T& y, float2 e) {
-        const float p = widen(x), q = widen(y);
-        x = narrow<T>(fmaf(p, e.x, -q * e.y));
-        y = narrow<T>(fmaf(q, e.x, p * e.y));
+    static __device__ __forceinline__ void turn(float& x, float& y, float2 e) {
+        const float p = x, q = y;
+        x = fmaf(p, e.x, -q * e.y);
+        y = fmaf(q, e.x, p * e.y);
     }
 };
 

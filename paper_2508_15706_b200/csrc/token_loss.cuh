@@ -2,8 +2,10 @@
 //
 // Bound: HBM (logits read once, gradient written once).  A row stays in the registers of its CTA, or of the CTAs of a cluster where
 // one CTA cannot hold it or there are fewer rows than SMs: one pass for a maximum and a sum of exponentials per thread, one
-// exchange, then the gradient from the same registers.  (The maximum is taken off before the factor log2 e: a row of the type's
-// lowest value would overflow the other way round.)
+// exchange, then the gradient from the same registers.
+// Exponentials are 2^(x log2 e - M), one fused multiply-add and one instruction: M stands for the maximum in that scale, and its
+// rounding moves nothing as long as it is the same M everywhere.  Where |x log2 e| could overflow (a row of the type's lowest
+// value) the factor is 1 instead: numbers of that size are equal or differ by more than any exponential can show.
 // Rows that eight CTAs cannot hold, and gradients that sit elsewhere relative to 16 bytes than their logits, go through a kernel that
 // reads the row twice (the second time from L2).
 #pragma once
@@ -54,28 +56,30 @@ loss_count_kernel(const LossArgs a) {
     }
 }
 
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-__device__ __forceinline__ float exp_fast(float x) {  // e^x, 0 for -inf; relative error 2^-22 and the argument's rounding
+__device__ __forceinline__ float exp2_fast(float x) {  // 2^x, relative error 2^-22; 0 for -inf
     float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x * kLog2e));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ float loss_scale(float top) { return fabsf(top) < 1e30f ? kLog2e : 1.0f; }  // (1 for infinities)
+__device__ __forceinline__ float loss_offset(float top) { return top == -INFINITY ? 0.0f : top * loss_scale(top); }
 
-// Maximum and sum of exponentials relative to it; -inf with 0 = nothing seen, NaN and +inf end in the sum.
+// Scaled maximum and sum of exponentials relative to it; -inf with 0 = nothing seen, NaN and +inf end in the sum.
 __device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
     const float top = fmaxf(m, m2);
     if (top == -INFINITY) {
         s += s2;
         return;
     }
-    s = s * exp_fast(m - top) + s2 * exp_fast(m2 - top);
+    s = s * exp2_fast(m - top) + s2 * exp2_fast(m2 - top);
     m = top;
 }
 
 // What a row comes to, from its maximum, sum and target.
 struct LossRow {
-    float m, s, sum, lse, w;
+    float m, s, sum, lse, w, scale;
     long long target;
     int valid;
     bool counts, inside, empty;
@@ -83,7 +87,8 @@ struct LossRow {
 };
 __device__ __forceinline__ void finish_row(const LossArgs& a, LossRow& r) {
     r.empty = r.m == -INFINITY && r.s == 0.0f;  // every logit is -inf
-    r.lse = r.empty ? -INFINITY : r.m + logf(r.s);
+    r.scale = fabsf(r.m) < 1e30f ? kLog2e : 1.0f;
+    r.lse = r.empty ? -INFINITY : r.scale == 1.0f ? r.m + logf(r.s) : (r.m + log2f(r.s)) * kLn2;
     cudaGridDependencySynchronize();
     r.valid = __ldcg(&a.work->valid);
     r.w = a.mean ? a.scale / (float)(r.valid > 0 ? r.valid : 1) : a.scale;
@@ -162,31 +167,39 @@ loss_row_kernel(const LossArgs a, const T* logits, T* grad, int cluster) {
 
     float m = fmaxf(first, last_one);
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int i = 0; i < NV; ++i) {
+        float f[VEC];
+        v[i].get(f);
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) m = fmaxf(m, widen(v[i].v[j]));
-    const float ref = m == -INFINITY ? 0.0f : m;
-    float s = exp_fast(first - ref) + exp_fast(last_one - ref), sum = 0.0f;
+        for (int j = 0; j < VEC; ++j) m = fmaxf(m, f[j]);
+    }
+    const float scale = loss_scale(m), ref = loss_offset(m);
+    float s = exp2_fast(fmaf(first, scale, -ref)) + exp2_fast(fmaf(last_one, scale, -ref)), sum = 0.0f;
     if (a.smoothing != 0.0f) {
         sum = (before >= 0 ? first : 0.0f) + (behind >= 0 ? last_one : 0.0f);
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-            if (begin + i * threads + tid < end)
+            if (begin + i * threads + tid < end) {
+                float f[VEC];
+                v[i].get(f);
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) sum += widen(v[i].v[j]);
+                for (int j = 0; j < VEC; ++j) sum += f[j];
+            }
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        float part = 0.0f;  // (short chains of additions)
+        float f[VEC], part = 0.0f;  // (short chains of additions)
+        v[i].get(f);
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) part += exp_fast(widen(v[i].v[j]) - ref);
+        for (int j = 0; j < VEC; ++j) part += exp2_fast(fmaf(f[j], scale, -ref));
         s += part;
     }
+    m *= scale;
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
         const float m2 = __shfl_xor_sync(kFullMask, m, o), s2 = __shfl_xor_sync(kFullMask, s, o);
         join(m, s, m2, s2);
-        sum += __shfl_xor_sync(kFullMask, sum, o);
+        if (a.smoothing != 0.0f) sum += __shfl_xor_sync(kFullMask, sum, o);
     }
     if ((tid & 31) == 0) sm[tid >> 5] = m, ss[tid >> 5] = s, sx[tid >> 5] = sum;
     __syncthreads();
@@ -217,14 +230,15 @@ loss_row_kernel(const LossArgs a, const T* logits, T* grad, int cluster) {
                     hit = r.w * (1.0f - a.smoothing);
         const int t = some ? (int)r.target : -1;
         const int tv = t >= head && t < tail ? (t - head) / VEC : -1, te = t - head - tv * VEC;  // the target's vector and place in it
-        const float top = some ? r.m : 0.0f;
+        const float top = some ? r.m : 0.0f, scale = r.scale;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int at = begin + i * threads + tid;
             if (at < end) {
                 float f[VEC];
+                v[i].get(f);
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) f[j] = fmaf(k, exp_fast(widen(v[i].v[j]) - top), -off);
+                for (int j = 0; j < VEC; ++j) f[j] = fmaf(k, exp2_fast(fmaf(f[j], scale, -top)), -off);
                 if (at == tv) {
 #pragma unroll
                     for (int j = 0; j < VEC; ++j)
@@ -240,7 +254,7 @@ loss_row_kernel(const LossArgs a, const T* logits, T* grad, int cluster) {
             }
         }
         auto one = [&](int at, float val) {
-            float d = some ? fmaf(k, exp_fast(val - top), -off) : 0.0f;
+            float d = some ? fmaf(k, exp2_fast(fmaf(val, scale, -top)), -off) : 0.0f;
             if (at == t) d -= hit;
             g[at] = narrow<T>(d);
         };
@@ -271,15 +285,19 @@ loss_stream_kernel(const LossArgs a, const T* logits, T* grad) {
     r.counts = r.target != a.ignore_index;
     r.inside = r.target >= 0 && r.target < a.vocab;
     float m = -INFINITY, s = 0.0f, sum = 0.0f;
-    auto rise = [&](float top) {  // the maximum so far goes up to top
+    float scale = kLog2e, ref = 0.0f;           // m in the scale of the exponentials
+    auto rise = [&](float top) {                // the maximum so far goes up to top
         if (top > m) {
-            s *= exp_fast(m - top);
+            const float to = loss_offset(top);
+            s *= exp2_fast(m == -INFINITY ? m : ref - to);
             m = top;
+            scale = loss_scale(top);
+            ref = to;
         }
     };
     auto see = [&](float v) {
         sum += v;
-        if (v != -INFINITY) s += exp_fast(m == -INFINITY ? v : v - m);  // (NaN and +inf end here and stay in the sum)
+        s += exp2_fast(fmaf(v, scale, -ref));   // (0 for -inf; NaN and +inf end here and stay in the sum)
     };
     for (int i = tid; i < head; i += kLossThreads) rise(widen(x[i])), see(widen(x[i]));
     for (int i = tid; i < body; i += kLossThreads) {
@@ -295,6 +313,7 @@ loss_stream_kernel(const LossArgs a, const T* logits, T* grad) {
         for (int j = 0; j < VEC; ++j) see(f[j]);
     }
     for (int i = rest + tid; i < a.vocab; i += kLossThreads) rise(widen(x[i])), see(widen(x[i]));
+    m = m == -INFINITY ? m : ref;
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
         const float m2 = __shfl_xor_sync(kFullMask, m, o), s2 = __shfl_xor_sync(kFullMask, s, o);
@@ -317,7 +336,7 @@ loss_stream_kernel(const LossArgs a, const T* logits, T* grad) {
         const float k = some ? r.w * fmaf(2.0f * a.z, r.lse, 1.0f) / r.s : 0.0f, off = r.w * a.smoothing / (float)a.vocab, hit = r.w * (1.0f - a.smoothing);
         auto of = [&](float v, int i) {
             if (!some) return 0.0f;
-            const float d = fmaf(k, exp_fast(v - r.m), -off);
+            const float d = fmaf(k, exp2_fast(fmaf(v, r.scale, -r.m)), -off);
             return i == (int)r.target ? d - hit : d;
         };
         for (int i = tid; i < head; i += kLossThreads) g[i] = narrow<T>(of(widen(x[i]), i));
