@@ -16,78 +16,130 @@
 namespace {
 
 struct NormShape {
-    int vec, nv, threads, rows_per_cta;
+    int vec, nv, threads, rows_per_cta, stages;
+    bool team;  // the kernels with whole rows per warp
+    unsigned grid;
+    size_t smem;
 };
 
-// A warp takes a row of up to 32 vectors; wider rows are spread over a CTA of at most 512 threads, with as few vectors per thread
-// as that allows.  (Single values: four per thread at least.  Forward, two vectors from five warps a row on: a row's sums cost every
-// warp the same, however many columns it has.)
-NormShape norm_shape(int cols, int vec, bool backward) {
-    NormShape s;
-    s.vec = vec;
-    const int vectors = (cols + vec - 1) / vec;
+constexpr long long kNormShared = 220 * 1024;
+
+// Pieces of 8 on 16-byte boundaries: a warp per row up to 8 pieces a lane, as many warps as it takes beyond; with no more rows than a
+// few per SM, as many threads as the row has pieces (up to 256).  A CTA per SM with as many rows as registers and a ring of two rows
+// each allow.  False where shared memory does not hold two rows of everything.
+bool norm_team_shape(NormShape* s, int cols, int bytes, int arrays, long long rows, int n_sms, bool backward) {
+    const int vectors = cols / 8;
+    int threads = (vectors + 32 * kTeamMaxPieces - 1) / (32 * kTeamMaxPieces) * 32;
+    if (rows <= 4ll * n_sms) threads = std::min(256, std::max(threads, (vectors + 31) / 32 * 32));
+    int nv = (vectors + threads - 1) / threads;
+    if (nv == 7 || (threads > 32 && nv > 4)) nv = 8;
+    if (threads > 32 && nv == 3) nv = 4;
+    const long long table = 2ll * 2 * nv * threads * 16, one = (long long)arrays * nv * threads * 8 * bytes;
+    if (threads > norm_team_threads(nv, backward) || table + 2 * one > kNormShared) return false;
+    long long r = threads > 32 ? 1 : norm_team_threads(nv, backward) / 32;
+    r = std::min(r, (kNormShared - table) / (2 * one));
+    r = std::max(1ll, std::min(r, (rows + n_sms - 1) / n_sms));
+    // of the counts near the largest one, that whose last round of rows is fullest
+    long long best = r;
+    const auto filled = [&](long long k) { return (double)rows / (double)((rows + n_sms * k - 1) / (n_sms * k) * n_sms * k); };
+    for (long long k = r; k >= 1 && 3 * k >= 2 * r; --k)
+        if (filled(k) > filled(best) + 0.02) best = k;
+    r = best;
+    s->team = true;
+    s->vec = 8;
+    s->nv = nv;
+    s->threads = threads;
+    s->rows_per_cta = (int)r;
+    // one row per CTA (wide rows, few rows): as many CTAs per SM as threads and shared memory allow
+    const long long ctas = r > 1 ? 1 : std::max(1ll, std::min((long long)norm_team_threads(nv, backward) / threads, kNormShared / (table + 2 * one + 2048)));
+    s->stages = (int)std::max(2ll, std::min(4ll, (kNormShared / ctas - table) / (r * one)));
+    s->grid = (unsigned)std::min((rows + r - 1) / r, (long long)n_sms * ctas);
+    s->smem = (size_t)(table + r * s->stages * one);
+    if (backward) s->smem = std::max(s->smem, (size_t)(table + r * 2 * cols * 4));
+    return true;
+}
+
+// Other rows: a warp takes a row of up to 32 vectors; wider rows are spread over a CTA of at most 512 threads, with as few vectors per
+// thread as that allows.  (Single values: four per thread at least.)
+NormShape norm_shape(int cols, int vec, int bytes, int arrays, long long rows, int n_sms, bool backward) {
+    NormShape s = {};
+    if (vec == 8 && norm_team_shape(&s, cols, bytes, arrays, rows, n_sms, backward)) return s;
+    s.vec = vec == 8 ? 16 / bytes : vec;
+    const int vectors = (cols + s.vec - 1) / s.vec;
     const int need = (vectors + kNormMaxThreads - 1) / kNormMaxThreads;
-    if (vec >= 4) s.nv = need <= 1 && (backward || vectors <= 128) ? 1 : need <= 2 ? 2 : need <= 4 ? 4 : 8;
-    else if (vec == 2) s.nv = need <= 4 ? 4 : 16;
+    if (s.vec >= 4) s.nv = 32 / s.vec;  // (wide rows only)
+    else if (s.vec == 2) s.nv = need <= 4 ? 4 : 16;
     else s.nv = need <= 4 ? 4 : need <= 8 ? 8 : 32;
     s.threads = ((vectors + s.nv - 1) / s.nv + 31) / 32 * 32;
     s.rows_per_cta = s.threads == 32 ? kNormWarpRows : 1;
+    // CTAs per SM: the registers of a thread decide (the kernels' launch bounds hold them to this)
+    const int threads = s.threads * s.rows_per_cta;
+    const long long ctas = std::max(1, std::min(32, 65536 / norm_regs(s.nv * s.vec, backward) / threads));
+    s.grid = (unsigned)std::min((rows + s.rows_per_cta - 1) / s.rows_per_cta, n_sms * ctas);
+    // rows in a CTA's ring: up to four, as many as the SM's shared memory holds for its CTAs, two at least (one being used, one on its
+    // way), but no more than a CTA has rows
+    const bool few = s.nv * s.vec <= (backward ? 8 : 16);
+    const long long one = (long long)threads * s.nv * s.vec * bytes * arrays, per = (long long)std::max(1u, s.grid) * s.rows_per_cta;
+    s.stages = (int)std::max(2ll, std::min(std::min(4ll, kNormShared / ctas / one), (rows + per - 1) / per + 1));
+    s.smem = few ? (size_t)(one * s.stages) : 0;
+    if (backward && s.rows_per_cta > 1) s.smem = std::max(s.smem, sizeof(float) * 2 * (size_t)cols);
     return s;
 }
 
-// CTAs per SM: the registers of a thread decide (the kernels' launch bounds hold them to this)
-int norm_ctas(const NormShape& s, bool backward) {
-    return std::max(1, std::min(32, 65536 / norm_regs(s.nv * s.vec, backward) / (s.threads * s.rows_per_cta)));
-}
-unsigned norm_grid(const NormShape& s, long long rows, int n_sms, bool backward) {
-    const long long want = (rows + s.rows_per_cta - 1) / s.rows_per_cta;
-    return (unsigned)std::min(want, (long long)n_sms * norm_ctas(s, backward));
-}
-// Rows in a CTA's ring: up to four, as many as the SM's shared memory holds for its CTAs, two at least (one being used, one on its
-// way), but no more than a CTA has rows.
-int norm_stages(const NormShape& s, int arrays, int bytes, long long rows, unsigned grid, bool backward) {
-    const long long one = (long long)s.threads * s.rows_per_cta * s.nv * s.vec * bytes * arrays;
-    const long long fit = 220ll * 1024 / norm_ctas(s, backward) / one;
-    const long long has = (rows + (long long)grid * s.rows_per_cta - 1) / ((long long)grid * s.rows_per_cta) + 1;
-    return (int)std::max(2ll, std::min(std::min(4ll, fit), has));
-}
-
-template <class T, class W, int VEC, int NV, bool FULL>
-sl_status launch_norm_gate(const NormArgs& given, const NormShape& s, unsigned grid, bool backward, cudaStream_t st) {
-    NormArgs a = given;
-    const int arrays = (backward ? 4 : 2) + (FULL ? 1 : 0), threads = s.threads * s.rows_per_cta;
-    a.stages = norm_stages(s, arrays, (int)sizeof(T), a.rows, grid, backward);
-    const bool few = backward ? kNormFewBackward<VEC, NV> : kNormFew<VEC, NV>;
-    size_t smem = few ? (size_t)threads * NV * VEC * sizeof(T) * arrays * a.stages : 0;
-    if (backward && s.rows_per_cta > 1) smem = std::max(smem, sizeof(float) * 2 * (size_t)a.cols);
-    auto kern = backward ? norm_backward_kernel<T, W, VEC, NV, FULL> : norm_forward_kernel<T, W, VEC, NV, FULL>;
-    if (smem > 47 * 1024) SL_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024));  // (1 KB stays for the sums)
-    kern<<<grid, dim3((unsigned)s.threads, (unsigned)s.rows_per_cta), smem, st>>>(a);
+template <class K>
+sl_status launch_norm_kernel(K kern, const NormArgs& a, const NormShape& s, cudaStream_t st) {
+    if (s.smem > 47 * 1024) SL_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024));  // (1 KB stays for the sums)
+    kern<<<s.grid, dim3((unsigned)s.threads, (unsigned)s.rows_per_cta), s.smem, st>>>(a);
     SL_CUDA(cudaGetLastError());
     return SL_OK;
 }
 
+template <class T, class W, int NV, bool WARP>
+sl_status launch_norm_team(const NormArgs& a, const NormShape& s, bool backward, cudaStream_t st) {
+    const bool full = a.gate_kind == SL_GATE_FULL;
+    if (backward) return full ? launch_norm_kernel(norm_backward_team_kernel<T, W, NV, true, WARP>, a, s, st) : launch_norm_kernel(norm_backward_team_kernel<T, W, NV, false, WARP>, a, s, st);
+    return full ? launch_norm_kernel(norm_forward_team_kernel<T, W, NV, true, WARP>, a, s, st) : launch_norm_kernel(norm_forward_team_kernel<T, W, NV, false, WARP>, a, s, st);
+}
+
 template <class T, class W, int VEC, int NV>
-sl_status launch_norm(const NormArgs& a, const NormShape& s, unsigned grid, bool backward, cudaStream_t st) {
-    return a.gate_kind == SL_GATE_FULL ? launch_norm_gate<T, W, VEC, NV, true>(a, s, grid, backward, st) : launch_norm_gate<T, W, VEC, NV, false>(a, s, grid, backward, st);
+sl_status launch_norm(const NormArgs& a, const NormShape& s, bool backward, cudaStream_t st) {
+    const bool full = a.gate_kind == SL_GATE_FULL;
+    if (backward) return full ? launch_norm_kernel(norm_backward_kernel<T, W, VEC, NV, true>, a, s, st) : launch_norm_kernel(norm_backward_kernel<T, W, VEC, NV, false>, a, s, st);
+    return full ? launch_norm_kernel(norm_forward_kernel<T, W, VEC, NV, true>, a, s, st) : launch_norm_kernel(norm_forward_kernel<T, W, VEC, NV, false>, a, s, st);
 }
 
 template <class T, class W>
-sl_status launch_norm_shape(const NormArgs& a, const NormShape& s, unsigned grid, bool backward, cudaStream_t st) {
-    constexpr int V = 16 / (int)sizeof(T);
-    if (s.vec == 1) return s.nv == 4 ? launch_norm<T, W, 1, 4>(a, s, grid, backward, st) : s.nv == 8 ? launch_norm<T, W, 1, 8>(a, s, grid, backward, st)
-                                                                                                     : launch_norm<T, W, 1, 32>(a, s, grid, backward, st);
-    if (s.vec == 2) return s.nv == 4 ? launch_norm<T, W, 2, 4>(a, s, grid, backward, st) : launch_norm<T, W, 2, 16>(a, s, grid, backward, st);
-    if (s.nv == 1) return launch_norm<T, W, V, 1>(a, s, grid, backward, st);
-    if (s.nv == 2) return launch_norm<T, W, V, 2>(a, s, grid, backward, st);
-    if (s.nv == 4) return launch_norm<T, W, V, 4>(a, s, grid, backward, st);
-    return launch_norm<T, W, V, 32 / V>(a, s, grid, backward, st);
+sl_status launch_norm_shape(const NormArgs& given, const NormShape& s, bool backward, cudaStream_t st) {
+    NormArgs a = given;
+    a.stages = s.stages;
+    if (s.team && s.threads == 32) {
+        switch (s.nv) {
+            case 1: return launch_norm_team<T, W, 1, true>(a, s, backward, st);
+            case 2: return launch_norm_team<T, W, 2, true>(a, s, backward, st);
+            case 3: return launch_norm_team<T, W, 3, true>(a, s, backward, st);
+            case 4: return launch_norm_team<T, W, 4, true>(a, s, backward, st);
+            case 5: return launch_norm_team<T, W, 5, true>(a, s, backward, st);
+            case 6: return launch_norm_team<T, W, 6, true>(a, s, backward, st);
+            default: return launch_norm_team<T, W, 8, true>(a, s, backward, st);
+        }
+    }
+    if (s.team) {
+        switch (s.nv) {
+            case 1: return launch_norm_team<T, W, 1, false>(a, s, backward, st);
+            case 2: return launch_norm_team<T, W, 2, false>(a, s, backward, st);
+            case 4: return launch_norm_team<T, W, 4, false>(a, s, backward, st);
+            default: return launch_norm_team<T, W, 8, false>(a, s, backward, st);
+        }
+    }
+    if (s.vec == 1) return s.nv == 4 ? launch_norm<T, W, 1, 4>(a, s, backward, st) : s.nv == 8 ? launch_norm<T, W, 1, 8>(a, s, backward, st) : launch_norm<T, W, 1, 32>(a, s, backward, st);
+    if (s.vec == 2) return s.nv == 4 ? launch_norm<T, W, 2, 4>(a, s, backward, st) : launch_norm<T, W, 2, 16>(a, s, backward, st);
+    return launch_norm<T, W, 16 / (int)sizeof(T), 2 * (int)sizeof(T)>(a, s, backward, st);
 }
 
-sl_status launch_norm_types(const sl_norm_desc* d, const NormArgs& a, const NormShape& s, unsigned grid, bool backward, cudaStream_t st) {
-    if (d->dtype == SL_F32) return launch_norm_shape<float, float>(a, s, grid, backward, st);
-    if (d->weight_dtype == SL_F32) return launch_norm_shape<bf16, float>(a, s, grid, backward, st);
-    return launch_norm_shape<bf16, bf16>(a, s, grid, backward, st);
+sl_status launch_norm_types(const sl_norm_desc* d, const NormArgs& a, const NormShape& s, bool backward, cudaStream_t st) {
+    if (d->dtype == SL_F32) return launch_norm_shape<float, float>(a, s, backward, st);
+    if (d->weight_dtype == SL_F32) return launch_norm_shape<bf16, float>(a, s, backward, st);
+    return launch_norm_shape<bf16, bf16>(a, s, backward, st);
 }
 
 template <class W>
@@ -137,17 +189,17 @@ void norm_strides(const sl_norm_desc* d, NormArgs* a) {
     a->ld_gate = d->ld_gate ? d->ld_gate : (d->gate_kind == SL_GATE_FULL ? d->cols : 1);
 }
 
-// The values per access that columns, row strides and pointers of everything allow: 16 bytes, or two values, or one.
+// The values per piece that columns, row strides and pointers of everything allow: 8 (on 16-byte boundaries), or two, or one.
 struct NormAlign {
     int bytes, vec;
     bool element;
-    explicit NormAlign(const sl_norm_desc* d) : bytes(dtype_bytes(d->dtype)), vec(16 / dtype_bytes(d->dtype)), element(true) { all(d->cols); }
-    void all(long long n) { vec = n % vec == 0 ? vec : n % 2 == 0 ? std::min(vec, 2) : 1; }
+    explicit NormAlign(const sl_norm_desc* d) : bytes(dtype_bytes(d->dtype)), vec(8), element(true) { all(d->cols, 8); }
+    void all(long long n, int whole) { vec = n % whole == 0 ? vec : n % 2 == 0 ? std::min(vec, 2) : 1; }
     void matrix(const void* p, long long ld) {
         if (!p) return;
         element = element && fits(p, bytes);
-        all(ld);
-        all((long long)(reinterpret_cast<uintptr_t>(p) / (unsigned)bytes));
+        all(ld, 16 / bytes);
+        all((long long)(reinterpret_cast<uintptr_t>(p) / (unsigned)bytes), 16 / bytes);
     }
     void vector(const void* p, int b) {  // weights: 16 bytes at a time, or as many values
         if (!p) return;
@@ -190,12 +242,11 @@ sl_status sl_norm_forward(const sl_norm_desc* d, const void* x, const void* bran
     else if (d->gate_kind == SL_GATE_FULL) al.matrix(gate, a.ld_gate);
     else if (!fits(gate, al.bytes)) return SL_ERR_ALIGNMENT;
     if (!al.element || !fits(branch_rstd, 4) || !fits(rstd, 4)) return SL_ERR_ALIGNMENT;
-    const NormShape sh = norm_shape(a.cols, al.vec, false);
     int n_sms = 0;
     s = sm_count(&n_sms);
     if (s != SL_OK) return s;
-    const unsigned grid = norm_grid(sh, d->rows, n_sms, false);
-    return launch_norm_types(d, a, sh, grid, false, static_cast<cudaStream_t>(stream));
+    const NormShape sh = norm_shape(a.cols, al.vec, al.bytes, d->gate_kind == SL_GATE_FULL ? 3 : 2, d->rows, n_sms, false);
+    return launch_norm_types(d, a, sh, false, static_cast<cudaStream_t>(stream));
 }
 
 sl_status sl_norm_workspace_bytes(const sl_norm_desc* d, size_t* bytes) {
@@ -205,11 +256,14 @@ sl_status sl_norm_workspace_bytes(const sl_norm_desc* d, size_t* bytes) {
     int n_sms = 0;
     s = sm_count(&n_sms);
     if (s != SL_OK) return s;
-    // the largest of the launch shapes that alignment decides between
+    // the largest of the launch shapes that alignment and the gate decide between
     size_t most = 0;
-    for (int vec : {1, 2, 16 / dtype_bytes(d->dtype)}) {
-        const NormShape sh = norm_shape((int)d->cols, vec, true);
-        most = std::max(most, sizeof(float) * 2 * (size_t)d->cols * norm_grid(sh, d->rows, n_sms, true));
+    for (int vec : {1, 2, 8}) {
+        if (vec == 8 && d->cols % 8) continue;
+        for (int arrays : {4, 5}) {
+            const NormShape sh = norm_shape((int)d->cols, vec, dtype_bytes(d->dtype), arrays, d->rows, n_sms, true);
+            most = std::max(most, sizeof(float) * 2 * (size_t)d->cols * sh.grid);
+        }
     }
     *bytes = up256(most);
     return SL_OK;
@@ -260,14 +314,14 @@ sl_status sl_norm_backward(const sl_norm_desc* d, const void* dy, const void* dh
     s = sm_count(&n_sms);
     if (s != SL_OK) return s;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const NormShape sh = norm_shape(a.cols, al.vec, true);
-    const unsigned grid = norm_grid(sh, d->rows, n_sms, true);
+    const NormShape sh = norm_shape(a.cols, al.vec, al.bytes, d->gate_kind == SL_GATE_FULL ? 5 : 4, d->rows, n_sms, true);
+    const unsigned grid = d->rows ? sh.grid : 0;
     if (columns) {
         if (grid && (!workspace || workspace_bytes < sizeof(float) * 2 * (size_t)a.cols * grid)) return SL_ERR_NOMEM;
         a.part = static_cast<float*>(workspace);
     }
     if (grid) {
-        s = launch_norm_types(d, a, sh, grid, true, st);
+        s = launch_norm_types(d, a, sh, true, st);
         if (s != SL_OK) return s;
     }
     if (columns) {

@@ -457,6 +457,362 @@ norm_backward_kernel(const NormArgs a) {
     }
 }
 
+// ------------------------------------------------------------------------------------------------------------------------------
+// Rows that divide into pieces of 8 values on 16-byte boundaries (what models have): a warp takes a whole row of up to 2048 columns,
+// up to 8 pieces per lane, wider rows a few warps.  What a row costs besides its values (its sums' exchange, addresses, loop) is paid
+// once per warp, so few warps per row it is; weights sit in shared memory as fp32, column sums in registers, rows come through a ring
+// that every lane fills for itself.  (With 8 columns per thread and 5 to 8 warps a row, the kernels above were bound by issue: 3300 and 1600
+// instructions a row at 1280 and 2048 columns, about 950 and 650 here.)
+// ------------------------------------------------------------------------------------------------------------------------------
+constexpr int kTeamMaxPieces = 8;
+__host__ __device__ constexpr int norm_team_threads(int nv, bool backward) {  // of a CTA: what its registers allow
+    return backward ? (nv <= 1 ? 640 : nv <= 2 ? 512 : nv <= 5 ? 384 : 256) : (nv <= 2 ? 1024 : nv <= 4 ? 512 : 384);
+}
+
+// Threads of a row: a warp, known when compiling (offsets become immediate), or as many as the launch says.
+template <bool WARP>
+__device__ __forceinline__ int team_width() { return WARP ? 32 : (int)blockDim.x; }
+
+// 8 values of T as 16-byte chunks, chunk h of all threads together (no bank conflicts)
+template <class T>
+struct Chunks {
+    static constexpr int kNum = 8 * (int)sizeof(T) / 16;
+};
+
+// `first`: shared address of the chunk 0 of piece 0 of this thread; `plane`: bytes from chunk to chunk.
+template <class T>
+__device__ __forceinline__ void team_get(unsigned at, unsigned plane, float2 (&f)[4]) {
+    unsigned w[4 * Chunks<T>::kNum];
+#pragma unroll
+    for (int h = 0; h < Chunks<T>::kNum; ++h) shared_load<16>(at + h * plane, w + 4 * h);
+    if (sizeof(T) == 2) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f[j] = widen2(w[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f[j] = make_float2(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + (sizeof(T) == 4 ? 1 : 0)]));
+    }
+}
+template <class T>
+__device__ __forceinline__ void team_put(T* p, const float2 (&f)[4]) {
+    if (sizeof(T) == 2) {
+        *reinterpret_cast<uint4*>(p) = make_uint4(narrow2(f[0]), narrow2(f[1]), narrow2(f[2]), narrow2(f[3]));
+    } else {
+        reinterpret_cast<float4*>(p)[0] = make_float4(f[0].x, f[0].y, f[1].x, f[1].y);
+        reinterpret_cast<float4*>(p)[1] = make_float4(f[2].x, f[2].y, f[3].x, f[3].y);
+    }
+}
+
+// The thread's pieces of a matrix, row by row.
+template <class T, int NV, bool WARP>
+struct TeamMatrix {
+    const T* row;    // null: absent
+    long long step;
+    unsigned place;  // in the ring's first row
+    __device__ __forceinline__ TeamMatrix(const void* base, long long ld, long long first, long long stride, unsigned ring, int array) {
+        row = base ? static_cast<const T*>(base) + first * ld + threadIdx.x * 8 : nullptr;
+        step = base ? stride * ld : 0;
+        place = ring + (unsigned)(array * NV * Chunks<T>::kNum * team_width<WARP>() + (int)threadIdx.x) * 16u;
+    }
+    __device__ __forceinline__ unsigned at(int i) const { return place + (unsigned)(i * Chunks<T>::kNum * team_width<WARP>()) * 16u; }
+    __device__ __forceinline__ void clear(int stages, unsigned stage_bytes, int pieces) const {
+        for (int s = 0; s < stages; ++s)
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (!row || i >= pieces)
+#pragma unroll
+                    for (int h = 0; h < Chunks<T>::kNum; ++h)
+                        asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at(i) + (unsigned)s * stage_bytes + (unsigned)(h * team_width<WARP>()) * 16u), "r"(0u) : "memory");
+    }
+    __device__ __forceinline__ void fetch(unsigned stage_at, int pieces) {
+        if (!row) return;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (i < pieces)
+#pragma unroll
+                for (int h = 0; h < Chunks<T>::kNum; ++h)
+                    copy_async<16>(at(i) + stage_at + (unsigned)(h * team_width<WARP>()) * 16u, row + i * team_width<WARP>() * 8 + h * (16 / (int)sizeof(T)));
+        row += step;
+    }
+    __device__ __forceinline__ void get(unsigned stage_at, int i, float2 (&f)[4]) const { team_get<T>(at(i) + stage_at, (unsigned)team_width<WARP>() * 16u, f); }
+};
+
+// fp32 weights (times those of `times`) of all columns into shared memory at `to`, by the CTA: chunk 0 of every piece, then chunk 1.
+template <class W, int NV, bool WARP>
+__device__ __forceinline__ void team_weights(unsigned to, const void* w, const void* times, int cols) {
+    for (int v = threadIdx.y * blockDim.x + threadIdx.x; v < NV * team_width<WARP>(); v += blockDim.x * blockDim.y) {
+        float f[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = 1.0f;
+        if (v * 8 < cols) {
+            Pack<W, 8> t;
+            if (w) {
+                t.load(static_cast<const W*>(w) + v * 8);
+                t.get(f);
+            }
+            if (times) {
+                float g[8];
+                t.load(static_cast<const W*>(times) + v * 8);
+                t.get(g);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[j] *= g[j];
+            }
+        }
+        // piece i, thread x: v = i * blockDim.x + x
+        const unsigned i = (unsigned)v / (unsigned)team_width<WARP>(), x = (unsigned)v - i * (unsigned)team_width<WARP>();
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to + ((2u * i + h) * (unsigned)team_width<WARP>() + x) * 16u), "f"(f[4 * h]), "f"(f[4 * h + 1]), "f"(f[4 * h + 2]), "f"(f[4 * h + 3]) : "memory");
+    }
+}
+
+// blockDim = (threads of a row, rows of the CTA); shared memory: weights [2][NV][2][blockDim.x] chunks, then every row's ring.
+template <class T, class W, int NV, bool FULL, bool WARP>
+__global__ void __launch_bounds__(norm_team_threads(NV, false), 1)
+norm_forward_team_kernel(const NormArgs a) {
+    extern __shared__ __align__(16) char shared[];
+    __shared__ float sums[2][16];
+    clear_sums(sums[0], 32);
+    const unsigned weights = (unsigned)__cvta_generic_to_shared(shared), table = 2u * NV * (unsigned)team_width<WARP>() * 16u;
+    const unsigned stage_bytes = (FULL ? 3u : 2u) * NV * Chunks<T>::kNum * (unsigned)team_width<WARP>() * 16u, ring_bytes = (unsigned)a.stages * stage_bytes;
+    const unsigned ring = weights + 2u * table + threadIdx.y * ring_bytes;
+    const long long stride = (long long)gridDim.x * blockDim.y;
+    long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y;
+    const bool normed = a.branch_weight != nullptr, has_branch = a.branch != nullptr;
+    const int vectors = a.cols / 8, pieces = vectors > (int)threadIdx.x ? min(NV, (vectors - (int)threadIdx.x - 1) / team_width<WARP>() + 1) : 0;
+    TeamMatrix<T, NV, WARP> mx(a.x, a.ld_x, row, stride, ring, 0), mb(a.branch, a.ld_branch, row, stride, ring, 1), mg(FULL ? a.gate : nullptr, a.ld_gate, row, stride, ring, 2);
+    mx.clear(a.stages, stage_bytes, pieces);
+    mb.clear(a.stages, stage_bytes, pieces);
+    if (FULL) mg.clear(a.stages, stage_bytes, pieces);
+    long long coming = row;
+    auto fetch = [&](unsigned stage_at) {
+        if (coming < a.rows) {
+            mx.fetch(stage_at, pieces);
+            mb.fetch(stage_at, pieces);
+            if (FULL) mg.fetch(stage_at, pieces);
+        }
+        coming += stride;
+        copy_commit();
+    };
+    for (int k = 0; k < a.stages - 1; ++k) fetch((unsigned)k * stage_bytes);
+    team_weights<W, NV, WARP>(weights, a.weight, nullptr, a.cols);
+    team_weights<W, NV, WARP>(weights + table, a.branch_weight, a.gate_kind == SL_GATE_COLUMN ? a.gate : nullptr, a.cols);
+    __syncthreads();
+    const unsigned mine = weights + threadIdx.x * 16u, plane = (unsigned)team_width<WARP>() * 16u;  // this thread's weights: piece i at mine + 2 i plane
+    T* y = static_cast<T*>(a.y) + (a.y ? row * a.ld_y + threadIdx.x * 8 : 0);
+    T* h = static_cast<T*>(a.h) + (a.h ? row * a.ld_h + threadIdx.x * 8 : 0);
+    for (unsigned at = 0; row < a.rows; row += stride) {
+        fetch(at ? at - stage_bytes : ring_bytes - stage_bytes);
+        copy_wait(a.stages - 1);
+        float2 v[NV][4], q = both(0.0f);
+        if (has_branch) {
+            float rb = 1.0f;
+            if (normed) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    float2 z[4];
+                    mb.get(at, i, z);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) q = fma2(z[j], z[j], q);
+                }
+                float s[1] = {q.x + q.y};
+                row_sums<1>(s, sums[0]);
+                rb = reciprocal_root(fmaf(s[0], a.inv_cols, a.eps));
+                if (a.branch_rstd && threadIdx.x == 0) a.branch_rstd[row] = rb;
+                q = both(0.0f);
+            }
+            float scale = a.alpha * rb;
+            if (a.gate_kind == SL_GATE_ROW) scale *= widen(static_cast<const T*>(a.gate)[row * a.ld_gate]);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                float2 z[4], c[4], g[4];
+                mx.get(at, i, v[i]);
+                mb.get(at, i, z);
+                if (FULL) mg.get(at, i, g);
+                team_get<float>(mine + table + 2u * i * plane, plane, c);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    v[i][j] = fma2(mul2(z[j], both(scale)), FULL ? mul2(c[j], g[j]) : c[j], v[i][j]);
+                    q = fma2(v[i][j], v[i][j], q);
+                }
+                if (i < pieces) team_put(y + i * team_width<WARP>() * 8, v[i]);
+            }
+            y += stride * a.ld_y;
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                mx.get(at, i, v[i]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) q = fma2(v[i][j], v[i][j], q);
+            }
+        }
+        at = at + stage_bytes == ring_bytes ? 0u : at + stage_bytes;
+        if (!a.h) continue;
+        float s[1] = {q.x + q.y};
+        row_sums<1>(s, sums[1]);
+        const float r = reciprocal_root(fmaf(s[0], a.inv_cols, a.eps));
+        if (a.rstd && threadIdx.x == 0) a.rstd[row] = r;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float2 w[4];
+            team_get<float>(mine + 2u * i * plane, plane, w);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = mul2(mul2(v[i][j], both(r)), w[j]);
+            if (i < pieces) team_put(h + i * team_width<WARP>() * 8, w);
+        }
+        h += stride * a.ld_h;
+    }
+}
+
+// The formulas are norm_backward_kernel's; a row's pieces and weights are read again for the second half.
+template <class T, class W, int NV, bool FULL, bool WARP>
+__global__ void __launch_bounds__(norm_team_threads(NV, true), 1)
+norm_backward_team_kernel(const NormArgs a) {
+    extern __shared__ __align__(16) char shared[];  // the rings become [rows of the CTA][2][cols] column sums at the end
+    __shared__ float sums[2][3 * 16];
+    clear_sums(sums[0], 2 * 3 * 16);
+    const unsigned weights = (unsigned)__cvta_generic_to_shared(shared), table = 2u * NV * (unsigned)team_width<WARP>() * 16u;
+    const unsigned stage_bytes = (FULL ? 5u : 4u) * NV * Chunks<T>::kNum * (unsigned)team_width<WARP>() * 16u, ring_bytes = (unsigned)a.stages * stage_bytes;
+    const unsigned ring = weights + 2u * table + threadIdx.y * ring_bytes;
+    const long long stride = (long long)gridDim.x * blockDim.y;
+    long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y;
+    const bool normed = a.branch_weight != nullptr, row_gate = a.gate_kind == SL_GATE_ROW;
+    const int vectors = a.cols / 8, pieces = vectors > (int)threadIdx.x ? min(NV, (vectors - (int)threadIdx.x - 1) / team_width<WARP>() + 1) : 0;
+    TeamMatrix<T, NV, WARP> mdy(a.dy, a.ld_dy, row, stride, ring, 0), mdh(a.dh, a.ld_dh, row, stride, ring, 1), my(a.dh ? a.x : nullptr, a.ld_y, row, stride, ring, 2),
+        mb(a.branch, a.ld_branch, row, stride, ring, 3), mg(FULL ? a.gate : nullptr, a.ld_gate, row, stride, ring, 4);
+    mdy.clear(a.stages, stage_bytes, pieces);
+    mdh.clear(a.stages, stage_bytes, pieces);
+    my.clear(a.stages, stage_bytes, pieces);
+    mb.clear(a.stages, stage_bytes, pieces);
+    if (FULL) mg.clear(a.stages, stage_bytes, pieces);
+    long long coming = row;
+    auto fetch = [&](unsigned stage_at) {
+        if (coming < a.rows) {
+            mdy.fetch(stage_at, pieces);
+            mdh.fetch(stage_at, pieces);
+            my.fetch(stage_at, pieces);
+            mb.fetch(stage_at, pieces);
+            if (FULL) mg.fetch(stage_at, pieces);
+        }
+        coming += stride;
+        copy_commit();
+    };
+    float r_next = 0.0f, rb_next = 1.0f, rg_next = 1.0f;
+    auto scalars = [&](long long at) {
+        if (a.dh) r_next = a.rstd[at];
+        if (normed) rb_next = a.branch_rstd[at];
+        if (row_gate) rg_next = widen(static_cast<const T*>(a.gate)[at * a.ld_gate]);
+    };
+    for (int k = 0; k < a.stages - 1; ++k) fetch((unsigned)k * stage_bytes);
+    if (row < a.rows) scalars(row);
+    team_weights<W, NV, WARP>(weights, a.weight, nullptr, a.cols);
+    team_weights<W, NV, WARP>(weights + table, a.branch_weight, a.gate_kind == SL_GATE_COLUMN ? a.gate : nullptr, a.cols);
+    __syncthreads();
+    const unsigned mine = weights + threadIdx.x * 16u, plane = (unsigned)team_width<WARP>() * 16u;
+    float2 acc[2][NV][4];
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[0][i][j] = acc[1][i][j] = both(0.0f);
+    T* dx = static_cast<T*>(a.dx) + (a.dx ? row * a.ld_x + threadIdx.x * 8 : 0);
+    T* dbranch = static_cast<T*>(a.dbranch) + (a.dbranch ? row * a.ld_branch + threadIdx.x * 8 : 0);
+    T* dgate = static_cast<T*>(a.dgate) + (FULL && a.dgate ? row * a.ld_gate + threadIdx.x * 8 : 0);
+    int turn = 0;
+    for (unsigned at = 0; row < a.rows; row += stride, turn ^= 1) {
+        fetch(at ? at - stage_bytes : ring_bytes - stage_bytes);
+        copy_wait(a.stages - 1);
+        const float r = r_next, rb = rb_next, rg = rg_next;
+        if (row + stride < a.rows) scalars(row + stride);
+        float2 t0 = both(0.0f), t1 = t0, t2 = t0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float2 dy[4], dh[4], yh[4], bh[4], g[4], w[4], c[4];
+            mdy.get(at, i, dy);
+            mdh.get(at, i, dh);
+            my.get(at, i, yh);
+            mb.get(at, i, bh);
+            if (FULL) mg.get(at, i, g);
+            team_get<float>(mine + 2u * i * plane, plane, w);
+            team_get<float>(mine + table + 2u * i * plane, plane, c);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {  // (r and rb come in after the sums)
+                const float2 u = mul2(dh[j], w[j]), q = FULL ? mul2(mul2(bh[j], c[j]), g[j]) : mul2(bh[j], c[j]);
+                t0 = fma2(u, yh[j], t0);
+                t1 = fma2(q, fma2(both(r), u, dy[j]), t1);
+                t2 = fma2(q, yh[j], t2);
+            }
+        }
+        float s[3] = {t0.x + t0.y, t1.x + t1.y, t2.x + t2.y};
+        row_sums<3>(s, sums[turn]);
+        const float mean = s[0] * r * a.inv_cols;
+        const float qdx = rb * fmaf(-r * mean, s[2] * r, s[1]);  // sum q dx
+        const float bmean = a.alpha * rg * qdx * a.inv_cols;      // mean(dz branch_weight bhat)
+        if (row_gate && a.dgate && threadIdx.x == 0) static_cast<T*>(a.dgate)[row * a.ld_gate] = narrow<T>(a.alpha * qdx);
+        const float scale = a.alpha * rg, rbm = normed ? rb * rb * bmean : 0.0f;
+        const float2 r2 = both(r), ry = both(-r * mean), rs = both(rb), sc = both(scale), nb = both(-rbm);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float2 dy[4], dh[4], yh[4], bh[4], g[4], w[4], c[4];
+            mdy.get(at, i, dy);
+            mdh.get(at, i, dh);
+            my.get(at, i, yh);
+            mb.get(at, i, bh);
+            if (FULL) mg.get(at, i, g);
+            team_get<float>(mine + 2u * i * plane, plane, w);
+            team_get<float>(mine + table + 2u * i * plane, plane, c);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                acc[0][i][j] = fma2(mul2(dh[j], r2), yh[j], acc[0][i][j]);
+                dy[j] = fma2(r2, fma2(yh[j], ry, mul2(dh[j], w[j])), dy[j]);  // dx
+                float2 e = mul2(dy[j], sc);
+                if (FULL) {
+                    const float2 up = e;
+                    e = mul2(e, g[j]);
+                    g[j] = mul2(mul2(up, rs), mul2(bh[j], c[j]));               // the element gate's (c is branch_weight then)
+                }
+                e = mul2(e, rs);
+                acc[1][i][j] = fma2(e, bh[j], acc[1][i][j]);
+                dh[j] = fma2(e, c[j], mul2(bh[j], nb));                          // dbranch (rb is 1 and rbm 0 without its norm)
+            }
+            if (i < pieces) {
+                if (a.dx) team_put(dx + i * team_width<WARP>() * 8, dy);
+                if (a.dbranch) team_put(dbranch + i * team_width<WARP>() * 8, dh);
+                if (FULL && a.dgate) team_put(dgate + i * team_width<WARP>() * 8, g);
+            }
+        }
+        dx += stride * a.ld_x;
+        dbranch += stride * a.ld_branch;
+        if (FULL) dgate += stride * a.ld_gate;
+        at = at + stage_bytes == ring_bytes ? 0u : at + stage_bytes;
+    }
+    cudaTriggerProgrammaticLaunchCompletion();
+    if (!a.part) return;
+    // every row of the CTA lays its sums down in shared memory; the columns are then added up row after row
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncthreads();
+    const unsigned down = weights + 2u * table;
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (i < pieces) {
+                const unsigned to = down + ((threadIdx.y * 2u + k) * (unsigned)a.cols + (unsigned)(i * team_width<WARP>() + (int)threadIdx.x) * 8u) * 4u;
+                asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to), "f"(acc[k][i][0].x), "f"(acc[k][i][0].y), "f"(acc[k][i][1].x), "f"(acc[k][i][1].y) : "memory");
+                asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to + 16u), "f"(acc[k][i][2].x), "f"(acc[k][i][2].y), "f"(acc[k][i][3].x), "f"(acc[k][i][3].y) : "memory");
+            }
+    __syncthreads();
+    float* part = a.part + (long long)blockIdx.x * 2 * a.cols;
+    for (int col = threadIdx.y * blockDim.x + threadIdx.x; col < 2 * a.cols; col += blockDim.x * blockDim.y) {
+        float sum = 0.0f;
+        for (int t = 0; t < (int)blockDim.y; ++t) {
+            float x;
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(down + (unsigned)(t * 2 * a.cols + col) * 4u));
+            sum += x;
+        }
+        part[col] = sum;
+    }
+}
+
 // Column sums of the CTAs' parts in a fixed order: 32 columns per CTA, 32 strands of parts, then the strands in order.
 template <class W>
 __global__ void __launch_bounds__(1024)
