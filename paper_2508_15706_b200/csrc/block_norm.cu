@@ -24,19 +24,19 @@ struct NormShape {
 
 constexpr long long kNormShared = 220 * 1024;
 
-// Pieces of 8 on 16-byte boundaries: a warp per row up to 8 pieces a lane, as many warps as it takes beyond; with no more rows than a
-// few per SM, as many threads as the row has pieces (up to 256).  A CTA per SM with as many rows as registers and a ring of two rows
+// Pieces of 8 on 16-byte boundaries: a warp per row up to 512 columns, two up to 4096, as many as it takes beyond; with no more rows than
+// a few per SM, as many threads as the row has pieces (up to 256).  A CTA per SM with as many rows as registers and a ring of two rows
 // each allow.  False where shared memory does not hold two rows of everything.
 bool norm_team_shape(NormShape* s, int cols, int bytes, int arrays, long long rows, int n_sms, bool backward) {
     const int vectors = cols / 8;
-    int threads = (vectors + 32 * kTeamMaxPieces - 1) / (32 * kTeamMaxPieces) * 32;
+    int threads = vectors <= 64 ? 32 : vectors <= 64 * kTeamMaxPieces ? 64 : (vectors + 32 * kTeamMaxPieces - 1) / (32 * kTeamMaxPieces) * 32;
     if (rows <= 4ll * n_sms) threads = std::min(256, std::max(threads, (vectors + 31) / 32 * 32));
     int nv = (vectors + threads - 1) / threads;
-    if (nv == 7 || (threads > 32 && nv > 4)) nv = 8;
-    if (threads > 32 && nv == 3) nv = 4;
+    if (nv == 7 || (threads > 64 && nv > 4)) nv = 8;
+    if (threads > 64 && nv == 3) nv = 4;
     const long long table = 2ll * 2 * nv * threads * 16, one = (long long)arrays * nv * threads * 8 * bytes;
     if (threads > norm_team_threads(nv, backward) || table + 2 * one > kNormShared) return false;
-    long long r = threads > 32 ? 1 : norm_team_threads(nv, backward) / 32;
+    long long r = threads > 64 ? 1 : std::min(15, norm_team_threads(nv, backward) / threads);  // (15: a barrier for each)
     r = std::min(r, (kNormShared - table) / (2 * one));
     r = std::max(1ll, std::min(r, (rows + n_sms - 1) / n_sms));
     // of the counts near the largest one, that whose last round of rows is fullest
@@ -52,8 +52,9 @@ bool norm_team_shape(NormShape* s, int cols, int bytes, int arrays, long long ro
     s->rows_per_cta = (int)r;
     // one row per CTA (wide rows, few rows): as many CTAs per SM as threads and shared memory allow
     const long long ctas = r > 1 ? 1 : std::max(1ll, std::min((long long)norm_team_threads(nv, backward) / threads, kNormShared / (table + 2 * one + 2048)));
-    s->stages = (int)std::max(2ll, std::min(4ll, (kNormShared / ctas - table) / (r * one)));
     s->grid = (unsigned)std::min((rows + r - 1) / r, (long long)n_sms * ctas);
+    const long long per = (long long)std::max(1u, s->grid) * r;  // (no more stages than a CTA has rows, and one)
+    s->stages = (int)std::max(2ll, std::min(std::min(4ll, (rows + per - 1) / per + 1), (kNormShared / ctas - table) / (r * one)));
     s->smem = (size_t)(table + r * s->stages * one);
     if (backward) s->smem = std::max(s->smem, (size_t)(table + r * 2 * cols * 4));
     return true;
@@ -94,11 +95,11 @@ sl_status launch_norm_kernel(K kern, const NormArgs& a, const NormShape& s, cuda
     return SL_OK;
 }
 
-template <class T, class W, int NV, bool WARP>
+template <class T, class W, int NV, int TEAM>
 sl_status launch_norm_team(const NormArgs& a, const NormShape& s, bool backward, cudaStream_t st) {
     const bool full = a.gate_kind == SL_GATE_FULL;
-    if (backward) return full ? launch_norm_kernel(norm_backward_team_kernel<T, W, NV, true, WARP>, a, s, st) : launch_norm_kernel(norm_backward_team_kernel<T, W, NV, false, WARP>, a, s, st);
-    return full ? launch_norm_kernel(norm_forward_team_kernel<T, W, NV, true, WARP>, a, s, st) : launch_norm_kernel(norm_forward_team_kernel<T, W, NV, false, WARP>, a, s, st);
+    if (backward) return full ? launch_norm_kernel(norm_backward_team_kernel<T, W, NV, true, TEAM>, a, s, st) : launch_norm_kernel(norm_backward_team_kernel<T, W, NV, false, TEAM>, a, s, st);
+    return full ? launch_norm_kernel(norm_forward_team_kernel<T, W, NV, true, TEAM>, a, s, st) : launch_norm_kernel(norm_forward_team_kernel<T, W, NV, false, TEAM>, a, s, st);
 }
 
 template <class T, class W, int VEC, int NV>
@@ -112,23 +113,24 @@ template <class T, class W>
 sl_status launch_norm_shape(const NormArgs& given, const NormShape& s, bool backward, cudaStream_t st) {
     NormArgs a = given;
     a.stages = s.stages;
-    if (s.team && s.threads == 32) {
+    if (s.team && s.rows_per_cta == 1 && s.threads > 64) {
         switch (s.nv) {
-            case 1: return launch_norm_team<T, W, 1, true>(a, s, backward, st);
-            case 2: return launch_norm_team<T, W, 2, true>(a, s, backward, st);
-            case 3: return launch_norm_team<T, W, 3, true>(a, s, backward, st);
-            case 4: return launch_norm_team<T, W, 4, true>(a, s, backward, st);
-            case 5: return launch_norm_team<T, W, 5, true>(a, s, backward, st);
-            case 6: return launch_norm_team<T, W, 6, true>(a, s, backward, st);
-            default: return launch_norm_team<T, W, 8, true>(a, s, backward, st);
+            case 1: return launch_norm_team<T, W, 1, 0>(a, s, backward, st);
+            case 2: return launch_norm_team<T, W, 2, 0>(a, s, backward, st);
+            case 4: return launch_norm_team<T, W, 4, 0>(a, s, backward, st);
+            default: return launch_norm_team<T, W, 8, 0>(a, s, backward, st);
         }
     }
+    if (s.team && s.threads == 32) return s.nv == 1 ? launch_norm_team<T, W, 1, 32>(a, s, backward, st) : launch_norm_team<T, W, 2, 32>(a, s, backward, st);
     if (s.team) {
         switch (s.nv) {
-            case 1: return launch_norm_team<T, W, 1, false>(a, s, backward, st);
-            case 2: return launch_norm_team<T, W, 2, false>(a, s, backward, st);
-            case 4: return launch_norm_team<T, W, 4, false>(a, s, backward, st);
-            default: return launch_norm_team<T, W, 8, false>(a, s, backward, st);
+            case 1: return launch_norm_team<T, W, 1, 64>(a, s, backward, st);
+            case 2: return launch_norm_team<T, W, 2, 64>(a, s, backward, st);
+            case 3: return launch_norm_team<T, W, 3, 64>(a, s, backward, st);
+            case 4: return launch_norm_team<T, W, 4, 64>(a, s, backward, st);
+            case 5: return launch_norm_team<T, W, 5, 64>(a, s, backward, st);
+            case 6: return launch_norm_team<T, W, 6, 64>(a, s, backward, st);
+            default: return launch_norm_team<T, W, 8, 64>(a, s, backward, st);
         }
     }
     if (s.vec == 1) return s.nv == 4 ? launch_norm<T, W, 1, 4>(a, s, backward, st) : s.nv == 8 ? launch_norm<T, W, 1, 8>(a, s, backward, st) : launch_norm<T, W, 1, 32>(a, s, backward, st);

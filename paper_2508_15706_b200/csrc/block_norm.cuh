@@ -458,20 +458,41 @@ norm_backward_kernel(const NormArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------------------------------------------
-// Rows that divide into pieces of 8 values on 16-byte boundaries (what models have): a warp takes a whole row of up to 2048 columns,
-// up to 8 pieces per lane, wider rows a few warps.  What a row costs besides its values (its sums' exchange, addresses, loop) is paid
-// once per warp, so few warps per row it is; weights sit in shared memory as fp32, column sums in registers, rows come through a ring
-// that every lane fills for itself.  (With 8 columns per thread and 5 to 8 warps a row, the kernels above were bound by issue: 3300 and 1600
-// instructions a row at 1280 and 2048 columns, about 950 and 650 here.)
+// Rows that divide into pieces of 8 values on 16-byte boundaries (what models have): a warp takes a whole row of up to 512 columns, two
+// warps wider ones, up to 8 pieces per lane.  What a row costs besides its values (its sums' exchange, addresses, loop) is paid once per
+// warp, so few warps per row it is; two rather than one, since twice the warps fit the registers and shared memory of the same rows.
+// Weights sit in shared memory as fp32, column sums in registers, rows come through a ring that every lane fills for itself.
 // ------------------------------------------------------------------------------------------------------------------------------
 constexpr int kTeamMaxPieces = 8;
 __host__ __device__ constexpr int norm_team_threads(int nv, bool backward) {  // of a CTA: what its registers allow
-    return backward ? (nv <= 1 ? 640 : nv <= 2 ? 512 : nv <= 5 ? 384 : 256) : (nv <= 2 ? 1024 : nv <= 4 ? 512 : 384);
+    return backward ? (nv <= 1 ? 640 : nv <= 3 ? 512 : nv <= 5 ? 384 : 256) : (nv <= 2 ? 1024 : nv <= 4 ? 640 : nv <= 6 ? 512 : 384);
 }
 
-// Threads of a row: a warp, known when compiling (offsets become immediate), or as many as the launch says.
-template <bool WARP>
-__device__ __forceinline__ int team_width() { return WARP ? 32 : (int)blockDim.x; }
+// Threads of a row: 32 or 64, known when compiling (offsets become immediate), or (TEAM = 0) as many as the launch says, the CTA's.
+template <int TEAM>
+__device__ __forceinline__ int team_width() { return TEAM ? TEAM : (int)blockDim.x; }
+
+// Sums over a row's threads, the same in all of them.  Two warps meet at a barrier of their own (one per row of the CTA); `buf` holds
+// [2 K] floats per row for them and must not be written again before both have read: callers alternate.
+template <int K, int TEAM>
+__device__ __forceinline__ void team_sums(float (&s)[K], float* buf) {
+    if (TEAM == 0) {
+        row_sums<K>(s, buf);
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) s[k] = warp_sum(s[k]);
+    if (TEAM == 64) {
+        float* own = buf + threadIdx.y * 2 * K;
+        if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) own[2 * k + (threadIdx.x >> 5)] = s[k];
+        }
+        asm volatile("bar.sync %0, 64;" ::"r"(threadIdx.y + 1) : "memory");
+#pragma unroll
+        for (int k = 0; k < K; ++k) s[k] = own[2 * k] + own[2 * k + 1];
+    }
+}
 
 // 8 values of T as 16-byte chunks, chunk h of all threads together (no bank conflicts)
 template <class T>
@@ -504,7 +525,7 @@ __device__ __forceinline__ void team_put(T* p, const float2 (&f)[4]) {
 }
 
 // The thread's pieces of a matrix, row by row.
-template <class T, int NV, bool WARP>
+template <class T, int NV, int TEAM>
 struct TeamMatrix {
     const T* row;    // null: absent
     long long step;
@@ -512,9 +533,9 @@ struct TeamMatrix {
     __device__ __forceinline__ TeamMatrix(const void* base, long long ld, long long first, long long stride, unsigned ring, int array) {
         row = base ? static_cast<const T*>(base) + first * ld + threadIdx.x * 8 : nullptr;
         step = base ? stride * ld : 0;
-        place = ring + (unsigned)(array * NV * Chunks<T>::kNum * team_width<WARP>() + (int)threadIdx.x) * 16u;
+        place = ring + (unsigned)(array * NV * Chunks<T>::kNum * team_width<TEAM>() + (int)threadIdx.x) * 16u;
     }
-    __device__ __forceinline__ unsigned at(int i) const { return place + (unsigned)(i * Chunks<T>::kNum * team_width<WARP>()) * 16u; }
+    __device__ __forceinline__ unsigned at(int i) const { return place + (unsigned)(i * Chunks<T>::kNum * team_width<TEAM>()) * 16u; }
     __device__ __forceinline__ void clear(int stages, unsigned stage_bytes, int pieces) const {
         for (int s = 0; s < stages; ++s)
 #pragma unroll
@@ -522,7 +543,7 @@ struct TeamMatrix {
                 if (!row || i >= pieces)
 #pragma unroll
                     for (int h = 0; h < Chunks<T>::kNum; ++h)
-                        asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at(i) + (unsigned)s * stage_bytes + (unsigned)(h * team_width<WARP>()) * 16u), "r"(0u) : "memory");
+                        asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at(i) + (unsigned)s * stage_bytes + (unsigned)(h * team_width<TEAM>()) * 16u), "r"(0u) : "memory");
     }
     __device__ __forceinline__ void fetch(unsigned stage_at, int pieces) {
         if (!row) return;
@@ -531,16 +552,16 @@ struct TeamMatrix {
             if (i < pieces)
 #pragma unroll
                 for (int h = 0; h < Chunks<T>::kNum; ++h)
-                    copy_async<16>(at(i) + stage_at + (unsigned)(h * team_width<WARP>()) * 16u, row + i * team_width<WARP>() * 8 + h * (16 / (int)sizeof(T)));
+                    copy_async<16>(at(i) + stage_at + (unsigned)(h * team_width<TEAM>()) * 16u, row + i * team_width<TEAM>() * 8 + h * (16 / (int)sizeof(T)));
         row += step;
     }
-    __device__ __forceinline__ void get(unsigned stage_at, int i, float2 (&f)[4]) const { team_get<T>(at(i) + stage_at, (unsigned)team_width<WARP>() * 16u, f); }
+    __device__ __forceinline__ void get(unsigned stage_at, int i, float2 (&f)[4]) const { team_get<T>(at(i) + stage_at, (unsigned)team_width<TEAM>() * 16u, f); }
 };
 
 // fp32 weights (times those of `times`) of all columns into shared memory at `to`, by the CTA: chunk 0 of every piece, then chunk 1.
-template <class W, int NV, bool WARP>
+template <class W, int NV, int TEAM>
 __device__ __forceinline__ void team_weights(unsigned to, const void* w, const void* times, int cols) {
-    for (int v = threadIdx.y * blockDim.x + threadIdx.x; v < NV * team_width<WARP>(); v += blockDim.x * blockDim.y) {
+    for (int v = threadIdx.y * blockDim.x + threadIdx.x; v < NV * team_width<TEAM>(); v += blockDim.x * blockDim.y) {
         float f[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) f[j] = 1.0f;
@@ -559,28 +580,28 @@ __device__ __forceinline__ void team_weights(unsigned to, const void* w, const v
             }
         }
         // piece i, thread x: v = i * blockDim.x + x
-        const unsigned i = (unsigned)v / (unsigned)team_width<WARP>(), x = (unsigned)v - i * (unsigned)team_width<WARP>();
+        const unsigned i = (unsigned)v / (unsigned)team_width<TEAM>(), x = (unsigned)v - i * (unsigned)team_width<TEAM>();
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to + ((2u * i + h) * (unsigned)team_width<WARP>() + x) * 16u), "f"(f[4 * h]), "f"(f[4 * h + 1]), "f"(f[4 * h + 2]), "f"(f[4 * h + 3]) : "memory");
+            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to + ((2u * i + h) * (unsigned)team_width<TEAM>() + x) * 16u), "f"(f[4 * h]), "f"(f[4 * h + 1]), "f"(f[4 * h + 2]), "f"(f[4 * h + 3]) : "memory");
     }
 }
 
 // blockDim = (threads of a row, rows of the CTA); shared memory: weights [2][NV][2][blockDim.x] chunks, then every row's ring.
-template <class T, class W, int NV, bool FULL, bool WARP>
+template <class T, class W, int NV, bool FULL, int TEAM>
 __global__ void __launch_bounds__(norm_team_threads(NV, false), 1)
 norm_forward_team_kernel(const NormArgs a) {
     extern __shared__ __align__(16) char shared[];
-    __shared__ float sums[2][16];
-    clear_sums(sums[0], 32);
-    const unsigned weights = (unsigned)__cvta_generic_to_shared(shared), table = 2u * NV * (unsigned)team_width<WARP>() * 16u;
-    const unsigned stage_bytes = (FULL ? 3u : 2u) * NV * Chunks<T>::kNum * (unsigned)team_width<WARP>() * 16u, ring_bytes = (unsigned)a.stages * stage_bytes;
+    __shared__ float sums[2][32];
+    if (TEAM == 0) clear_sums(sums[0], 64);
+    const unsigned weights = (unsigned)__cvta_generic_to_shared(shared), table = 2u * NV * (unsigned)team_width<TEAM>() * 16u;
+    const unsigned stage_bytes = (FULL ? 3u : 2u) * NV * Chunks<T>::kNum * (unsigned)team_width<TEAM>() * 16u, ring_bytes = (unsigned)a.stages * stage_bytes;
     const unsigned ring = weights + 2u * table + threadIdx.y * ring_bytes;
     const long long stride = (long long)gridDim.x * blockDim.y;
     long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y;
     const bool normed = a.branch_weight != nullptr, has_branch = a.branch != nullptr;
-    const int vectors = a.cols / 8, pieces = vectors > (int)threadIdx.x ? min(NV, (vectors - (int)threadIdx.x - 1) / team_width<WARP>() + 1) : 0;
-    TeamMatrix<T, NV, WARP> mx(a.x, a.ld_x, row, stride, ring, 0), mb(a.branch, a.ld_branch, row, stride, ring, 1), mg(FULL ? a.gate : nullptr, a.ld_gate, row, stride, ring, 2);
+    const int vectors = a.cols / 8, pieces = vectors > (int)threadIdx.x ? min(NV, (vectors - (int)threadIdx.x - 1) / team_width<TEAM>() + 1) : 0;
+    TeamMatrix<T, NV, TEAM> mx(a.x, a.ld_x, row, stride, ring, 0), mb(a.branch, a.ld_branch, row, stride, ring, 1), mg(FULL ? a.gate : nullptr, a.ld_gate, row, stride, ring, 2);
     mx.clear(a.stages, stage_bytes, pieces);
     mb.clear(a.stages, stage_bytes, pieces);
     if (FULL) mg.clear(a.stages, stage_bytes, pieces);
@@ -595,10 +616,10 @@ norm_forward_team_kernel(const NormArgs a) {
         copy_commit();
     };
     for (int k = 0; k < a.stages - 1; ++k) fetch((unsigned)k * stage_bytes);
-    team_weights<W, NV, WARP>(weights, a.weight, nullptr, a.cols);
-    team_weights<W, NV, WARP>(weights + table, a.branch_weight, a.gate_kind == SL_GATE_COLUMN ? a.gate : nullptr, a.cols);
+    team_weights<W, NV, TEAM>(weights, a.weight, nullptr, a.cols);
+    team_weights<W, NV, TEAM>(weights + table, a.branch_weight, a.gate_kind == SL_GATE_COLUMN ? a.gate : nullptr, a.cols);
     __syncthreads();
-    const unsigned mine = weights + threadIdx.x * 16u, plane = (unsigned)team_width<WARP>() * 16u;  // this thread's weights: piece i at mine + 2 i plane
+    const unsigned mine = weights + threadIdx.x * 16u, plane = (unsigned)team_width<TEAM>() * 16u;  // this thread's weights: piece i at mine + 2 i plane
     T* y = static_cast<T*>(a.y) + (a.y ? row * a.ld_y + threadIdx.x * 8 : 0);
     T* h = static_cast<T*>(a.h) + (a.h ? row * a.ld_h + threadIdx.x * 8 : 0);
     for (unsigned at = 0; row < a.rows; row += stride) {
@@ -616,7 +637,7 @@ norm_forward_team_kernel(const NormArgs a) {
                     for (int j = 0; j < 4; ++j) q = fma2(z[j], z[j], q);
                 }
                 float s[1] = {q.x + q.y};
-                row_sums<1>(s, sums[0]);
+                team_sums<1, TEAM>(s, sums[0]);
                 rb = reciprocal_root(fmaf(s[0], a.inv_cols, a.eps));
                 if (a.branch_rstd && threadIdx.x == 0) a.branch_rstd[row] = rb;
                 q = both(0.0f);
@@ -635,7 +656,7 @@ norm_forward_team_kernel(const NormArgs a) {
                     v[i][j] = fma2(mul2(z[j], both(scale)), FULL ? mul2(c[j], g[j]) : c[j], v[i][j]);
                     q = fma2(v[i][j], v[i][j], q);
                 }
-                if (i < pieces) team_put(y + i * team_width<WARP>() * 8, v[i]);
+                if (i < pieces) team_put(y + i * team_width<TEAM>() * 8, v[i]);
             }
             y += stride * a.ld_y;
         } else {
@@ -649,7 +670,7 @@ norm_forward_team_kernel(const NormArgs a) {
         at = at + stage_bytes == ring_bytes ? 0u : at + stage_bytes;
         if (!a.h) continue;
         float s[1] = {q.x + q.y};
-        row_sums<1>(s, sums[1]);
+        team_sums<1, TEAM>(s, sums[1]);
         const float r = reciprocal_root(fmaf(s[0], a.inv_cols, a.eps));
         if (a.rstd && threadIdx.x == 0) a.rstd[row] = r;
 #pragma unroll
@@ -658,27 +679,27 @@ norm_forward_team_kernel(const NormArgs a) {
             team_get<float>(mine + 2u * i * plane, plane, w);
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[j] = mul2(mul2(v[i][j], both(r)), w[j]);
-            if (i < pieces) team_put(h + i * team_width<WARP>() * 8, w);
+            if (i < pieces) team_put(h + i * team_width<TEAM>() * 8, w);
         }
         h += stride * a.ld_h;
     }
 }
 
 // The formulas are norm_backward_kernel's; a row's pieces and weights are read again for the second half.
-template <class T, class W, int NV, bool FULL, bool WARP>
+template <class T, class W, int NV, bool FULL, int TEAM>
 __global__ void __launch_bounds__(norm_team_threads(NV, true), 1)
 norm_backward_team_kernel(const NormArgs a) {
     extern __shared__ __align__(16) char shared[];  // the rings become [rows of the CTA][2][cols] column sums at the end
-    __shared__ float sums[2][3 * 16];
-    clear_sums(sums[0], 2 * 3 * 16);
-    const unsigned weights = (unsigned)__cvta_generic_to_shared(shared), table = 2u * NV * (unsigned)team_width<WARP>() * 16u;
-    const unsigned stage_bytes = (FULL ? 5u : 4u) * NV * Chunks<T>::kNum * (unsigned)team_width<WARP>() * 16u, ring_bytes = (unsigned)a.stages * stage_bytes;
+    __shared__ float sums[2][3 * 32];
+    if (TEAM == 0) clear_sums(sums[0], 2 * 3 * 32);
+    const unsigned weights = (unsigned)__cvta_generic_to_shared(shared), table = 2u * NV * (unsigned)team_width<TEAM>() * 16u;
+    const unsigned stage_bytes = (FULL ? 5u : 4u) * NV * Chunks<T>::kNum * (unsigned)team_width<TEAM>() * 16u, ring_bytes = (unsigned)a.stages * stage_bytes;
     const unsigned ring = weights + 2u * table + threadIdx.y * ring_bytes;
     const long long stride = (long long)gridDim.x * blockDim.y;
     long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y;
     const bool normed = a.branch_weight != nullptr, row_gate = a.gate_kind == SL_GATE_ROW;
-    const int vectors = a.cols / 8, pieces = vectors > (int)threadIdx.x ? min(NV, (vectors - (int)threadIdx.x - 1) / team_width<WARP>() + 1) : 0;
-    TeamMatrix<T, NV, WARP> mdy(a.dy, a.ld_dy, row, stride, ring, 0), mdh(a.dh, a.ld_dh, row, stride, ring, 1), my(a.dh ? a.x : nullptr, a.ld_y, row, stride, ring, 2),
+    const int vectors = a.cols / 8, pieces = vectors > (int)threadIdx.x ? min(NV, (vectors - (int)threadIdx.x - 1) / team_width<TEAM>() + 1) : 0;
+    TeamMatrix<T, NV, TEAM> mdy(a.dy, a.ld_dy, row, stride, ring, 0), mdh(a.dh, a.ld_dh, row, stride, ring, 1), my(a.dh ? a.x : nullptr, a.ld_y, row, stride, ring, 2),
         mb(a.branch, a.ld_branch, row, stride, ring, 3), mg(FULL ? a.gate : nullptr, a.ld_gate, row, stride, ring, 4);
     mdy.clear(a.stages, stage_bytes, pieces);
     mdh.clear(a.stages, stage_bytes, pieces);
@@ -705,10 +726,10 @@ norm_backward_team_kernel(const NormArgs a) {
     };
     for (int k = 0; k < a.stages - 1; ++k) fetch((unsigned)k * stage_bytes);
     if (row < a.rows) scalars(row);
-    team_weights<W, NV, WARP>(weights, a.weight, nullptr, a.cols);
-    team_weights<W, NV, WARP>(weights + table, a.branch_weight, a.gate_kind == SL_GATE_COLUMN ? a.gate : nullptr, a.cols);
+    team_weights<W, NV, TEAM>(weights, a.weight, nullptr, a.cols);
+    team_weights<W, NV, TEAM>(weights + table, a.branch_weight, a.gate_kind == SL_GATE_COLUMN ? a.gate : nullptr, a.cols);
     __syncthreads();
-    const unsigned mine = weights + threadIdx.x * 16u, plane = (unsigned)team_width<WARP>() * 16u;
+    const unsigned mine = weights + threadIdx.x * 16u, plane = (unsigned)team_width<TEAM>() * 16u;
     float2 acc[2][NV][4];
 #pragma unroll
     for (int i = 0; i < NV; ++i)
@@ -743,7 +764,7 @@ norm_backward_team_kernel(const NormArgs a) {
             }
         }
         float s[3] = {t0.x + t0.y, t1.x + t1.y, t2.x + t2.y};
-        row_sums<3>(s, sums[turn]);
+        team_sums<3, TEAM>(s, sums[turn]);
         const float mean = s[0] * r * a.inv_cols;
         const float qdx = rb * fmaf(-r * mean, s[2] * r, s[1]);  // sum q dx
         const float bmean = a.alpha * rg * qdx * a.inv_cols;      // mean(dz branch_weight bhat)
@@ -775,9 +796,9 @@ norm_backward_team_kernel(const NormArgs a) {
                 dh[j] = fma2(e, c[j], mul2(bh[j], nb));                          // dbranch (rb is 1 and rbm 0 without its norm)
             }
             if (i < pieces) {
-                if (a.dx) team_put(dx + i * team_width<WARP>() * 8, dy);
-                if (a.dbranch) team_put(dbranch + i * team_width<WARP>() * 8, dh);
-                if (FULL && a.dgate) team_put(dgate + i * team_width<WARP>() * 8, g);
+                if (a.dx) team_put(dx + i * team_width<TEAM>() * 8, dy);
+                if (a.dbranch) team_put(dbranch + i * team_width<TEAM>() * 8, dh);
+                if (FULL && a.dgate) team_put(dgate + i * team_width<TEAM>() * 8, g);
             }
         }
         dx += stride * a.ld_x;
@@ -796,7 +817,7 @@ norm_backward_team_kernel(const NormArgs a) {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if (i < pieces) {
-                const unsigned to = down + ((threadIdx.y * 2u + k) * (unsigned)a.cols + (unsigned)(i * team_width<WARP>() + (int)threadIdx.x) * 8u) * 4u;
+                const unsigned to = down + ((threadIdx.y * 2u + k) * (unsigned)a.cols + (unsigned)(i * team_width<TEAM>() + (int)threadIdx.x) * 8u) * 4u;
                 asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to), "f"(acc[k][i][0].x), "f"(acc[k][i][0].y), "f"(acc[k][i][1].x), "f"(acc[k][i][1].y) : "memory");
                 asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to + 16u), "f"(acc[k][i][2].x), "f"(acc[k][i][2].y), "f"(acc[k][i][3].x), "f"(acc[k][i][3].y) : "memory");
             }

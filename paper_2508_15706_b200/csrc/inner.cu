@@ -85,12 +85,20 @@ sl_status launch_rotary(const RopeArgs& a, bool half, unsigned grid, size_t smem
 }
 
 // ---- loss
-template <class K, class T>
-sl_status launch_loss_kernel(K kern, const LossArgs& a, const T* logits, T* grad, int threads, int cluster, cudaStream_t st) {
+template <class T, int NV>
+sl_status launch_loss_rows(const LossArgs& a, const T* logits, T* grad, int threads, int cluster, int n_sms, cudaStream_t st) {
+    constexpr int V = 16 / (int)sizeof(T);
+    // as many CTAs as are resident: threads (by the launch bounds' registers) and shared memory
+    const size_t smem = (size_t)kLossStages * NV * threads * 16;
+    const long long ctas = std::max(1ll, std::min(32ll, std::min((NV * V <= 32 ? 1024ll : 512ll) / threads, 222ll * 1024 / ((long long)smem + 2048))));
+    const long long teams = std::min((long long)a.rows, std::max(1ll, n_sms * ctas / cluster));
+    const auto kern = loss_row_kernel<T, V, NV>;
+    if (smem > 47 * 1024) SL_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024));
     cudaLaunchConfig_t lc;
     memset(&lc, 0, sizeof(lc));
-    lc.gridDim = dim3((unsigned)(a.rows * cluster));
+    lc.gridDim = dim3((unsigned)(teams * cluster));
     lc.blockDim = dim3((unsigned)threads);
+    lc.dynamicSmemBytes = smem;
     lc.stream = st;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // behind the count, which waits for what came before it
@@ -100,35 +108,34 @@ sl_status launch_loss_kernel(K kern, const LossArgs& a, const T* logits, T* grad
     at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     lc.attrs = at;
     lc.numAttrs = cluster > 1 ? 2 : 1;
-    SL_CUDA(kern(lc, a, logits, grad, cluster));
+    SL_CUDA(cudaLaunchKernelEx(&lc, kern, a, logits, grad, cluster));
     return SL_OK;
 }
 
-template <class T, int NV>
-sl_status launch_loss_rows(const LossArgs& a, const T* logits, T* grad, int threads, int cluster, cudaStream_t st) {
-    return launch_loss_kernel([](const cudaLaunchConfig_t& lc, const LossArgs& a_, const T* x, T* g, int c) { return cudaLaunchKernelEx(&lc, loss_row_kernel<T, 16 / (int)sizeof(T), NV>, a_, x, g, c); },
-                              a, logits, grad, threads, cluster, st);
+template <class T, int VEC>
+sl_status launch_loss_stream(const LossArgs& a, const T* logits, T* grad, cudaStream_t st) {
+    loss_stream_kernel<T, VEC><<<(unsigned)a.rows, kLossThreads, 0, st>>>(a, logits, grad);
+    SL_CUDA(cudaGetLastError());
+    return SL_OK;
 }
 
 template <class T>
 sl_status launch_loss(const LossArgs& a, const T* logits, T* grad, bool same, int n_sms, cudaStream_t st) {
     constexpr int V = 16 / (int)sizeof(T), kMaxNv = 8;
     const long long vectors = std::max(1, a.vocab / V);
-    if (!same)
-        return launch_loss_kernel([](const cudaLaunchConfig_t& lc, const LossArgs& a_, const T* x, T* g, int) { return cudaLaunchKernelEx(&lc, loss_stream_kernel<T, 1>, a_, x, g); }, a, logits,
-                                  grad, kLossThreads, 1, st);
-    if (vectors > 8ll * kLossThreads * kMaxNv || a.rows * 8 > 0x7FFFFFFFll)
-        return launch_loss_kernel([](const cudaLaunchConfig_t& lc, const LossArgs& a_, const T* x, T* g, int) { return cudaLaunchKernelEx(&lc, loss_stream_kernel<T, V>, a_, x, g); }, a, logits,
-                                  grad, kLossThreads, 1, st);
+    if (!same) return launch_loss_stream<T, 1>(a, logits, grad, st);
+    if (vectors > 8ll * kLossThreads * kMaxNv || a.rows * 8 > 0x7FFFFFFFll) return launch_loss_stream<T, V>(a, logits, grad, st);
     // as few CTAs as hold the row; more while there are SMs without one and every thread would keep a vector
     int cluster = 1;
     while (vectors > (long long)cluster * kLossThreads * kMaxNv) cluster *= 2;
     while (cluster < 8 && a.rows * cluster < n_sms && vectors >= 2ll * cluster * kLossThreads) cluster *= 2;
     const long long per = (vectors + cluster - 1) / cluster;
     const int nv = per <= kLossThreads ? 1 : per <= 2 * kLossThreads ? 2 : per <= 4 * kLossThreads ? 4 : 8;
+    // (a thread's last vector may be missing, the others are there in every part of every row: parts are at most cluster + 1 vectors
+    // shorter than `per`, far less than the vectors by which nv steps up)
     const int threads = (int)((per + nv - 1) / nv + 31) / 32 * 32;
-    return nv == 1 ? launch_loss_rows<T, 1>(a, logits, grad, threads, cluster, st) : nv == 2 ? launch_loss_rows<T, 2>(a, logits, grad, threads, cluster, st)
-         : nv == 4 ? launch_loss_rows<T, 4>(a, logits, grad, threads, cluster, st) : launch_loss_rows<T, 8>(a, logits, grad, threads, cluster, st);
+    return nv == 1 ? launch_loss_rows<T, 1>(a, logits, grad, threads, cluster, n_sms, st) : nv == 2 ? launch_loss_rows<T, 2>(a, logits, grad, threads, cluster, n_sms, st)
+         : nv == 4 ? launch_loss_rows<T, 4>(a, logits, grad, threads, cluster, n_sms, st) : launch_loss_rows<T, 8>(a, logits, grad, threads, cluster, n_sms, st);
 }
 
 bool overlaps_no(const sl_tensor_desc* tensors, int n) {

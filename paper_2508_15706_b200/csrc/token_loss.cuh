@@ -1,8 +1,9 @@
 // Next-token loss and its gradient.  Part of libsparseloco (inner.cu).
 //
-// Bound: HBM (logits read once, gradient written once).  A row stays in the registers of its CTA, or of the CTAs of a cluster where
-// one CTA cannot hold it or there are fewer rows than SMs: one pass for a maximum and a sum of exponentials per thread, one
-// exchange, then the gradient from the same registers.
+// Bound: HBM (logits read once, gradient written once).  CTAs stay and walk over rows.  A row, or the part of it that a CTA of a cluster
+// has, comes through a ring in shared memory two rows ahead; its exponentials relative to each thread's own maximum stay in
+// registers until the row's maximum and sum are known, and the gradient is those times one factor per thread: one exponential per
+// logit.  (Computed a second time instead, with the row's bits in registers, they bound the kernel: 318 us at 8192 x 32000.)
 // Exponentials are 2^(x log2 e - M), one fused multiply-add and one instruction: M stands for the maximum in that scale, and its
 // rounding moves nothing as long as it is the same M everywhere.  Where |x log2 e| could overflow (a row of the type's lowest
 // value) the factor is 1 instead: numbers of that size are equal or differ by more than any exponential can show.
@@ -77,21 +78,45 @@ __device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
     m = top;
 }
 
+// The CTA's maximum, sum and plain sum from its threads', the same in every thread, each exchange one scaling per thread: first the
+// maximum, then the sums relative to it.  `buf`: [3][32], not to be written again before every thread has read it: callers alternate.
+__device__ __forceinline__ void block_join(float& m, float& s, float& sum, bool with_sum, float (*buf)[32]) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    float top = warp_max(m);
+    s = top == -INFINITY ? warp_sum(s) : warp_sum(s * exp2_fast(m - top));
+    if (with_sum) sum = warp_sum(sum);
+    if (lane == 0) buf[0][warp] = top, buf[1][warp] = s, buf[2][warp] = sum;
+    __syncthreads();
+    m = lane < warps ? buf[0][lane] : -INFINITY;
+    s = lane < warps ? buf[1][lane] : 0.0f;
+    top = warp_max(m);
+    s = top == -INFINITY ? warp_sum(s) : warp_sum(s * exp2_fast(m - top));
+    if (with_sum) sum = warp_sum(lane < warps ? buf[2][lane] : 0.0f);
+    m = top;
+}
+
 // What a row comes to, from its maximum, sum and target.
 struct LossRow {
-    float m, s, sum, lse, w, scale;
+    float m, s, sum, lse, scale;
     long long target;
-    int valid;
     bool counts, inside, empty;
     __device__ __forceinline__ bool has_gradient() const { return counts && inside && !empty; }
+    __device__ __forceinline__ void aim(const LossArgs& a, long long its_target) {
+        target = its_target;
+        counts = target != a.ignore_index;
+        inside = target >= 0 && target < a.vocab;
+    }
+    __device__ __forceinline__ void finish() {
+        empty = m == -INFINITY && s == 0.0f;  // every logit is -inf
+        scale = fabsf(m) < 1e30f ? kLog2e : 1.0f;
+        lse = empty ? -INFINITY : scale == 1.0f ? m + logf(s) : (m + log2f(s)) * kLn2;
+    }
 };
-__device__ __forceinline__ void finish_row(const LossArgs& a, LossRow& r) {
-    r.empty = r.m == -INFINITY && r.s == 0.0f;  // every logit is -inf
-    r.scale = fabsf(r.m) < 1e30f ? kLog2e : 1.0f;
-    r.lse = r.empty ? -INFINITY : r.scale == 1.0f ? r.m + logf(r.s) : (r.m + log2f(r.s)) * kLn2;
+// 1 / (rows that count), or 1, times the caller's scale; the count comes from the kernel before
+__device__ __forceinline__ float row_weight(const LossArgs& a, int& valid) {
     cudaGridDependencySynchronize();
-    r.valid = __ldcg(&a.work->valid);
-    r.w = a.mean ? a.scale / (float)(r.valid > 0 ? r.valid : 1) : a.scale;
+    valid = __ldcg(&a.work->valid);
+    return a.mean ? a.scale / (float)(valid > 0 ? valid : 1) : a.scale;
 }
 __device__ __forceinline__ void write_row(const LossArgs& a, const LossRow& r, long long row, float xt) {
     float loss = 0.0f;
@@ -106,14 +131,14 @@ __device__ __forceinline__ void write_row(const LossArgs& a, const LossRow& r, l
     a.row_loss[row] = loss;
     if (a.lse) a.lse[row] = r.lse;
 }
-// The last of `rows` callers adds the rows' losses in a fixed order: thread by thread, then thread after thread.
-__device__ __forceinline__ void add_rows(const LossArgs& a, const LossRow& r) {
+// The last of `callers` CTAs adds the rows' losses in a fixed order: thread by thread, then thread after thread.
+__device__ __forceinline__ void add_rows(const LossArgs& a, unsigned callers, float w, int valid) {
     __shared__ int last;
     __shared__ double st[32];
     if (!a.total) return;
     if (threadIdx.x == 0) {
         __threadfence();
-        last = atomicAdd(&a.work->ticket, 1u) == (unsigned)(a.rows - 1);
+        last = atomicAdd(&a.work->ticket, 1u) == callers - 1;
     }
     __syncthreads();
     if (!last) return;
@@ -126,142 +151,207 @@ __device__ __forceinline__ void add_rows(const LossArgs& a, const LossRow& r) {
     if (threadIdx.x == 0) {
         t = 0.0;
         for (int i = 0; i < (int)(blockDim.x >> 5); ++i) t += st[i];
-        *a.total = r.valid > 0 ? (float)(t * (double)r.w) : 0.0f;
+        *a.total = valid > 0 ? (float)(t * (double)w) : 0.0f;
     }
 }
 
-// A row in registers: NV accesses of VEC values per thread, `cluster` CTAs per row.  The vector body begins at the row's first
-// 16-byte boundary; the values before it belong to the first CTA, those behind it to the last, one per thread.
+// The largest of a vector's values (never NaN unless all are).
+template <class T, int VEC>
+__device__ __forceinline__ float top_of(const unsigned (&w)[4]) {
+    if (sizeof(T) == 2) {
+        __nv_bfloat162 t[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) t[j] = *reinterpret_cast<const __nv_bfloat162*>(&w[j]);
+        t[0] = __hmax2(__hmax2(t[0], t[1]), __hmax2(t[2], t[3]));
+        const float2 f = widen2(*reinterpret_cast<const unsigned*>(&t[0]));
+        return fmaxf(f.x, f.y);
+    }
+    return fmaxf(fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1])), fmaxf(__uint_as_float(w[2]), __uint_as_float(w[3])));
+}
+template <class T, int VEC>
+__device__ __forceinline__ void unpack(const unsigned (&w)[4], float2 (&f)[VEC / 2]) {
+#pragma unroll
+    for (int j = 0; j < VEC / 2; ++j) f[j] = sizeof(T) == 2 ? widen2(w[j]) : make_float2(__uint_as_float(w[(2 * j) & 3]), __uint_as_float(w[(2 * j + 1) & 3]));
+}
+
+// A CTA's part of a row.  The vector body begins at the row's first 16-byte boundary; the values before it belong to the first CTA
+// of the cluster, those behind it to the last, one per thread.
+template <class T, int VEC>
+struct LossPart {
+    const T* x;     // the row
+    int head, begin, vectors, tail;  // this CTA's vectors begin at x + head + begin * VEC; single values from x + tail on
+    __device__ __forceinline__ LossPart(const LossArgs& a, const T* logits, long long row, int rank, int cluster) {
+        x = logits + row * a.ld_logits;
+        head = (int)((16u - (unsigned)(reinterpret_cast<uintptr_t>(x) & 15u)) & 15u) / (int)sizeof(T);
+        if (head > a.vocab) head = a.vocab;
+        const int body = (a.vocab - head) / VEC, per = cluster == 1 ? body : (body + cluster - 1) / cluster;
+        begin = rank * per;
+        vectors = min(body, begin + per) - begin;
+        tail = head + body * VEC;
+    }
+    __device__ __forceinline__ long long base() const { return head + (long long)begin * VEC; }
+    __device__ __forceinline__ int before(int rank) const { return rank == 0 && (int)threadIdx.x < head ? (int)threadIdx.x : -1; }
+    __device__ __forceinline__ int behind(const LossArgs& a, int rank, int cluster) const {
+        return rank == cluster - 1 && tail + (int)threadIdx.x < a.vocab ? tail + (int)threadIdx.x : -1;
+    }
+};
+
+constexpr int kLossStages = 3;
+
+// NV vectors of VEC values per thread; all but a thread's last one exist in every row (the launch sees to it).
 template <class T, int VEC, int NV>
-__global__ void __launch_bounds__(kLossThreads, NV * VEC * (int)sizeof(T) <= 128 ? 2 : 1)
+__global__ void __launch_bounds__(kLossThreads, NV * VEC <= 32 ? 2 : 1)
 loss_row_kernel(const LossArgs a, const T* logits, T* grad, int cluster) {
-    __shared__ float sm[32], ss[32], sx[32];
+    extern __shared__ __align__(16) char ring[];  // [stages][NV][threads] vectors
+    __shared__ float buf[2][3][32];
     __shared__ float mine[4];  // this CTA's maximum, sum of exponentials, sum: read by the cluster
     const int tid = threadIdx.x, threads = blockDim.x;
-    const long long row = blockIdx.x / (unsigned)cluster;
+    const unsigned teams = gridDim.x / (unsigned)cluster;
+    long long row = blockIdx.x / (unsigned)cluster;
     const int rank = (int)(blockIdx.x - (unsigned)row * (unsigned)cluster);
-    const T* x = logits + row * a.ld_logits;
-    int head = (int)((16u - (unsigned)(reinterpret_cast<uintptr_t>(x) & 15u)) & 15u) / (int)sizeof(T);
-    if (head > a.vocab) head = a.vocab;
-    const int body = (a.vocab - head) / VEC, tail = head + body * VEC, per = (body + cluster - 1) / cluster;
-    const int begin = rank * per, end = min(body, begin + per);
-    Pack<T, VEC> v[NV];
+    const unsigned place = (unsigned)__cvta_generic_to_shared(ring) + (unsigned)tid * 16u, pitch = (unsigned)threads * 16u, stage_bytes = (unsigned)NV * pitch;
+    long long coming = row;
+    auto fetch = [&](unsigned stage_at) {
+        if (coming < a.rows) {
+            const LossPart<T, VEC> p(a, logits, coming, rank, cluster);
+            const T* from = p.x + p.base() + tid * VEC;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int at = begin + i * threads + tid;
-        if (at < end) {
-            v[i].load_stream(x + head + at * VEC);
+            for (int i = 0; i < NV; ++i)
+                if (i < NV - 1 || i * threads + tid < p.vectors)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(place + stage_at + i * pitch), "l"(from + i * threads * VEC) : "memory");
+        }
+        coming += teams;
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    for (int k = 0; k < kLossStages - 1; ++k) fetch((unsigned)k * stage_bytes);
+    float w = 0.0f;
+    int valid = 0;
+    bool weighed = false;
+    unsigned at = 0;
+    // targets are known two rows ahead and their logits one row ahead (long before a gradient may take their place), so that no warp
+    // waits for the one to ask for the other
+    const bool writer = rank == 0 && tid == 0;
+    auto target_at = [&](long long i) { return i < a.rows ? target_of(a, i) : -1ll; };
+    auto logit_at = [&](long long i, long long t) { return writer && i < a.rows && t >= 0 && t < a.vocab ? widen(logits[i * a.ld_logits + t]) : 0.0f; };
+    long long target = target_at(row), target_next = target_at(row + teams);
+    float xt = logit_at(row, target);
+    for (int turn = 0; row < a.rows; row += teams, turn ^= 1) {
+        fetch(at ? at - stage_bytes : (kLossStages - 1) * stage_bytes);
+        LossRow r;
+        r.aim(a, target);
+        const LossPart<T, VEC> part(a, logits, row, rank, cluster);
+        const float xt_next = logit_at(row + teams, target_next);
+        const long long target_then = target_at(row + 2ll * teams);
+        const int before = part.before(rank), behind = part.behind(a, rank, cluster);
+        const bool last_too = (NV - 1) * threads + tid < part.vectors;
+        float m = -INFINITY, s, sum = 0.0f, ref;
+        float2 e[NV][VEC / 2];
+        asm volatile("cp.async.wait_group %0;" ::"n"(kLossStages - 1) : "memory");
+        {
+            const float first = before >= 0 ? widen(part.x[before]) : -INFINITY, last_one = behind >= 0 ? widen(part.x[behind]) : -INFINITY;
+            m = fmaxf(first, last_one);
+            unsigned v[NV][4];
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v[i][0]), "=r"(v[i][1]), "=r"(v[i][2]), "=r"(v[i][3]) : "r"(place + at + i * pitch));
+                if (i == NV - 1 && !last_too) v[i][0] = v[i][1] = v[i][2] = v[i][3] = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;  // -inf
+                m = fmaxf(m, top_of<T, VEC>(v[i]));
+            }
+            const float scale = loss_scale(m);
+            ref = loss_offset(m);
+            s = exp2_fast(fmaf(first, scale, -ref)) + exp2_fast(fmaf(last_one, scale, -ref));
+            if (a.smoothing != 0.0f) {
+                sum = (before >= 0 ? first : 0.0f) + (behind >= 0 ? last_one : 0.0f);
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    float2 f[VEC / 2];
+                    unpack<T, VEC>(v[i], f);
+                    if (i < NV - 1 || last_too)
+#pragma unroll
+                        for (int j = 0; j < VEC / 2; ++j) sum += f[j].x + f[j].y;
+                }
+            }
+            const float2 sc = both(scale), of = both(-ref);
+            float2 acc[2] = {both(0.0f), both(0.0f)};
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                unpack<T, VEC>(v[i], e[i]);
+#pragma unroll
+                for (int j = 0; j < VEC / 2; ++j) {
+                    const float2 t = fma2(e[i][j], sc, of);
+                    e[i][j] = make_float2(exp2_fast(t.x), exp2_fast(t.y));
+                    acc[j & 1] = add2(acc[j & 1], e[i][j]);
+                }
+            }
+            acc[0] = add2(acc[0], acc[1]);
+            s += acc[0].x + acc[0].y;
+            m *= scale;
+        }
+        block_join(m, s, sum, a.smoothing != 0.0f, buf[turn]);
+        r.m = m, r.s = s, r.sum = sum;
+        if (cluster > 1) {
+            namespace cg = cooperative_groups;
+            auto group = cg::this_cluster();
+            if (tid == 0) mine[0] = r.m, mine[1] = r.s, mine[2] = r.sum;
+            group.sync();
+            for (int c = 0; c < cluster; ++c) {  // in the same order in every CTA
+                const float* other = group.map_shared_rank(mine, (unsigned)c);
+                const float m2 = other[0], s2 = other[1], x2 = other[2];
+                if (c == 0) r.m = m2, r.s = s2, r.sum = x2;
+                else join(r.m, r.s, m2, s2), r.sum += x2;
+            }
+            group.sync();  // nobody leaves, or writes the next row's, while its values are read
+        }
+        r.finish();
+        if (!weighed) {
+            w = row_weight(a, valid);
+            weighed = true;
+        }
+        if (writer) write_row(a, r, row, xt);
+        target = target_next, target_next = target_then, xt = xt_next;
+        at = at + stage_bytes == kLossStages * stage_bytes ? 0u : at + stage_bytes;
+        if (!grad) continue;
+        T* g = grad + row * a.ld_grad;
+        T* gb = g + part.base() + tid * VEC;
+        if (r.has_gradient()) {
+            const float k = w * fmaf(2.0f * a.z, r.lse, 1.0f) / r.s, off = w * a.smoothing / (float)a.vocab, hit = w * (1.0f - a.smoothing);
+            const float2 k2 = both(k * exp2_fast(ref - r.m)), off2 = both(-off);             // (from the thread's maximum to the row's)
+            const int t = (int)r.target - (int)part.base();                                  // the target's place in this CTA's part
+            const int tv = t >= 0 && t < part.vectors * VEC ? t / VEC : -1, ti = tv - tid;    // ... and its vector, if it is one of this thread's
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                float2 q[VEC / 2];
+#pragma unroll
+                for (int j = 0; j < VEC / 2; ++j) q[j] = fma2(k2, e[i][j], off2);
+                if (tv >= 0 && ti == i * threads) {
+#pragma unroll
+                    for (int j = 0; j < VEC / 2; ++j) {
+                        if (2 * j == t - tv * VEC) q[j].x -= hit;
+                        if (2 * j + 1 == t - tv * VEC) q[j].y -= hit;
+                    }
+                }
+                if (i < NV - 1 || last_too) {
+                    uint4 o;
+                    if (sizeof(T) == 2) o = make_uint4(narrow2(q[0]), narrow2(q[1]), narrow2(q[(VEC / 2 - 1) & 2]), narrow2(q[VEC / 2 - 1]));
+                    else o = make_uint4(__float_as_uint(q[0].x), __float_as_uint(q[0].y), __float_as_uint(q[1].x), __float_as_uint(q[1].y));
+                    __stcs(reinterpret_cast<uint4*>(gb + i * threads * VEC), o);
+                }
+            }
+            auto one = [&](int i) {
+                const float d = fmaf(k, exp2_fast(fmaf(widen(part.x[i]), r.scale, -r.m)), -off);
+                g[i] = narrow<T>(i == (int)r.target ? d - hit : d);
+            };
+            if (before >= 0) one(before);
+            if (behind >= 0) one(behind);
         } else {
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) v[i].v[j] = narrow<T>(-INFINITY);
+            for (int i = 0; i < NV; ++i)
+                if (i < NV - 1 || last_too) __stcs(reinterpret_cast<uint4*>(gb + i * threads * VEC), make_uint4(0u, 0u, 0u, 0u));
+            if (before >= 0) g[before] = narrow<T>(0.0f);
+            if (behind >= 0) g[behind] = narrow<T>(0.0f);
         }
     }
-    // a single value before or behind the body (each at most VEC - 1 of them; both ends may be in one CTA)
-    const int before = rank == 0 && tid < head ? tid : -1, behind = rank == cluster - 1 && tail + tid < a.vocab ? tail + tid : -1;
-    const float first = before >= 0 ? widen(x[before]) : -INFINITY, last_one = behind >= 0 ? widen(x[behind]) : -INFINITY;
-    LossRow r;
-    r.target = target_of(a, row);
-    r.counts = r.target != a.ignore_index;
-    r.inside = r.target >= 0 && r.target < a.vocab;
-    const float xt = r.counts && r.inside ? widen(x[r.target]) : 0.0f;  // (before any gradient takes its place: a barrier follows)
-
-    float m = fmaxf(first, last_one);
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        float f[VEC];
-        v[i].get(f);
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) m = fmaxf(m, f[j]);
-    }
-    const float scale = loss_scale(m), ref = loss_offset(m);
-    float s = exp2_fast(fmaf(first, scale, -ref)) + exp2_fast(fmaf(last_one, scale, -ref)), sum = 0.0f;
-    if (a.smoothing != 0.0f) {
-        sum = (before >= 0 ? first : 0.0f) + (behind >= 0 ? last_one : 0.0f);
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (begin + i * threads + tid < end) {
-                float f[VEC];
-                v[i].get(f);
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) sum += f[j];
-            }
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        float f[VEC], part = 0.0f;  // (short chains of additions)
-        v[i].get(f);
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) part += exp2_fast(fmaf(f[j], scale, -ref));
-        s += part;
-    }
-    m *= scale;
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        const float m2 = __shfl_xor_sync(kFullMask, m, o), s2 = __shfl_xor_sync(kFullMask, s, o);
-        join(m, s, m2, s2);
-        if (a.smoothing != 0.0f) sum += __shfl_xor_sync(kFullMask, sum, o);
-    }
-    if ((tid & 31) == 0) sm[tid >> 5] = m, ss[tid >> 5] = s, sx[tid >> 5] = sum;
-    __syncthreads();
-    r.m = sm[0], r.s = ss[0], r.sum = sx[0];
-    for (int w = 1; w < threads / 32; ++w) {
-        join(r.m, r.s, sm[w], ss[w]);
-        r.sum += sx[w];
-    }
-    if (cluster > 1) {
-        namespace cg = cooperative_groups;
-        auto group = cg::this_cluster();
-        if (tid == 0) mine[0] = r.m, mine[1] = r.s, mine[2] = r.sum;
-        group.sync();
-        for (int c = 0; c < cluster; ++c) {  // in the same order in every CTA
-            const float* other = group.map_shared_rank(mine, (unsigned)c);
-            const float m2 = other[0], s2 = other[1], x2 = other[2];
-            if (c == 0) r.m = m2, r.s = s2, r.sum = x2;
-            else join(r.m, r.s, m2, s2), r.sum += x2;
-        }
-        group.sync();  // nobody leaves while its values are read
-    }
-    finish_row(a, r);
-    if (rank == 0 && tid == 0) write_row(a, r, row, xt);
-    if (grad) {
-        T* g = grad + row * a.ld_grad;
-        const bool some = r.has_gradient();
-        const float k = some ? r.w * fmaf(2.0f * a.z, r.lse, 1.0f) / r.s : 0.0f, off = some ? r.w * a.smoothing / (float)a.vocab : 0.0f,
-                    hit = r.w * (1.0f - a.smoothing);
-        const int t = some ? (int)r.target : -1;
-        const int tv = t >= head && t < tail ? (t - head) / VEC : -1, te = t - head - tv * VEC;  // the target's vector and place in it
-        const float top = some ? r.m : 0.0f, scale = r.scale;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int at = begin + i * threads + tid;
-            if (at < end) {
-                float f[VEC];
-                v[i].get(f);
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) f[j] = fmaf(k, exp2_fast(fmaf(f[j], scale, -top)), -off);
-                if (at == tv) {
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j)
-                        if (j == te) f[j] -= hit;
-                }
-                if (!some) {  // (0 times what overflows or is NaN would not be 0)
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) f[j] = 0.0f;
-                }
-                Pack<T, VEC> o;
-                o.set(f);
-                o.store_stream(g + head + at * VEC);
-            }
-        }
-        auto one = [&](int at, float val) {
-            float d = some ? fmaf(k, exp2_fast(fmaf(val, scale, -top)), -off) : 0.0f;
-            if (at == t) d -= hit;
-            g[at] = narrow<T>(d);
-        };
-        if (before >= 0) one(before, first);
-        if (behind >= 0) one(behind, last_one);
-    }
-    if (rank == 0) add_rows(a, r);
+    if (rank == 0) add_rows(a, teams, w, valid);
 }
 
 // The row read twice: a running maximum and sum, then the gradient.
@@ -269,7 +359,7 @@ loss_row_kernel(const LossArgs a, const T* logits, T* grad, int cluster) {
 template <class T, int VEC>
 __global__ void __launch_bounds__(kLossThreads)
 loss_stream_kernel(const LossArgs a, const T* logits, T* grad) {
-    __shared__ float sm[32], ss[32], sx[32];
+    __shared__ float buf[3][32];
     const int tid = threadIdx.x;
     const long long row = blockIdx.x;
     const T* x = logits + row * a.ld_logits;
@@ -281,9 +371,7 @@ loss_stream_kernel(const LossArgs a, const T* logits, T* grad) {
     const int body = VEC > 1 ? (a.vocab - head) / VEC : 0;  // vectors
     const int rest = head + body * VEC;                     // scalars from here on
     LossRow r;
-    r.target = target_of(a, row);
-    r.counts = r.target != a.ignore_index;
-    r.inside = r.target >= 0 && r.target < a.vocab;
+    r.aim(a, target_of(a, row));
     float m = -INFINITY, s = 0.0f, sum = 0.0f;
     float scale = kLog2e, ref = 0.0f;           // m in the scale of the exponentials
     auto rise = [&](float top) {                // the maximum so far goes up to top
@@ -314,26 +402,17 @@ loss_stream_kernel(const LossArgs a, const T* logits, T* grad) {
     }
     for (int i = rest + tid; i < a.vocab; i += kLossThreads) rise(widen(x[i])), see(widen(x[i]));
     m = m == -INFINITY ? m : ref;
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        const float m2 = __shfl_xor_sync(kFullMask, m, o), s2 = __shfl_xor_sync(kFullMask, s, o);
-        join(m, s, m2, s2);
-    }
-    sum = warp_sum(sum);
-    if ((tid & 31) == 0) sm[tid >> 5] = m, ss[tid >> 5] = s, sx[tid >> 5] = sum;
     const float xt = r.counts && r.inside ? widen(x[r.target]) : 0.0f;  // (read before any thread writes a gradient in its place)
-    __syncthreads();
-    r.m = sm[0], r.s = ss[0], r.sum = sx[0];
-    for (int w = 1; w < kLossThreads / 32; ++w) {
-        join(r.m, r.s, sm[w], ss[w]);
-        r.sum += sx[w];
-    }
-    finish_row(a, r);
+    block_join(m, s, sum, true, buf);
+    r.m = m, r.s = s, r.sum = sum;
+    r.finish();
+    int valid;
+    const float w = row_weight(a, valid);
     if (tid == 0) write_row(a, r, row, xt);
     if (grad) {
         T* g = grad + row * a.ld_grad;
         const bool some = r.has_gradient();
-        const float k = some ? r.w * fmaf(2.0f * a.z, r.lse, 1.0f) / r.s : 0.0f, off = r.w * a.smoothing / (float)a.vocab, hit = r.w * (1.0f - a.smoothing);
+        const float k = some ? w * fmaf(2.0f * a.z, r.lse, 1.0f) / r.s : 0.0f, off = w * a.smoothing / (float)a.vocab, hit = w * (1.0f - a.smoothing);
         auto of = [&](float v, int i) {
             if (!some) return 0.0f;
             const float d = fmaf(k, exp2_fast(fmaf(v, r.scale, -r.m)), -off);
@@ -349,7 +428,7 @@ loss_stream_kernel(const LossArgs a, const T* logits, T* grad) {
         }
         for (int i = rest + tid; i < a.vocab; i += kLossThreads) g[i] = narrow<T>(of(widen(x[i]), i));
     }
-    add_rows(a, r);
+    add_rows(a, gridDim.x, w, valid);
 }
 
 }  // namespace
