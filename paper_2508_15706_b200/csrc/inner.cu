@@ -85,14 +85,14 @@ sl_status launch_rotary(const RopeArgs& a, bool half, unsigned grid, size_t smem
 }
 
 // ---- loss
-template <class T, int NV>
+template <class T, int NV, bool RAGGED>
 sl_status launch_loss_rows(const LossArgs& a, const T* logits, T* grad, int threads, int cluster, int n_sms, cudaStream_t st) {
     constexpr int V = 16 / (int)sizeof(T);
     // as many CTAs as are resident: threads (by the launch bounds' registers) and shared memory
-    const size_t smem = (size_t)kLossStages * NV * threads * 16;
+    const size_t smem = (size_t)kLossStages * threads * (NV * 16 + 8);
     const long long ctas = std::max(1ll, std::min(32ll, std::min((NV * V <= 32 ? 1024ll : 512ll) / threads, 222ll * 1024 / ((long long)smem + 2048))));
     const long long teams = std::min((long long)a.rows, std::max(1ll, n_sms * ctas / cluster));
-    const auto kern = loss_row_kernel<T, V, NV>;
+    const auto kern = loss_row_kernel<T, V, NV, RAGGED>;
     if (smem > 47 * 1024) SL_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024));
     cudaLaunchConfig_t lc;
     memset(&lc, 0, sizeof(lc));
@@ -119,6 +119,12 @@ sl_status launch_loss_stream(const LossArgs& a, const T* logits, T* grad, cudaSt
     return SL_OK;
 }
 
+template <class T, bool RAGGED>
+sl_status launch_loss_nv(const LossArgs& a, const T* logits, T* grad, int nv, int threads, int cluster, int n_sms, cudaStream_t st) {
+    return nv == 1 ? launch_loss_rows<T, 1, RAGGED>(a, logits, grad, threads, cluster, n_sms, st) : nv == 2 ? launch_loss_rows<T, 2, RAGGED>(a, logits, grad, threads, cluster, n_sms, st)
+         : nv == 4 ? launch_loss_rows<T, 4, RAGGED>(a, logits, grad, threads, cluster, n_sms, st) : launch_loss_rows<T, 8, RAGGED>(a, logits, grad, threads, cluster, n_sms, st);
+}
+
 template <class T>
 sl_status launch_loss(const LossArgs& a, const T* logits, T* grad, bool same, int n_sms, cudaStream_t st) {
     constexpr int V = 16 / (int)sizeof(T), kMaxNv = 8;
@@ -130,12 +136,21 @@ sl_status launch_loss(const LossArgs& a, const T* logits, T* grad, bool same, in
     while (vectors > (long long)cluster * kLossThreads * kMaxNv) cluster *= 2;
     while (cluster < 8 && a.rows * cluster < n_sms && vectors >= 2ll * cluster * kLossThreads) cluster *= 2;
     const long long per = (vectors + cluster - 1) / cluster;
-    const int nv = per <= kLossThreads ? 1 : per <= 2 * kLossThreads ? 2 : per <= 4 * kLossThreads ? 4 : 8;
+    // as many vectors per thread as there are (what a row costs besides its values is paid by every thread), unless there are so few
+    // rows that the SMs are better filled with threads
+    const int least = a.rows * cluster > 2 * n_sms ? 32 : 256;
+    int nv = 8;
+    while (nv > 1 && per < (long long)nv * least) nv /= 2;
+    while (per > (long long)nv * kLossThreads) nv *= 2;
     // (a thread's last vector may be missing, the others are there in every part of every row: parts are at most cluster + 1 vectors
-    // shorter than `per`, far less than the vectors by which nv steps up)
-    const int threads = (int)((per + nv - 1) / nv + 31) / 32 * 32;
-    return nv == 1 ? launch_loss_rows<T, 1>(a, logits, grad, threads, cluster, n_sms, st) : nv == 2 ? launch_loss_rows<T, 2>(a, logits, grad, threads, cluster, n_sms, st)
-         : nv == 4 ? launch_loss_rows<T, 4>(a, logits, grad, threads, cluster, n_sms, st) : launch_loss_rows<T, 8>(a, logits, grad, threads, cluster, n_sms, st);
+    // shorter than `per`)
+    int threads = (int)((per + nv - 1) / nv + 31) / 32 * 32;
+    while (nv > 1 && (long long)(nv - 1) * threads > per - cluster - 1) {
+        nv /= 2;
+        threads = (int)((per + nv - 1) / nv + 31) / 32 * 32;
+    }
+    const bool ragged = !fits(logits, 16) || a.ld_logits % V || a.vocab % V;
+    return ragged ? launch_loss_nv<T, true>(a, logits, grad, nv, threads, cluster, n_sms, st) : launch_loss_nv<T, false>(a, logits, grad, nv, threads, cluster, n_sms, st);
 }
 
 bool overlaps_no(const sl_tensor_desc* tensors, int n) {

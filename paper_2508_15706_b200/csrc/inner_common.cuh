@@ -106,10 +106,10 @@ __device__ __forceinline__ V warp_sum(V x) {
     for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(kFullMask, x, o);
     return x;
 }
-__device__ __forceinline__ float warp_max(float x) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) x = fmaxf(x, __shfl_xor_sync(kFullMask, x, o));
-    return x;
+__device__ __forceinline__ float warp_max(float x) {  // NaN only where all are
+    float y;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+    return y;
 }
 
 inline bool fits(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) % (uintptr_t)bytes) == 0; }

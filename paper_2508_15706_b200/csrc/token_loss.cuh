@@ -97,7 +97,7 @@ __device__ __forceinline__ void block_join(float& m, float& s, float& sum, bool 
 
 // What a row comes to, from its maximum, sum and target.
 struct LossRow {
-    float m, s, sum, lse, scale;
+    float m, s, sum, scale;
     long long target;
     bool counts, inside, empty;
     __device__ __forceinline__ bool has_gradient() const { return counts && inside && !empty; }
@@ -109,8 +109,11 @@ struct LossRow {
     __device__ __forceinline__ void finish() {
         empty = m == -INFINITY && s == 0.0f;  // every logit is -inf
         scale = fabsf(m) < 1e30f ? kLog2e : 1.0f;
-        lse = empty ? -INFINITY : scale == 1.0f ? m + logf(s) : (m + log2f(s)) * kLn2;
     }
+    __device__ __forceinline__ float lse() const { return empty ? -INFINITY : scale == 1.0f ? m + logf(s) : (m + log2f(s)) * kLn2; }
+    // ... within 2^-21 of it or so: what the gradient's factor of p needs
+    __device__ __forceinline__ float near_lse() const { return scale == 1.0f ? m + __logf(s) : (m + __log2f(s)) * kLn2; }
+    __device__ __forceinline__ float factor(const LossArgs& a, float w) const { return __fdividef(a.z == 0.0f ? w : w * fmaf(2.0f * a.z, near_lse(), 1.0f), s); }
 };
 // 1 / (rows that count), or 1, times the caller's scale; the count comes from the kernel before
 __device__ __forceinline__ float row_weight(const LossArgs& a, int& valid) {
@@ -120,16 +123,17 @@ __device__ __forceinline__ float row_weight(const LossArgs& a, int& valid) {
 }
 __device__ __forceinline__ void write_row(const LossArgs& a, const LossRow& r, long long row, float xt) {
     float loss = 0.0f;
+    const float lse = r.lse();
     if (r.counts) {
         if (!r.inside) loss = __int_as_float(0x7FC00000);
         else if (r.empty) loss = INFINITY;
         else {
-            loss = r.lse - (1.0f - a.smoothing) * xt + a.z * r.lse * r.lse;
+            loss = lse - (1.0f - a.smoothing) * xt + a.z * lse * lse;
             if (a.smoothing != 0.0f) loss -= a.smoothing * (r.sum / (float)a.vocab);
         }
     }
     a.row_loss[row] = loss;
-    if (a.lse) a.lse[row] = r.lse;
+    if (a.lse) a.lse[row] = lse;
 }
 // The last of `callers` CTAs adds the rows' losses in a fixed order: thread by thread, then thread after thread.
 __device__ __forceinline__ void add_rows(const LossArgs& a, unsigned callers, float w, int valid) {
@@ -175,46 +179,56 @@ __device__ __forceinline__ void unpack(const unsigned (&w)[4], float2 (&f)[VEC /
 }
 
 // A CTA's part of a row.  The vector body begins at the row's first 16-byte boundary; the values before it belong to the first CTA
-// of the cluster, those behind it to the last, one per thread.
-template <class T, int VEC>
+// of the cluster, those behind it to the last, one per thread.  RAGGED: there may be such values, else every row is all vectors.
+template <class T, int VEC, bool RAGGED>
 struct LossPart {
-    const T* x;     // the row
-    int head, begin, vectors, tail;  // this CTA's vectors begin at x + head + begin * VEC; single values from x + tail on
-    __device__ __forceinline__ LossPart(const LossArgs& a, const T* logits, long long row, int rank, int cluster) {
-        x = logits + row * a.ld_logits;
-        head = (int)((16u - (unsigned)(reinterpret_cast<uintptr_t>(x) & 15u)) & 15u) / (int)sizeof(T);
-        if (head > a.vocab) head = a.vocab;
+    int head, begin, vectors, tail;  // this CTA's vectors begin at value head + begin * VEC of the row; single values from `tail` on
+    __device__ __forceinline__ LossPart(const LossArgs& a, const T* x, int rank, int cluster) {
+        head = RAGGED ? (int)((16u - (unsigned)(reinterpret_cast<uintptr_t>(x) & 15u)) & 15u) / (int)sizeof(T) : 0;
+        if (RAGGED && head > a.vocab) head = a.vocab;
         const int body = (a.vocab - head) / VEC, per = cluster == 1 ? body : (body + cluster - 1) / cluster;
         begin = rank * per;
         vectors = min(body, begin + per) - begin;
         tail = head + body * VEC;
     }
-    __device__ __forceinline__ long long base() const { return head + (long long)begin * VEC; }
-    __device__ __forceinline__ int before(int rank) const { return rank == 0 && (int)threadIdx.x < head ? (int)threadIdx.x : -1; }
+    __device__ __forceinline__ int base() const { return head + begin * VEC; }
+    __device__ __forceinline__ int before(int rank) const { return RAGGED && rank == 0 && (int)threadIdx.x < head ? (int)threadIdx.x : -1; }
     __device__ __forceinline__ int behind(const LossArgs& a, int rank, int cluster) const {
-        return rank == cluster - 1 && tail + (int)threadIdx.x < a.vocab ? tail + (int)threadIdx.x : -1;
+        return RAGGED && rank == cluster - 1 && tail + (int)threadIdx.x < a.vocab ? tail + (int)threadIdx.x : -1;
     }
 };
 
 constexpr int kLossStages = 3;
 
+__device__ __forceinline__ void shared_value(unsigned at, float& x) { asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(at)); }
+__device__ __forceinline__ void shared_value(unsigned at, bf16& x) {
+    unsigned short h;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(at));
+    x = __ushort_as_bfloat16(h);
+}
+
 // NV vectors of VEC values per thread; all but a thread's last one exist in every row (the launch sees to it).
-template <class T, int VEC, int NV>
+template <class T, int VEC, int NV, bool RAGGED>
 __global__ void __launch_bounds__(kLossThreads, NV * VEC <= 32 ? 2 : 1)
 loss_row_kernel(const LossArgs a, const T* logits, T* grad, int cluster) {
-    extern __shared__ __align__(16) char ring[];  // [stages][NV][threads] vectors
-    __shared__ float buf[2][3][32];
+    extern __shared__ __align__(16) char ring[];  // [stages][NV][threads] vectors, then [stages][threads] targets
+    __shared__ float buf[2][3][32], xts[2];
     __shared__ float mine[4];  // this CTA's maximum, sum of exponentials, sum: read by the cluster
     const int tid = threadIdx.x, threads = blockDim.x;
     const unsigned teams = gridDim.x / (unsigned)cluster;
     long long row = blockIdx.x / (unsigned)cluster;
     const int rank = (int)(blockIdx.x - (unsigned)row * (unsigned)cluster);
     const unsigned place = (unsigned)__cvta_generic_to_shared(ring) + (unsigned)tid * 16u, pitch = (unsigned)threads * 16u, stage_bytes = (unsigned)NV * pitch;
+    const unsigned target_place = (unsigned)__cvta_generic_to_shared(ring) + kLossStages * stage_bytes + (unsigned)tid * 8u, target_pitch = (unsigned)threads * 8u;
     long long coming = row;
-    auto fetch = [&](unsigned stage_at) {
+    // every thread copies its vectors and the target: what it reads afterwards is its own copy, nothing but that is waited for
+    auto fetch = [&](unsigned stage_at, unsigned stage) {
         if (coming < a.rows) {
-            const LossPart<T, VEC> p(a, logits, coming, rank, cluster);
-            const T* from = p.x + p.base() + tid * VEC;
+            if (a.target_bits == 64) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(target_place + stage * target_pitch), "l"(static_cast<const long long*>(a.targets) + coming) : "memory");
+            else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(target_place + stage * target_pitch), "l"(static_cast<const int*>(a.targets) + coming) : "memory");
+            const T* x = logits + coming * a.ld_logits;
+            const LossPart<T, VEC, RAGGED> p(a, x, rank, cluster);
+            const T* from = x + p.base() + tid * VEC;
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 if (i < NV - 1 || i * threads + tid < p.vectors)
@@ -223,32 +237,52 @@ loss_row_kernel(const LossArgs a, const T* logits, T* grad, int cluster) {
         coming += teams;
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    for (int k = 0; k < kLossStages - 1; ++k) fetch((unsigned)k * stage_bytes);
+    for (int k = 0; k < kLossStages - 1; ++k) fetch((unsigned)k * stage_bytes, (unsigned)k);
     float w = 0.0f;
     int valid = 0;
     bool weighed = false;
-    unsigned at = 0;
-    // targets are known two rows ahead and their logits one row ahead (long before a gradient may take their place), so that no warp
-    // waits for the one to ask for the other
-    const bool writer = rank == 0 && tid == 0;
-    auto target_at = [&](long long i) { return i < a.rows ? target_of(a, i) : -1ll; };
-    auto logit_at = [&](long long i, long long t) { return writer && i < a.rows && t >= 0 && t < a.vocab ? widen(logits[i * a.ld_logits + t]) : 0.0f; };
-    long long target = target_at(row), target_next = target_at(row + teams);
-    float xt = logit_at(row, target);
+    unsigned at = 0, stage = 0;
+    // single values of the next row, asked for a row ahead
+    float first = -INFINITY, last_one = -INFINITY, first_next = -INFINITY, last_next = -INFINITY;
+    auto singles = [&](long long i, float& front, float& back) {
+        if (!RAGGED || i >= a.rows) return;
+        const T* x = logits + i * a.ld_logits;
+        const LossPart<T, VEC, RAGGED> p(a, x, rank, cluster);
+        const int f = p.before(rank), b = p.behind(a, rank, cluster);
+        front = f >= 0 ? widen(x[f]) : -INFINITY;
+        back = b >= 0 ? widen(x[b]) : -INFINITY;
+    };
+    singles(row, first, last_one);
+    const float inv_threads = 1.0f / (float)threads;
+    float off_all = 0.0f;
     for (int turn = 0; row < a.rows; row += teams, turn ^= 1) {
-        fetch(at ? at - stage_bytes : (kLossStages - 1) * stage_bytes);
-        LossRow r;
-        r.aim(a, target);
-        const LossPart<T, VEC> part(a, logits, row, rank, cluster);
-        const float xt_next = logit_at(row + teams, target_next);
-        const long long target_then = target_at(row + 2ll * teams);
+        const unsigned behind_stage = stage ? stage - 1 : kLossStages - 1;
+        fetch(behind_stage * stage_bytes, behind_stage);
+        singles(row + teams, first_next, last_next);
+        const T* x = logits + row * a.ld_logits;
+        const LossPart<T, VEC, RAGGED> part(a, x, rank, cluster);
         const int before = part.before(rank), behind = part.behind(a, rank, cluster);
         const bool last_too = (NV - 1) * threads + tid < part.vectors;
         float m = -INFINITY, s, sum = 0.0f, ref;
         float2 e[NV][VEC / 2];
         asm volatile("cp.async.wait_group %0;" ::"n"(kLossStages - 1) : "memory");
+        long long its_target;
+        if (a.target_bits == 64) {
+            asm volatile("ld.shared.s64 %0, [%1];" : "=l"(its_target) : "r"(target_place + stage * target_pitch));
+        } else {
+            int t32;
+            asm volatile("ld.shared.s32 %0, [%1];" : "=r"(t32) : "r"(target_place + stage * target_pitch));
+            its_target = t32;
+        }
+        LossRow r;
+        r.aim(a, its_target);
+        // the target's place in this CTA's part, its vector there, whose it is; the CTA that has it writes the row's loss
+        const int t = r.counts && r.inside ? (int)r.target - part.base() : -1;
+        const bool in_body = t >= 0 && t < part.vectors * VEC;
+        const int tv = in_body ? t / VEC : 0, ti = (int)(((float)tv + 0.5f) * inv_threads), te = t - tv * VEC;
+        const bool owner = in_body && tid == tv - ti * threads;  // of the target: value te of its vector ti
+        const bool writes = r.counts && r.inside ? in_body || (rank == 0 && r.target < part.head) || (rank == cluster - 1 && r.target >= part.tail) : rank == 0;
         {
-            const float first = before >= 0 ? widen(part.x[before]) : -INFINITY, last_one = behind >= 0 ? widen(part.x[behind]) : -INFINITY;
             m = fmaxf(first, last_one);
             unsigned v[NV][4];
 #pragma unroll
@@ -256,6 +290,15 @@ loss_row_kernel(const LossArgs a, const T* logits, T* grad, int cluster) {
                 asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v[i][0]), "=r"(v[i][1]), "=r"(v[i][2]), "=r"(v[i][3]) : "r"(place + at + i * pitch));
                 if (i == NV - 1 && !last_too) v[i][0] = v[i][1] = v[i][2] = v[i][3] = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;  // -inf
                 m = fmaxf(m, top_of<T, VEC>(v[i]));
+            }
+            if (r.counts && r.inside) {
+                if (before == (int)r.target) xts[turn] = first;
+                if (behind == (int)r.target) xts[turn] = last_one;
+                if (owner) {
+                    T own;
+                    shared_value(place + at + (unsigned)ti * pitch + (unsigned)te * (unsigned)sizeof(T), own);
+                    xts[turn] = widen(own);
+                }
             }
             const float scale = loss_scale(m);
             ref = loss_offset(m);
@@ -305,29 +348,26 @@ loss_row_kernel(const LossArgs a, const T* logits, T* grad, int cluster) {
         r.finish();
         if (!weighed) {
             w = row_weight(a, valid);
+            off_all = w * a.smoothing / (float)a.vocab;
             weighed = true;
         }
-        if (writer) write_row(a, r, row, xt);
-        target = target_next, target_next = target_then, xt = xt_next;
-        at = at + stage_bytes == kLossStages * stage_bytes ? 0u : at + stage_bytes;
-        if (!grad) continue;
+        if (writes && tid == 0) write_row(a, r, row, xts[turn]);
         T* g = grad + row * a.ld_grad;
         T* gb = g + part.base() + tid * VEC;
-        if (r.has_gradient()) {
-            const float k = w * fmaf(2.0f * a.z, r.lse, 1.0f) / r.s, off = w * a.smoothing / (float)a.vocab, hit = w * (1.0f - a.smoothing);
+        if (!grad) {
+        } else if (r.has_gradient()) {
+            const float k = r.factor(a, w), off = off_all, hit = w * (1.0f - a.smoothing);
             const float2 k2 = both(k * exp2_fast(ref - r.m)), off2 = both(-off);             // (from the thread's maximum to the row's)
-            const int t = (int)r.target - (int)part.base();                                  // the target's place in this CTA's part
-            const int tv = t >= 0 && t < part.vectors * VEC ? t / VEC : -1, ti = tv - tid;    // ... and its vector, if it is one of this thread's
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 float2 q[VEC / 2];
 #pragma unroll
                 for (int j = 0; j < VEC / 2; ++j) q[j] = fma2(k2, e[i][j], off2);
-                if (tv >= 0 && ti == i * threads) {
+                if (owner && ti == i) {
 #pragma unroll
                     for (int j = 0; j < VEC / 2; ++j) {
-                        if (2 * j == t - tv * VEC) q[j].x -= hit;
-                        if (2 * j + 1 == t - tv * VEC) q[j].y -= hit;
+                        if (2 * j == te) q[j].x -= hit;
+                        if (2 * j + 1 == te) q[j].y -= hit;
                     }
                 }
                 if (i < NV - 1 || last_too) {
@@ -338,7 +378,7 @@ loss_row_kernel(const LossArgs a, const T* logits, T* grad, int cluster) {
                 }
             }
             auto one = [&](int i) {
-                const float d = fmaf(k, exp2_fast(fmaf(widen(part.x[i]), r.scale, -r.m)), -off);
+                const float d = fmaf(k, exp2_fast(fmaf(widen(x[i]), r.scale, -r.m)), -off);
                 g[i] = narrow<T>(i == (int)r.target ? d - hit : d);
             };
             if (before >= 0) one(before);
@@ -350,8 +390,11 @@ loss_row_kernel(const LossArgs a, const T* logits, T* grad, int cluster) {
             if (before >= 0) g[before] = narrow<T>(0.0f);
             if (behind >= 0) g[behind] = narrow<T>(0.0f);
         }
+        first = first_next, last_one = last_next;
+        stage = stage + 1 == kLossStages ? 0u : stage + 1;
+        at = stage * stage_bytes;
     }
-    if (rank == 0) add_rows(a, teams, w, valid);
+    add_rows(a, gridDim.x, w, valid);
 }
 
 // The row read twice: a running maximum and sum, then the gradient.
@@ -412,7 +455,7 @@ loss_stream_kernel(const LossArgs a, const T* logits, T* grad) {
     if (grad) {
         T* g = grad + row * a.ld_grad;
         const bool some = r.has_gradient();
-        const float k = some ? w * fmaf(2.0f * a.z, r.lse, 1.0f) / r.s : 0.0f, off = w * a.smoothing / (float)a.vocab, hit = w * (1.0f - a.smoothing);
+        const float k = some ? r.factor(a, w) : 0.0f, off = w * a.smoothing / (float)a.vocab, hit = w * (1.0f - a.smoothing);
         auto of = [&](float v, int i) {
             if (!some) return 0.0f;
             const float d = fmaf(k, exp2_fast(fmaf(v, r.scale, -r.m)), -off);
