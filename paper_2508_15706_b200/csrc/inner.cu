@@ -89,7 +89,7 @@ template <class T, int NV, bool RAGGED>
 sl_status launch_loss_rows(const LossArgs& a, const T* logits, T* grad, int threads, int cluster, int n_sms, cudaStream_t st) {
     constexpr int V = 16 / (int)sizeof(T);
     // as many CTAs as are resident: threads (by the launch bounds' registers) and shared memory
-    const size_t smem = (size_t)kLossStages * threads * (NV * 16 + 8);
+    const size_t smem = (size_t)kLossStages * threads * NV * 16;
     const long long ctas = std::max(1ll, std::min(32ll, std::min((NV * V <= 32 ? 1024ll : 512ll) / threads, 222ll * 1024 / ((long long)smem + 2048))));
     const long long teams = std::min((long long)a.rows, std::max(1ll, n_sms * ctas / cluster));
     const auto kern = loss_row_kernel<T, V, NV, RAGGED>;

@@ -199,6 +199,20 @@ struct LossPart {
 };
 
 constexpr int kLossStages = 3;
+constexpr unsigned kLossPolls = 1u << 22;  // of a wait for a copy; if one ever runs out, nothing more is asked or waited for, and the losses from there on are NaN
+
+__device__ __forceinline__ void bulk_expect(unsigned barrier, unsigned bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(barrier), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bulk_copy(unsigned to, const void* from, unsigned bytes, unsigned barrier) {
+    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from), "r"(bytes), "r"(barrier) : "memory");
+}
+__device__ __forceinline__ bool bulk_wait(unsigned barrier, unsigned phase) {
+    unsigned done = 0;
+    for (unsigned n = 0; !done && n < kLossPolls; ++n)
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(barrier), "r"(phase) : "memory");
+    return done != 0;
+}
 
 __device__ __forceinline__ void shared_value(unsigned at, float& x) { asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(at)); }
 __device__ __forceinline__ void shared_value(unsigned at, bf16& x) {
@@ -211,37 +225,38 @@ __device__ __forceinline__ void shared_value(unsigned at, bf16& x) {
 template <class T, int VEC, int NV, bool RAGGED>
 __global__ void __launch_bounds__(kLossThreads, NV * VEC <= 32 ? 2 : 1)
 loss_row_kernel(const LossArgs a, const T* logits, T* grad, int cluster) {
-    extern __shared__ __align__(16) char ring[];  // [stages][NV][threads] vectors, then [stages][threads] targets
+    extern __shared__ __align__(16) char ring[];  // [stages][NV * threads] vectors
+    __shared__ __align__(8) unsigned long long landed[kLossStages];
     __shared__ float buf[2][3][32], xts[2];
     __shared__ float mine[4];  // this CTA's maximum, sum of exponentials, sum: read by the cluster
     const int tid = threadIdx.x, threads = blockDim.x;
     const unsigned teams = gridDim.x / (unsigned)cluster;
     long long row = blockIdx.x / (unsigned)cluster;
     const int rank = (int)(blockIdx.x - (unsigned)row * (unsigned)cluster);
-    const unsigned place = (unsigned)__cvta_generic_to_shared(ring) + (unsigned)tid * 16u, pitch = (unsigned)threads * 16u, stage_bytes = (unsigned)NV * pitch;
-    const unsigned target_place = (unsigned)__cvta_generic_to_shared(ring) + kLossStages * stage_bytes + (unsigned)tid * 8u, target_pitch = (unsigned)threads * 8u;
-    long long coming = row;
-    // every thread copies its vectors and the target: what it reads afterwards is its own copy, nothing but that is waited for
-    auto fetch = [&](unsigned stage_at, unsigned stage) {
-        if (coming < a.rows) {
-            if (a.target_bits == 64) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(target_place + stage * target_pitch), "l"(static_cast<const long long*>(a.targets) + coming) : "memory");
-            else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(target_place + stage * target_pitch), "l"(static_cast<const int*>(a.targets) + coming) : "memory");
-            const T* x = logits + coming * a.ld_logits;
-            const LossPart<T, VEC, RAGGED> p(a, x, rank, cluster);
-            const T* from = x + p.base() + tid * VEC;
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (i < NV - 1 || i * threads + tid < p.vectors)
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(place + stage_at + i * pitch), "l"(from + i * threads * VEC) : "memory");
-        }
-        coming += teams;
-        asm volatile("cp.async.commit_group;" ::: "memory");
+    const unsigned ring_at = (unsigned)__cvta_generic_to_shared(ring), place = ring_at + (unsigned)tid * 16u, pitch = (unsigned)threads * 16u, stage_bytes = (unsigned)NV * pitch;
+    const unsigned landed_at = (unsigned)__cvta_generic_to_shared(landed);
+    // one thread asks for a CTA's whole part of a row in one copy
+    auto fetch = [&](long long i, unsigned stage) {
+        if (i >= a.rows) return;
+        const T* x = logits + i * a.ld_logits;
+        const LossPart<T, VEC, RAGGED> p(a, x, rank, cluster);
+        const unsigned bytes = (unsigned)p.vectors * 16u;
+        bulk_expect(landed_at + stage * 8u, bytes);
+        if (bytes) bulk_copy(ring_at + stage * stage_bytes, x + p.base(), bytes, landed_at + stage * 8u);
     };
-    for (int k = 0; k < kLossStages - 1; ++k) fetch((unsigned)k * stage_bytes, (unsigned)k);
+    if (tid == 0) {
+        for (int k = 0; k < kLossStages; ++k) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(landed_at + k * 8u) : "memory");
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        for (int k = 0; k < kLossStages; ++k) fetch(row + (long long)k * teams, (unsigned)k);
+    }
+    __syncthreads();
     float w = 0.0f;
     int valid = 0;
     bool weighed = false;
-    unsigned at = 0, stage = 0;
+    unsigned at = 0, stage = 0, phase = 0;
+    bool arrived = true;
+    auto target_at = [&](long long i) { return i < a.rows ? target_of(a, i) : -1ll; };
+    long long its_target = target_at(row);
     // single values of the next row, asked for a row ahead
     float first = -INFINITY, last_one = -INFINITY, first_next = -INFINITY, last_next = -INFINITY;
     auto singles = [&](long long i, float& front, float& back) {
@@ -256,8 +271,7 @@ loss_row_kernel(const LossArgs a, const T* logits, T* grad, int cluster) {
     const float inv_threads = 1.0f / (float)threads;
     float off_all = 0.0f;
     for (int turn = 0; row < a.rows; row += teams, turn ^= 1) {
-        const unsigned behind_stage = stage ? stage - 1 : kLossStages - 1;
-        fetch(behind_stage * stage_bytes, behind_stage);
+        const long long target_next = target_at(row + teams);
         singles(row + teams, first_next, last_next);
         const T* x = logits + row * a.ld_logits;
         const LossPart<T, VEC, RAGGED> part(a, x, rank, cluster);
@@ -265,15 +279,7 @@ loss_row_kernel(const LossArgs a, const T* logits, T* grad, int cluster) {
         const bool last_too = (NV - 1) * threads + tid < part.vectors;
         float m = -INFINITY, s, sum = 0.0f, ref;
         float2 e[NV][VEC / 2];
-        asm volatile("cp.async.wait_group %0;" ::"n"(kLossStages - 1) : "memory");
-        long long its_target;
-        if (a.target_bits == 64) {
-            asm volatile("ld.shared.s64 %0, [%1];" : "=l"(its_target) : "r"(target_place + stage * target_pitch));
-        } else {
-            int t32;
-            asm volatile("ld.shared.s32 %0, [%1];" : "=r"(t32) : "r"(target_place + stage * target_pitch));
-            its_target = t32;
-        }
+        arrived = arrived && bulk_wait(landed_at + stage * 8u, phase);
         LossRow r;
         r.aim(a, its_target);
         // the target's place in this CTA's part, its vector there, whose it is; the CTA that has it writes the row's loss
@@ -329,8 +335,11 @@ loss_row_kernel(const LossArgs a, const T* logits, T* grad, int cluster) {
             acc[0] = add2(acc[0], acc[1]);
             s += acc[0].x + acc[0].y;
             m *= scale;
+            if (!arrived) s = __int_as_float(0x7FC00000);
         }
         block_join(m, s, sum, a.smoothing != 0.0f, buf[turn]);
+        // (behind the barrier in there nobody reads this stage any more)
+        if (tid == 0 && arrived) fetch(row + (long long)kLossStages * teams, stage);
         r.m = m, r.s = s, r.sum = sum;
         if (cluster > 1) {
             namespace cg = cooperative_groups;
@@ -390,10 +399,13 @@ loss_row_kernel(const LossArgs a, const T* logits, T* grad, int cluster) {
             if (before >= 0) g[before] = narrow<T>(0.0f);
             if (behind >= 0) g[behind] = narrow<T>(0.0f);
         }
-        first = first_next, last_one = last_next;
+        first = first_next, last_one = last_next, its_target = target_next;
         stage = stage + 1 == kLossStages ? 0u : stage + 1;
+        if (stage == 0) phase ^= 1u;
         at = stage * stage_bytes;
     }
+    if (!arrived && tid == 0)  // (a last bounded wait for what may still be on its way into this CTA's memory)
+        for (int k = 0; k < kLossStages; ++k, stage = stage + 1 == kLossStages ? 0u : stage + 1, phase ^= stage == 0) bulk_wait(landed_at + stage * 8u, phase);
     add_rows(a, gridDim.x, w, valid);
 }
 
