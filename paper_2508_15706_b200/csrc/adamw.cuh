@@ -216,13 +216,12 @@ __device__ __forceinline__ void encode_moments(const float (&m)[kAdamVec], const
             tv = fmaxf(tv, finite_abs(v[i]));
         }
     }
+    // scale bytes grow with the largest value: the block's are the largest of its threads', found for both moments at once
+    unsigned scales = (unsigned)scale_byte_m(tm) | ((unsigned)scale_byte_v(tv) << 16);
 #pragma unroll
-    for (int o = 8; o; o >>= 1) {
-        tm = fmaxf(tm, __shfl_xor_sync(kFullMask, tm, o));
-        tv = fmaxf(tv, __shfl_xor_sync(kFullMask, tv, o));
-    }
-    bm = scale_byte_m(tm);
-    bv = scale_byte_v(tv);
+    for (int o = 8; o; o >>= 1) scales = __vmaxu2(scales, __shfl_xor_sync(kFullMask, scales, o));
+    bm = (int)(scales & 0xFFFFu);
+    bv = (int)(scales >> 16);
     const float im = inv_pow2_byte(bm), iv = inv_pow2_byte(bv);
     // (8 consecutive offsets that begin at a multiple of 4 may cross a multiple of 2^32)
     const unsigned base0 = lot_base(hash_key(seed, at), (unsigned)at), base1 = lot_base(hash_key(seed, at + 4), (unsigned)at + 4u);
@@ -331,22 +330,28 @@ struct AdamArgs {
 
 // The moments are formed by single-rounded operations in the order of the formula, so that the 8-bit codes do not depend
 // on how a compiler contracts them.  sqrt and reciprocal are the fast ones (2^-22 relative): theta's own rounding is coarser.
-// FLUSH: denormal operands of the two may count as 0, for a denominator of at least eps >= 1e-15 hides a sqrt(v) below 2^-63.
-template <bool FLUSH>
 __device__ __forceinline__ void adamw_element(float& p, float g, float& m, float& v, const AdamArgs& a, float c, float decay) {
     g = __fmul_rn(g, c);
     m = __fadd_rn(__fmul_rn(m, a.beta1), __fmul_rn(g, a.omb1));
     v = __fadd_rn(__fmul_rn(v, a.beta2), __fmul_rn(__fmul_rn(g, g), a.omb2));
-    float r, q;
-    if (FLUSH) {
-        asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(q) : "f"(fmaf(r, a.inv_sqrt_bc2, a.eps)));
-        q *= m;
-    } else {
-        asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
-        q = __fdividef(m, fmaf(r, a.inv_sqrt_bc2, a.eps));
-    }
-    p = fmaf(-a.step_size, q, fmaf(-decay, p, p));
+    float r;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+    p = fmaf(-a.step_size, __fdividef(m, fmaf(r, a.inv_sqrt_bc2, a.eps)), fmaf(-decay, p, p));
+}
+
+// Two elements at once, the moments operation by operation the same.  Denormal operands of sqrt and reciprocal count as 0: for
+// eps >= 1e-15, which hides a sqrt(v) below 2^-63.
+__device__ __forceinline__ void adamw_pair(float2& p, float2 g, float2& m, float2& v, const AdamArgs& a, float2 c, float2 decay) {
+    g = mul2(g, c);
+    m = add2(mul2(m, both(a.beta1)), mul2(g, both(a.omb1)));
+    v = add2(mul2(v, both(a.beta2)), mul2(mul2(g, g), both(a.omb2)));
+    float2 r, q;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(v.x));
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(v.y));
+    r = fma2(r, both(a.inv_sqrt_bc2), both(a.eps));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(q.x) : "f"(r.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(q.y) : "f"(r.y));
+    p = fma2(both(-a.step_size), mul2(q, m), fma2(decay, p, p));  // decay: -lr * weight decay
 }
 
 // What a thread reads for its 8 elements.
@@ -391,7 +396,8 @@ adamw_step_kernel(const AdamTile* __restrict__ tiles, const float* __restrict__ 
     const G* grad = static_cast<const G*>(a.grad) + tile.base;
     const float decay = a.lr * weight_decay[tile.tensor];
     constexpr int kIters = kAdamTile / (kAdamThreads * kAdamVec);
-    // everything that does not depend on the norm is fetched first, all iterations at once where that is few registers
+    // everything that does not depend on the norm is fetched first, both iterations at once where that is few bytes: 160 a thread
+    // (one at a time with a CTA more per SM: 1304 us for a step of 200 M elements and its read-out, 1103 this way)
     constexpr int kAhead = BITS == 8 ? kIters : 1;
     AdamLoads<P, G, BITS, A8> in[kAhead];
 #pragma unroll
@@ -412,10 +418,14 @@ adamw_step_kernel(const AdamTile* __restrict__ tiles, const float* __restrict__ 
         for (int j = 0; j < kAdamVec; ++j) p[j] = x.p[j];
         if (a.eps >= 1e-15f) {
 #pragma unroll
-            for (int j = 0; j < kAdamVec; ++j) adamw_element<true>(p[j], x.g[j], m[j], v[j], a, c, decay);
+            for (int j = 0; j < kAdamVec; j += 2) {
+                float2 pp = make_float2(p[j], p[j + 1]), mm = make_float2(m[j], m[j + 1]), vv = make_float2(v[j], v[j + 1]);
+                adamw_pair(pp, make_float2(x.g[j], x.g[j + 1]), mm, vv, a, both(c), both(-decay));
+                p[j] = pp.x, p[j + 1] = pp.y, m[j] = mm.x, m[j + 1] = mm.y, v[j] = vv.x, v[j + 1] = vv.y;
+            }
         } else {
 #pragma unroll
-            for (int j = 0; j < kAdamVec; ++j) adamw_element<false>(p[j], x.g[j], m[j], v[j], a, c, decay);
+            for (int j = 0; j < kAdamVec; ++j) adamw_element(p[j], x.g[j], m[j], v[j], a, c, decay);
         }
         store_some<P, A8>(theta + i, n, p);
         if (a.copy) store_some<bf16, A8>(a.copy + tile.base + i, n, p);
@@ -442,39 +452,69 @@ adamw_step_kernel(const AdamTile* __restrict__ tiles, const float* __restrict__ 
     }
 }
 
-// WRITE: fp32 moments -> codes and scales; else codes and scales -> fp32 moments.
-template <bool WRITE, bool A8>
+// fp32 moments -> codes and scales.
+template <bool A8>
 __global__ void __launch_bounds__(kAdamThreads)
-adamw_state_kernel(const AdamTile* __restrict__ tiles, float* m32, float* v32, uint8_t* m8, uint8_t* v8, uint8_t* scales, long long blocks,
-                   unsigned seed) {
+adamw_write_kernel(const AdamTile* __restrict__ tiles, const float* __restrict__ m32, const float* __restrict__ v32, uint8_t* m8, uint8_t* v8, uint8_t* scales,
+                   long long blocks, unsigned seed) {
     const AdamTile tile = tiles[blockIdx.x];
     const int tid = threadIdx.x;
-    constexpr int kIters = kAdamTile / (kAdamThreads * kAdamVec);
 #pragma unroll
-    for (int it = 0; it < kIters; ++it) {
+    for (int it = 0; it < kAdamTile / (kAdamThreads * kAdamVec); ++it) {
         const int i = (it * kAdamThreads + tid) * kAdamVec;
         if ((it * kAdamThreads + (tid & ~31)) * kAdamVec >= tile.len) return;  // whole warps only
         const int n = tile.len - i;
         const long long blk = tile.block0 + i / kAdamBlock;
         float m[kAdamVec], v[kAdamVec];
-        if (WRITE) {
-            load_some<float, A8>(m32 + tile.base + i, n, m);
-            load_some<float, A8>(v32 + tile.base + i, n, v);
-            uint2 cm, cv;
-            int bm, bv;
-            encode_moments<true>(m, v, seed, (unsigned long long)(tile.base + i), cm, cv, bm, bv);
-            store_codes<A8>(m8 + tile.base + i, n, cm);
-            store_codes<A8>(v8 + tile.base + i, n, cv);
-            if (n > 0 && (tid & 15) == 0) {
-                scales[blk] = (uint8_t)bm;
-                scales[blocks + blk] = (uint8_t)bv;
+        load_some<float, A8>(m32 + tile.base + i, n, m);
+        load_some<float, A8>(v32 + tile.base + i, n, v);
+        uint2 cm, cv;
+        int bm, bv;
+        encode_moments<true>(m, v, seed, (unsigned long long)(tile.base + i), cm, cv, bm, bv);
+        store_codes<A8>(m8 + tile.base + i, n, cm);
+        store_codes<A8>(v8 + tile.base + i, n, cv);
+        if (n > 0 && (tid & 15) == 0) {
+            scales[blk] = (uint8_t)bm;
+            scales[blocks + blk] = (uint8_t)bv;
+        }
+    }
+}
+
+// Codes and scales -> fp32 moments.  Mostly stores: 4 elements per thread, so that a warp's store fills whole sectors (8 per thread,
+// two stores of half sectors: 70 us more for 200 M elements).
+__global__ void __launch_bounds__(kAdamThreads)
+adamw_read_kernel(const AdamTile* __restrict__ tiles, float* m32, float* v32, const uint8_t* m8, const uint8_t* v8, const uint8_t* scales,
+                  long long blocks) {
+    constexpr int kIters = kAdamTile / (kAdamThreads * 4);
+    const AdamTile tile = tiles[blockIdx.x];
+    unsigned wm[kIters], wv[kIters];
+    int bm[kIters], bv[kIters];
+#pragma unroll
+    for (int it = 0; it < kIters; ++it) {
+        const int i = (it * kAdamThreads + (int)threadIdx.x) * 4;
+        if (i + 4 <= tile.len) {
+            const long long blk = tile.block0 + i / kAdamBlock;
+            wm[it] = __ldcs(reinterpret_cast<const unsigned*>(m8 + tile.base + i));
+            wv[it] = __ldcs(reinterpret_cast<const unsigned*>(v8 + tile.base + i));
+            bm[it] = scales[blk];
+            bv[it] = scales[blocks + blk];
+        }
+    }
+#pragma unroll
+    for (int it = 0; it < kIters; ++it) {
+        const int i = (it * kAdamThreads + (int)threadIdx.x) * 4;
+        if (i + 4 <= tile.len) {
+            const float sm = pow2_byte(bm[it]), sv = pow2_byte(bv[it]);
+            const float2 a = value_m2(wm[it] & 0xFFFFu), b = value_m2(wm[it] >> 16);
+            __stcs(reinterpret_cast<float4*>(m32 + tile.base + i), make_float4(a.x * sm, a.y * sm, b.x * sm, b.y * sm));
+            __stcs(reinterpret_cast<float4*>(v32 + tile.base + i),
+                   make_float4(value_v(wv[it] & 255u) * sv, value_v((wv[it] >> 8) & 255u) * sv, value_v((wv[it] >> 16) & 255u) * sv, value_v(wv[it] >> 24) * sv));
+        } else {
+            for (int j = i; j < tile.len; ++j) {
+                const long long blk = tile.block0 + j / kAdamBlock;
+                m32[tile.base + j] = value_m2(m8[tile.base + j]).x * pow2_byte(scales[blk]);
+                v32[tile.base + j] = value_v(v8[tile.base + j]) * pow2_byte(scales[blocks + blk]);
             }
-        } else if (n > 0) {
-            const uint2 wm = load_codes<A8>(m8 + tile.base + i, n), wv = load_codes<A8>(v8 + tile.base + i, n);
-            values_m(wm, pow2_byte(scales[blk]), m);
-            values_v(wv, pow2_byte(scales[blocks + blk]), v);
-            store_some<float, A8>(m32 + tile.base + i, n, m);
-            store_some<float, A8>(v32 + tile.base + i, n, v);
         }
     }
 }

@@ -84,30 +84,11 @@ __device__ __forceinline__ int norm_pieces(int cols) {
     return n;
 }
 
-template <int BYTES>
-__device__ __forceinline__ void copy_async(unsigned shared, const void* global) {
-    if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(shared), "l"(global) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(shared), "l"(global), "n"(BYTES) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void copy_wait(int behind) {  // all but the `behind` last groups have landed, for this thread
     if (behind == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
     else if (behind == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
     else asm volatile("cp.async.wait_group 3;" ::: "memory");
 }
-template <int BYTES>
-__device__ __forceinline__ void shared_load(unsigned at, void* to) {
-    unsigned* w = static_cast<unsigned*>(to);
-    if (BYTES == 16) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at));
-    else if (BYTES == 8) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at));
-    else if (BYTES == 4) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(at));
-    else {
-        unsigned short h;
-        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(at));
-        *static_cast<unsigned short*>(to) = h;
-    }
-}
-
 // One matrix as a thread sees it.  RING: a ring of rows in shared memory that the thread fills for itself, asynchronously and rows
 // ahead (a piece is read by the thread that copied it, so nothing is waited for but the copy); places of absent matrices and of
 // columns beyond the row's end are zeroed once.  Else (many columns per thread): global memory.

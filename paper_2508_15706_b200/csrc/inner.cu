@@ -316,9 +316,11 @@ static sl_status adamw_state(sl_adamw* c, bool write, float* m32, float* v32, ui
     }
     DeviceGuard guard(c->device);
     if (!guard.ok) return SL_ERR_CUDA;
-    auto kern = write ? (c->aligned8 ? adamw_state_kernel<true, true> : adamw_state_kernel<true, false>)
-                      : (c->aligned8 ? adamw_state_kernel<false, true> : adamw_state_kernel<false, false>);
-    kern<<<(unsigned)c->n_tiles, kAdamThreads, 0, static_cast<cudaStream_t>(stream)>>>(c->d_tiles, m32, v32, m8, v8, scales, c->blocks, seed);
+    const unsigned grid = (unsigned)c->n_tiles;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (!write) adamw_read_kernel<<<grid, kAdamThreads, 0, st>>>(c->d_tiles, m32, v32, m8, v8, scales, c->blocks);
+    else if (c->aligned8) adamw_write_kernel<true><<<grid, kAdamThreads, 0, st>>>(c->d_tiles, m32, v32, m8, v8, scales, c->blocks, seed);
+    else adamw_write_kernel<false><<<grid, kAdamThreads, 0, st>>>(c->d_tiles, m32, v32, m8, v8, scales, c->blocks, seed);
     SL_CUDA(cudaGetLastError());
     return SL_OK;
 }
