@@ -17,6 +17,7 @@ constexpr int kAdamThreads = 256;
 constexpr int kAdamVec = 8;       // consecutive elements of a thread
 constexpr int kAdamBlock = 128;   // elements under one scale of an 8-bit moment: 16 threads
 constexpr int kAdamMaxParts = 2048;
+constexpr int kAdamNormCtas = 8;  // of the norm pass per SM, all resident
 
 struct AdamTile {
     long long base;    // element offset in the flat buffers
@@ -241,17 +242,41 @@ __device__ __forceinline__ void encode_moments(const float (&m)[kAdamVec], const
     cv.y = __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410);
 }
 
+constexpr double kAdamTwo896 = 5.2829453113566525e269;  // 2^896
+
+// acc + 2^896 small gains the squares of 8 values, each exact.  A conversion to fp64 runs at 16 per SM and clock, too few for
+// bfloat16 at the memory's rate; but a bfloat16's square is exact in fp32, with zeros in the 8 lowest bits, and the bits of a fp32
+// shifted right by 3 are the upper word of the fp64 2^-896 times as large.  What that does not hold for (squares that overflow
+// or come near underflow) is converted.
+template <class G>
+__device__ __forceinline__ void add_squares(const float (&f)[kAdamVec], double& acc, double& small) {
+    if (sizeof(G) == 2) {
+        unsigned top = 0u;
+#pragma unroll
+        for (int j = 0; j < kAdamVec; ++j) top = max(top, __float_as_uint(f[j]) & 0x7FFFFFFFu);
+        if (top - 0x30000000u < 0x5F000000u - 0x30000000u) {  // the largest is in 2^-31 .. 2^63: a square that underflows beside it is nothing
+            double s[2] = {0.0, 0.0};
+#pragma unroll
+            for (int j = 0; j < kAdamVec; ++j) s[j & 1] += __hiloint2double((int)(__float_as_uint(f[j] * f[j]) >> 3), 0);
+            small += s[0] + s[1];
+            return;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < kAdamVec; ++j) acc = fma((double)f[j], (double)f[j], acc);
+}
+
 // Sum of squares of the gradient in fp64: every CTA leaves one partial sum, the last one to finish adds them in index
 // order and turns the norm into the coefficient of the update.  The assignment of tiles to CTAs is fixed, so is the sum.
 template <class G, bool A8>
-__global__ void __launch_bounds__(kAdamThreads)
+__global__ void __launch_bounds__(kAdamThreads, kAdamNormCtas)
 adamw_norm_kernel(const AdamTile* __restrict__ tiles, long long n_tiles, const G* __restrict__ grad, double grad_scale, double max_norm,
                   double* __restrict__ parts, AdamClip* __restrict__ clip, float* __restrict__ norm_out) {
     __shared__ double warp_part[kAdamThreads / 32];
     __shared__ int last;
     const int tid = threadIdx.x;
     cudaTriggerProgrammaticLaunchCompletion();  // the update's CTAs may come and load their operands
-    double acc = 0.0;
+    double acc = 0.0, small = 0.0;
     AdamTile next = tiles[blockIdx.x];
     for (long long t = blockIdx.x; t < n_tiles; t += gridDim.x) {
         const AdamTile tile = next;
@@ -268,18 +293,10 @@ adamw_norm_kernel(const AdamTile* __restrict__ tiles, long long n_tiles, const G
         }
 #pragma unroll
         for (int it = 0; it < kIters; ++it) {
-            if (sizeof(G) == 4) {
-#pragma unroll
-                for (int j = 0; j < kAdamVec; ++j) acc = fma((double)f[it][j], (double)f[it][j], acc);
-            } else {
-                // a bfloat16 square is exact in fp32 and four of them lose at most 2^-23 together: one conversion (of 16 per
-                // SM and clock) in place of four
-#pragma unroll
-                for (int j = 0; j < kAdamVec; j += 4)
-                    acc += (double)fmaf(f[it][j], f[it][j], fmaf(f[it][j + 1], f[it][j + 1], fmaf(f[it][j + 2], f[it][j + 2], f[it][j + 3] * f[it][j + 3])));
-            }
+            add_squares<G>(f[it], acc, small);
         }
     }
+    acc = fma(small, kAdamTwo896, acc);
     acc = warp_sum(acc);
     if ((tid & 31) == 0) warp_part[tid >> 5] = acc;
     __syncthreads();
@@ -329,22 +346,23 @@ struct AdamArgs {
 };
 
 // The moments are formed by single-rounded operations in the order of the formula, so that the 8-bit codes do not depend
-// on how a compiler contracts them.  sqrt and reciprocal are the fast ones (2^-22 relative): theta's own rounding is coarser.
-__device__ __forceinline__ void adamw_element(float& p, float g, float& m, float& v, const AdamArgs& a, float c, float decay) {
+// on how a compiler contracts them.  (Not by the paired ones: their products and sums are contracted, explicit rounding or not.)
+__device__ __forceinline__ void adamw_moments(float g, float& m, float& v, const AdamArgs& a, float c) {
     g = __fmul_rn(g, c);
     m = __fadd_rn(__fmul_rn(m, a.beta1), __fmul_rn(g, a.omb1));
     v = __fadd_rn(__fmul_rn(v, a.beta2), __fmul_rn(__fmul_rn(g, g), a.omb2));
+}
+// sqrt and reciprocal are the fast ones (2^-22 relative): theta's own rounding is coarser.
+__device__ __forceinline__ void adamw_element(float& p, float g, float& m, float& v, const AdamArgs& a, float c, float decay) {
+    adamw_moments(g, m, v, a, c);
     float r;
     asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
     p = fmaf(-a.step_size, __fdividef(m, fmaf(r, a.inv_sqrt_bc2, a.eps)), fmaf(-decay, p, p));
 }
-
-// Two elements at once, the moments operation by operation the same.  Denormal operands of sqrt and reciprocal count as 0: for
-// eps >= 1e-15, which hides a sqrt(v) below 2^-63.
-__device__ __forceinline__ void adamw_pair(float2& p, float2 g, float2& m, float2& v, const AdamArgs& a, float2 c, float2 decay) {
-    g = mul2(g, c);
-    m = add2(mul2(m, both(a.beta1)), mul2(g, both(a.omb1)));
-    v = add2(mul2(v, both(a.beta2)), mul2(mul2(g, g), both(a.omb2)));
+// ... for eps >= 1e-15, which hides a sqrt(v) below 2^-63: denormal operands of sqrt and reciprocal may count as 0.
+__device__ __forceinline__ void adamw_pair(float2& p, float2 g, float2& m, float2& v, const AdamArgs& a, float c, float2 decay) {
+    adamw_moments(g.x, m.x, v.x, a, c);
+    adamw_moments(g.y, m.y, v.y, a, c);
     float2 r, q;
     asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(v.x));
     asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(v.y));
@@ -420,7 +438,7 @@ adamw_step_kernel(const AdamTile* __restrict__ tiles, const float* __restrict__ 
 #pragma unroll
             for (int j = 0; j < kAdamVec; j += 2) {
                 float2 pp = make_float2(p[j], p[j + 1]), mm = make_float2(m[j], m[j + 1]), vv = make_float2(v[j], v[j + 1]);
-                adamw_pair(pp, make_float2(x.g[j], x.g[j + 1]), mm, vv, a, both(c), both(-decay));
+                adamw_pair(pp, make_float2(x.g[j], x.g[j + 1]), mm, vv, a, c, both(-decay));
                 p[j] = pp.x, p[j + 1] = pp.y, m[j] = mm.x, m[j + 1] = mm.y, v[j] = vv.x, v[j + 1] = vv.y;
             }
         } else {

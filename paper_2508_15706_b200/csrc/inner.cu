@@ -45,7 +45,7 @@ namespace {
 // ---- AdamW
 template <class G>
 sl_status launch_adamw_norm(const sl_adamw* c, const void* grad, double grad_scale, float* norm, cudaStream_t st) {
-    const long long want = c->n_tiles, most = (long long)c->n_sms * 8;
+    const long long want = c->n_tiles, most = (long long)c->n_sms * kAdamNormCtas;
     const unsigned grid = (unsigned)std::min(std::min(want, most), (long long)kAdamMaxParts);
     auto kern = c->aligned8 ? adamw_norm_kernel<G, true> : adamw_norm_kernel<G, false>;
     kern<<<grid, kAdamThreads, 0, st>>>(c->d_tiles, c->n_tiles, static_cast<const G*>(grad), grad_scale, c->cfg.max_norm, c->d_parts, c->d_clip, norm);

@@ -164,6 +164,69 @@ def test_steps_with_8_bit_moments(align, gap, param_dtype, grad_dtype):
     assert torch.all(m8[outside] == 0x55) and torch.all(v8[outside] == 0xAA)
 
 
+@pytest.mark.parametrize("grad_dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("max_norm", [0.0, 0.05])
+def test_8_bit_codes_bit_for_bit(grad_dtype, max_norm):
+    """A million elements against the formula in fp32, each operation rounded once, in the order the header gives them: codes and
+    scales equal, the norm the rounded fp64 sum."""
+    from paper_2508_15706_b200.inner import AdamW
+    n = 1 << 20
+    opt = AdamW([(1024, 1024)], state_bits=8, max_norm=max_norm, grad_dtype=grad_dtype)
+    g = torch.Generator(device="cuda").manual_seed(31)
+    theta = torch.randn(n, generator=g, device="cuda")
+    state, norm = opt.new_state(), torch.zeros(1, device="cuda")
+    m32, v32 = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    f = np.float32
+    for t in range(1, 4):
+        grad = (torch.randn(n, generator=g, device="cuda") * torch.exp(torch.randn(n, generator=g, device="cuda")) * 1e-3).to(grad_dtype)
+        opt.read_state(*state, m32, v32)
+        m0, v0, gr = m32.cpu().numpy(), v32.cpu().numpy(), grad.float().cpu().numpy()
+        opt.step(theta, grad, *state, step=t, lr=1e-3, seed=t, norm=norm)
+        size = math.sqrt(np.sum(gr.astype(np.float64) ** 2))
+        assert norm.item() == f(size)
+        gs = gr * f(min(1.0, max_norm / (size + 1e-6)) if max_norm else 1.0)
+        m = m0 * f(0.9) + gs * f(1 - 0.9)
+        v = v0 * f(0.95) + (gs * gs) * f(1 - 0.95)
+        top_m = np.abs(m).reshape(-1, 128).max(1).view(np.uint32)
+        top_v = v.reshape(-1, 128).max(1).view(np.uint32)
+        em = np.maximum((top_m >> 23).astype(np.int64) + ((top_m & 0x7FFFFF) > 0x600000) - 8, 1)
+        ev = np.clip((top_v >> 23).astype(np.int64) + ((top_v & 0x7FFFFF) > 0x780000), 1, 254)
+        assert np.array_equal(state[2].cpu().numpy(), np.stack([em, ev]).astype(np.uint8))
+        scaled = torch.from_numpy((m.reshape(-1, 128) * np.exp2(127.0 - em)[:, None].astype(f)).reshape(-1))
+        assert torch.equal(state[0].cpu(), scaled.to(torch.float8_e4m3fn).view(torch.uint8))
+        x = (v.reshape(-1, 128) * np.exp2(127.0 - ev)[:, None].astype(f)).reshape(-1)
+        i = np.arange(n, dtype=np.uint64) ^ np.uint64(mix(t))
+        lot = i ^ (i >> np.uint64(16))
+        lot = lot * np.uint64(0x7FEB352D) & np.uint64(0xFFFFFFFF)
+        lot ^= lot >> np.uint64(15)
+        lot = lot * np.uint64(0x846CA68B) & np.uint64(0xFFFFFFFF)
+        lot = ((lot ^ (lot >> np.uint64(16))) >> np.uint64(13)).astype(np.int64)
+        code = np.clip(((x.view(np.uint32).astype(np.int64) + lot) >> 19) - 1792, 1, 255)
+        assert np.array_equal(state[1].cpu().numpy(), np.where(x == 0, 0, code).astype(np.uint8))
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-15, 1.0, 1e15, 1e25])
+@pytest.mark.parametrize("grad_dtype", [torch.float32, torch.bfloat16])
+def test_norm_over_the_whole_range(scale, grad_dtype):
+    """Zeros, tiny and huge gradients beside each other: the fp64 sum of exact squares, rounded once."""
+    from paper_2508_15706_b200.inner import AdamW
+    n = 70001
+    opt = AdamW([(1, n)], max_norm=1.0, grad_dtype=grad_dtype)
+    g = torch.Generator(device="cuda").manual_seed(8)
+    norm, theta = torch.zeros(1, device="cuda"), torch.zeros(n, device="cuda")
+    for mixed in (False, True):
+        grad = torch.randn(n, generator=g, device="cuda") * scale
+        if mixed:
+            grad[::3] = 0.0
+            grad[1::3] *= 1e-9
+        grad = grad.to(grad_dtype)
+        opt.step(theta, grad, *opt.new_state()[:2], step=1, lr=0.0, norm=norm)
+        want = grad.double().square().sum().sqrt().item()
+        assert norm.item() == np.float32(want)
+    opt.step(theta, torch.zeros_like(grad), *opt.new_state()[:2], step=1, lr=0.0, norm=norm)
+    assert norm.item() == 0.0
+
+
 def test_8_bit_state_round_trip_and_ranges():
     """Blocks of zeros, denormals, huge values, one outlier, infinities and NaN; a state that was read back keeps its values
     when it is written again (they are code points: nothing to round)."""
