@@ -358,7 +358,8 @@ def _heads(x, out, dev, batch, seq, head_dim, dtype, what):
 class _Turn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, rope, positions, first):
-        ctx.rope, ctx.positions, ctx.first = rope, positions, first
+        ctx.rope, ctx.first = rope, first
+        ctx.save_for_backward(positions)
         out_q, out_k = torch.empty(q.shape, dtype=q.dtype, device=q.device), torch.empty(k.shape, dtype=k.dtype, device=k.device)
         rope.apply(q, k, positions, first=first, out_q=out_q, out_k=out_k)
         return out_q, out_k
@@ -367,7 +368,7 @@ class _Turn(torch.autograd.Function):
     def backward(ctx, dq, dk):
         out_q, out_k = torch.empty(dq.shape, dtype=dq.dtype, device=dq.device), torch.empty(dk.shape, dtype=dk.dtype, device=dk.device)
         dq, dk = (t if t.stride(-1) == 1 else t.contiguous() for t in (dq, dk))
-        ctx.rope.apply(dq, dk, ctx.positions, first=ctx.first, inverse=True, out_q=out_q, out_k=out_k)
+        ctx.rope.apply(dq, dk, ctx.saved_tensors[0], first=ctx.first, inverse=True, out_q=out_q, out_k=out_k)
         return out_q, out_k, None, None, None
 
 
