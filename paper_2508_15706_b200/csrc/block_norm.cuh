@@ -95,9 +95,11 @@ __device__ __forceinline__ void copy_wait(int behind) {  // all but the `behind`
 template <class T, int VEC, int NV, bool RING>
 struct NormMatrix {
     typedef Pack<T, VEC> Piece;
+    static constexpr bool kLate = Piece::kBytes < 4;  // too small for an asynchronous copy: in registers for a row, then into the ring
     const T* row;    // the thread's first column in the row to be copied (RING) or used next; null: absent
     long long step;  // elements from one of the CTA's rows to the next
     unsigned place;  // shared address of its first piece in the ring's first row
+    unsigned short held[kLate ? NV : 1];
     __device__ __forceinline__ NormMatrix(const void* base, long long ld, long long first, long long stride, const char* ring, int array) {
         row = base ? static_cast<const T*>(base) + first * ld + norm_column<VEC>(0) : nullptr;
         step = base ? stride * ld : 0;
@@ -114,20 +116,25 @@ struct NormMatrix {
                     for (int j = 0; j < VEC * (int)sizeof(T); j += 2)
                         asm volatile("st.shared.u16 [%0], %1;" ::"r"(place + (unsigned)s * stage_bytes + pitch(i) + (unsigned)j), "h"((unsigned short)0) : "memory");
     }
+    // the next row on its way to stage_at (kLate: into `held`, which settle() then puts there)
     __device__ __forceinline__ void fetch(unsigned stage_at, int pieces) {
         if (!row) return;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if (i < pieces) {
-                if constexpr (Piece::kBytes >= 4) {
-                    copy_async<Piece::kBytes>(place + stage_at + pitch(i), row + offset(i));
-                } else {
-                    const unsigned short h = *reinterpret_cast<const unsigned short*>(row + offset(i));
-                    asm volatile("st.shared.u16 [%0], %1;" ::"r"(place + stage_at + pitch(i)), "h"(h) : "memory");
-                }
+                if constexpr (kLate) held[i] = *reinterpret_cast<const unsigned short*>(row + offset(i));
+                else copy_async<Piece::kBytes>(place + stage_at + pitch(i), row + offset(i));
             }
         }
         row += step;
+    }
+    __device__ __forceinline__ void settle(unsigned held_at, int pieces) const {
+        if constexpr (kLate) {
+            if (!row) return;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (i < pieces) asm volatile("st.shared.u16 [%0], %1;" ::"r"(place + held_at + pitch(i)), "h"(held[i]) : "memory");
+        }
     }
     // all of the thread's values as pairs, 0 beyond the row's end or without a matrix
     __device__ __forceinline__ void get(unsigned stage_at, int pieces, float2 (&f)[NV * VEC / 2]) const {
@@ -210,6 +217,7 @@ __global__ void __launch_bounds__(NV* VEC <= 8 ? 1024 : NV * VEC <= 16 ? 640 : k
 norm_forward_kernel(const NormArgs a) {
     constexpr bool kFew = kNormFew<VEC, NV>;
     constexpr int P = NV * VEC / 2;
+    constexpr bool kLate = VEC * sizeof(T) < 4;
     extern __shared__ __align__(16) char ring[];
     __shared__ float sums[2][16];
     clear_sums(sums[0], 32);
@@ -222,6 +230,12 @@ norm_forward_kernel(const NormArgs a) {
     const unsigned stage_bytes = (unsigned)((FULL ? 3 : 2) * NV * VEC * sizeof(T) * blockDim.x * blockDim.y), ring_bytes = (unsigned)a.stages * stage_bytes;
     long long coming = row;  // the row to be copied next
     auto fetch = [&](unsigned stage_at) {
+        if (kLate && coming > row && coming - stride < a.rows) {  // the row before, held until now
+            const unsigned held_at = stage_at ? stage_at - stage_bytes : ring_bytes - stage_bytes;
+            mx.settle(held_at, pieces);
+            mb.settle(held_at, pieces);
+            if (FULL) mg.settle(held_at, pieces);
+        }
         if (coming < a.rows) {
             mx.fetch(stage_at, pieces);
             mb.fetch(stage_at, pieces);
@@ -304,6 +318,7 @@ __global__ void __launch_bounds__(NV* VEC <= 8 ? 640 : kNormMaxThreads)
 norm_backward_kernel(const NormArgs a) {
     constexpr bool kFew = kNormFewBackward<VEC, NV>;
     constexpr int P = NV * VEC / 2;
+    constexpr bool kLate = VEC * sizeof(T) < 4;
     extern __shared__ __align__(16) char ring[];  // afterwards [2][cols] column sums, only where blockDim.y > 1
     __shared__ float sums[2][3 * 16];
     clear_sums(sums[0], 2 * 3 * 16);
@@ -317,6 +332,14 @@ norm_backward_kernel(const NormArgs a) {
     const unsigned stage_bytes = (unsigned)((FULL ? 5 : 4) * NV * VEC * sizeof(T) * blockDim.x * blockDim.y), ring_bytes = (unsigned)a.stages * stage_bytes;
     long long coming = row;
     auto fetch = [&](unsigned stage_at) {
+        if (kLate && coming > row && coming - stride < a.rows) {  // the row before, held until now
+            const unsigned held_at = stage_at ? stage_at - stage_bytes : ring_bytes - stage_bytes;
+            mdy.settle(held_at, pieces);
+            mdh.settle(held_at, pieces);
+            my.settle(held_at, pieces);
+            mb.settle(held_at, pieces);
+            if (FULL) mg.settle(held_at, pieces);
+        }
         if (coming < a.rows) {
             mdy.fetch(stage_at, pieces);
             mdh.fetch(stage_at, pieces);
@@ -475,13 +498,19 @@ __device__ __forceinline__ void team_sums(float (&s)[K], float* buf) {
     }
 }
 
-// 8 values of T as 16-byte chunks, chunk h of all threads together (no bank conflicts)
+// A piece is 8 values: one 16-byte chunk of bfloat16, or two of fp32 that lie a team apart, so that every access of a warp is one
+// contiguous stretch.  Chunk k of thread x begins at column (k * threads + x) * (values of a chunk).
 template <class T>
 struct Chunks {
-    static constexpr int kNum = 8 * (int)sizeof(T) / 16;
+    static constexpr int kNum = 8 * (int)sizeof(T) / 16, kValues = 16 / (int)sizeof(T);
 };
+template <class T, int NV, int TEAM>
+__device__ __forceinline__ int team_chunks(int cols) {  // of this thread that the row has
+    const int all = cols / Chunks<T>::kValues, x = (int)threadIdx.x;
+    return all > x ? min(NV * Chunks<T>::kNum, (all - x - 1) / team_width<TEAM>() + 1) : 0;
+}
 
-// `first`: shared address of the chunk 0 of piece 0 of this thread; `plane`: bytes from chunk to chunk.
+// The 8 values of a piece from shared memory: chunk 0 at `at`, chunk 1 `plane` bytes on.
 template <class T>
 __device__ __forceinline__ void team_get(unsigned at, unsigned plane, float2 (&f)[4]) {
     unsigned w[4 * Chunks<T>::kNum];
@@ -495,13 +524,15 @@ __device__ __forceinline__ void team_get(unsigned at, unsigned plane, float2 (&f
         for (int j = 0; j < 4; ++j) f[j] = make_float2(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + (sizeof(T) == 4 ? 1 : 0)]));
     }
 }
-template <class T>
-__device__ __forceinline__ void team_put(T* p, const float2 (&f)[4]) {
+// Piece i into the row whose first column of this thread is at p.
+template <class T, int TEAM>
+__device__ __forceinline__ void team_put(T* p, int i, int chunks, const float2 (&f)[4]) {
     if (sizeof(T) == 2) {
-        *reinterpret_cast<uint4*>(p) = make_uint4(narrow2(f[0]), narrow2(f[1]), narrow2(f[2]), narrow2(f[3]));
+        if (i < chunks) *reinterpret_cast<uint4*>(p + i * team_width<TEAM>() * 8) = make_uint4(narrow2(f[0]), narrow2(f[1]), narrow2(f[2]), narrow2(f[3]));
     } else {
-        reinterpret_cast<float4*>(p)[0] = make_float4(f[0].x, f[0].y, f[1].x, f[1].y);
-        reinterpret_cast<float4*>(p)[1] = make_float4(f[2].x, f[2].y, f[3].x, f[3].y);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (2 * i + h < chunks) *reinterpret_cast<float4*>(p + (2 * i + h) * team_width<TEAM>() * 4) = make_float4(f[2 * h].x, f[2 * h].y, f[2 * h + 1].x, f[2 * h + 1].y);
     }
 }
 
@@ -512,59 +543,50 @@ struct TeamMatrix {
     long long step;
     unsigned place;  // in the ring's first row
     __device__ __forceinline__ TeamMatrix(const void* base, long long ld, long long first, long long stride, unsigned ring, int array) {
-        row = base ? static_cast<const T*>(base) + first * ld + threadIdx.x * 8 : nullptr;
+        row = base ? static_cast<const T*>(base) + first * ld + threadIdx.x * Chunks<T>::kValues : nullptr;
         step = base ? stride * ld : 0;
         place = ring + (unsigned)(array * NV * Chunks<T>::kNum * team_width<TEAM>() + (int)threadIdx.x) * 16u;
     }
-    __device__ __forceinline__ unsigned at(int i) const { return place + (unsigned)(i * Chunks<T>::kNum * team_width<TEAM>()) * 16u; }
-    __device__ __forceinline__ void clear(int stages, unsigned stage_bytes, int pieces) const {
+    __device__ __forceinline__ unsigned at(int k) const { return place + (unsigned)(k * team_width<TEAM>()) * 16u; }  // chunk k
+    __device__ __forceinline__ void clear(int stages, unsigned stage_bytes, int chunks) const {
         for (int s = 0; s < stages; ++s)
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (!row || i >= pieces)
-#pragma unroll
-                    for (int h = 0; h < Chunks<T>::kNum; ++h)
-                        asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at(i) + (unsigned)s * stage_bytes + (unsigned)(h * team_width<TEAM>()) * 16u), "r"(0u) : "memory");
+            for (int k = 0; k < NV * Chunks<T>::kNum; ++k)
+                if (!row || k >= chunks) asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at(k) + (unsigned)s * stage_bytes), "r"(0u) : "memory");
     }
-    __device__ __forceinline__ void fetch(unsigned stage_at, int pieces) {
+    __device__ __forceinline__ void fetch(unsigned stage_at, int chunks) {
         if (!row) return;
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (i < pieces)
-#pragma unroll
-                for (int h = 0; h < Chunks<T>::kNum; ++h)
-                    copy_async<16>(at(i) + stage_at + (unsigned)(h * team_width<TEAM>()) * 16u, row + i * team_width<TEAM>() * 8 + h * (16 / (int)sizeof(T)));
+        for (int k = 0; k < NV * Chunks<T>::kNum; ++k)
+            if (k < chunks) copy_async<16>(at(k) + stage_at, row + k * team_width<TEAM>() * Chunks<T>::kValues);
         row += step;
     }
-    __device__ __forceinline__ void get(unsigned stage_at, int i, float2 (&f)[4]) const { team_get<T>(at(i) + stage_at, (unsigned)team_width<TEAM>() * 16u, f); }
+    __device__ __forceinline__ void get(unsigned stage_at, int i, float2 (&f)[4]) const { team_get<T>(at(i * Chunks<T>::kNum) + stage_at, (unsigned)team_width<TEAM>() * 16u, f); }
 };
 
-// fp32 weights (times those of `times`) of all columns into shared memory at `to`, by the CTA: chunk 0 of every piece, then chunk 1.
-template <class W, int NV, int TEAM>
+// fp32 weights (times those of `times`) of all columns into shared memory at `to`, by the CTA, in the order in which threads read
+// them: plane 2 i + h holds values 4 h .. 4 h + 3 of every thread's piece i.
+template <class T, class W, int NV, int TEAM>
 __device__ __forceinline__ void team_weights(unsigned to, const void* w, const void* times, int cols) {
-    for (int v = threadIdx.y * blockDim.x + threadIdx.x; v < NV * team_width<TEAM>(); v += blockDim.x * blockDim.y) {
-        float f[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = 1.0f;
-        if (v * 8 < cols) {
-            Pack<W, 8> t;
+    for (int v = threadIdx.y * blockDim.x + threadIdx.x; v < 2 * NV * team_width<TEAM>(); v += blockDim.x * blockDim.y) {
+        const int plane = v / team_width<TEAM>(), x = v - plane * team_width<TEAM>();
+        const int col = sizeof(T) == 2 ? ((plane >> 1) * team_width<TEAM>() + x) * 8 + (plane & 1) * 4 : (plane * team_width<TEAM>() + x) * 4;
+        float f[4] = {1.0f, 1.0f, 1.0f, 1.0f};
+        if (col < cols) {
+            Pack<W, 4> t;
             if (w) {
-                t.load(static_cast<const W*>(w) + v * 8);
+                t.load(static_cast<const W*>(w) + col);
                 t.get(f);
             }
             if (times) {
-                float g[8];
-                t.load(static_cast<const W*>(times) + v * 8);
+                float g[4];
+                t.load(static_cast<const W*>(times) + col);
                 t.get(g);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) f[j] *= g[j];
+                for (int j = 0; j < 4; ++j) f[j] *= g[j];
             }
         }
-        // piece i, thread x: v = i * blockDim.x + x
-        const unsigned i = (unsigned)v / (unsigned)team_width<TEAM>(), x = (unsigned)v - i * (unsigned)team_width<TEAM>();
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to + ((2u * i + h) * (unsigned)team_width<TEAM>() + x) * 16u), "f"(f[4 * h]), "f"(f[4 * h + 1]), "f"(f[4 * h + 2]), "f"(f[4 * h + 3]) : "memory");
+        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to + (unsigned)v * 16u), "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]) : "memory");
     }
 }
 
@@ -581,28 +603,29 @@ norm_forward_team_kernel(const NormArgs a) {
     const long long stride = (long long)gridDim.x * blockDim.y;
     long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y;
     const bool normed = a.branch_weight != nullptr, has_branch = a.branch != nullptr;
-    const int vectors = a.cols / 8, pieces = vectors > (int)threadIdx.x ? min(NV, (vectors - (int)threadIdx.x - 1) / team_width<TEAM>() + 1) : 0;
+    const int chunks = team_chunks<T, NV, TEAM>(a.cols);
+    constexpr int kFirst = Chunks<T>::kValues;
     TeamMatrix<T, NV, TEAM> mx(a.x, a.ld_x, row, stride, ring, 0), mb(a.branch, a.ld_branch, row, stride, ring, 1), mg(FULL ? a.gate : nullptr, a.ld_gate, row, stride, ring, 2);
-    mx.clear(a.stages, stage_bytes, pieces);
-    mb.clear(a.stages, stage_bytes, pieces);
-    if (FULL) mg.clear(a.stages, stage_bytes, pieces);
+    mx.clear(a.stages, stage_bytes, chunks);
+    mb.clear(a.stages, stage_bytes, chunks);
+    if (FULL) mg.clear(a.stages, stage_bytes, chunks);
     long long coming = row;
     auto fetch = [&](unsigned stage_at) {
         if (coming < a.rows) {
-            mx.fetch(stage_at, pieces);
-            mb.fetch(stage_at, pieces);
-            if (FULL) mg.fetch(stage_at, pieces);
+            mx.fetch(stage_at, chunks);
+            mb.fetch(stage_at, chunks);
+            if (FULL) mg.fetch(stage_at, chunks);
         }
         coming += stride;
         copy_commit();
     };
     for (int k = 0; k < a.stages - 1; ++k) fetch((unsigned)k * stage_bytes);
-    team_weights<W, NV, TEAM>(weights, a.weight, nullptr, a.cols);
-    team_weights<W, NV, TEAM>(weights + table, a.branch_weight, a.gate_kind == SL_GATE_COLUMN ? a.gate : nullptr, a.cols);
+    team_weights<T, W, NV, TEAM>(weights, a.weight, nullptr, a.cols);
+    team_weights<T, W, NV, TEAM>(weights + table, a.branch_weight, a.gate_kind == SL_GATE_COLUMN ? a.gate : nullptr, a.cols);
     __syncthreads();
     const unsigned mine = weights + threadIdx.x * 16u, plane = (unsigned)team_width<TEAM>() * 16u;  // this thread's weights: piece i at mine + 2 i plane
-    T* y = static_cast<T*>(a.y) + (a.y ? row * a.ld_y + threadIdx.x * 8 : 0);
-    T* h = static_cast<T*>(a.h) + (a.h ? row * a.ld_h + threadIdx.x * 8 : 0);
+    T* y = static_cast<T*>(a.y) + (a.y ? row * a.ld_y + threadIdx.x * kFirst : 0);
+    T* h = static_cast<T*>(a.h) + (a.h ? row * a.ld_h + threadIdx.x * kFirst : 0);
     for (unsigned at = 0; row < a.rows; row += stride) {
         fetch(at ? at - stage_bytes : ring_bytes - stage_bytes);
         copy_wait(a.stages - 1);
@@ -637,7 +660,7 @@ norm_forward_team_kernel(const NormArgs a) {
                     v[i][j] = fma2(mul2(z[j], both(scale)), FULL ? mul2(c[j], g[j]) : c[j], v[i][j]);
                     q = fma2(v[i][j], v[i][j], q);
                 }
-                if (i < pieces) team_put(y + i * team_width<TEAM>() * 8, v[i]);
+                team_put<T, TEAM>(y, i, chunks, v[i]);
             }
             y += stride * a.ld_y;
         } else {
@@ -660,7 +683,7 @@ norm_forward_team_kernel(const NormArgs a) {
             team_get<float>(mine + 2u * i * plane, plane, w);
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[j] = mul2(mul2(v[i][j], both(r)), w[j]);
-            if (i < pieces) team_put(h + i * team_width<TEAM>() * 8, w);
+            team_put<T, TEAM>(h, i, chunks, w);
         }
         h += stride * a.ld_h;
     }
@@ -679,22 +702,23 @@ norm_backward_team_kernel(const NormArgs a) {
     const long long stride = (long long)gridDim.x * blockDim.y;
     long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y;
     const bool normed = a.branch_weight != nullptr, row_gate = a.gate_kind == SL_GATE_ROW;
-    const int vectors = a.cols / 8, pieces = vectors > (int)threadIdx.x ? min(NV, (vectors - (int)threadIdx.x - 1) / team_width<TEAM>() + 1) : 0;
+    const int chunks = team_chunks<T, NV, TEAM>(a.cols);
+    constexpr int kFirst = Chunks<T>::kValues;
     TeamMatrix<T, NV, TEAM> mdy(a.dy, a.ld_dy, row, stride, ring, 0), mdh(a.dh, a.ld_dh, row, stride, ring, 1), my(a.dh ? a.x : nullptr, a.ld_y, row, stride, ring, 2),
         mb(a.branch, a.ld_branch, row, stride, ring, 3), mg(FULL ? a.gate : nullptr, a.ld_gate, row, stride, ring, 4);
-    mdy.clear(a.stages, stage_bytes, pieces);
-    mdh.clear(a.stages, stage_bytes, pieces);
-    my.clear(a.stages, stage_bytes, pieces);
-    mb.clear(a.stages, stage_bytes, pieces);
-    if (FULL) mg.clear(a.stages, stage_bytes, pieces);
+    mdy.clear(a.stages, stage_bytes, chunks);
+    mdh.clear(a.stages, stage_bytes, chunks);
+    my.clear(a.stages, stage_bytes, chunks);
+    mb.clear(a.stages, stage_bytes, chunks);
+    if (FULL) mg.clear(a.stages, stage_bytes, chunks);
     long long coming = row;
     auto fetch = [&](unsigned stage_at) {
         if (coming < a.rows) {
-            mdy.fetch(stage_at, pieces);
-            mdh.fetch(stage_at, pieces);
-            my.fetch(stage_at, pieces);
-            mb.fetch(stage_at, pieces);
-            if (FULL) mg.fetch(stage_at, pieces);
+            mdy.fetch(stage_at, chunks);
+            mdh.fetch(stage_at, chunks);
+            my.fetch(stage_at, chunks);
+            mb.fetch(stage_at, chunks);
+            if (FULL) mg.fetch(stage_at, chunks);
         }
         coming += stride;
         copy_commit();
@@ -707,8 +731,8 @@ norm_backward_team_kernel(const NormArgs a) {
     };
     for (int k = 0; k < a.stages - 1; ++k) fetch((unsigned)k * stage_bytes);
     if (row < a.rows) scalars(row);
-    team_weights<W, NV, TEAM>(weights, a.weight, nullptr, a.cols);
-    team_weights<W, NV, TEAM>(weights + table, a.branch_weight, a.gate_kind == SL_GATE_COLUMN ? a.gate : nullptr, a.cols);
+    team_weights<T, W, NV, TEAM>(weights, a.weight, nullptr, a.cols);
+    team_weights<T, W, NV, TEAM>(weights + table, a.branch_weight, a.gate_kind == SL_GATE_COLUMN ? a.gate : nullptr, a.cols);
     __syncthreads();
     const unsigned mine = weights + threadIdx.x * 16u, plane = (unsigned)team_width<TEAM>() * 16u;
     float2 acc[2][NV][4];
@@ -716,9 +740,9 @@ norm_backward_team_kernel(const NormArgs a) {
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[0][i][j] = acc[1][i][j] = both(0.0f);
-    T* dx = static_cast<T*>(a.dx) + (a.dx ? row * a.ld_x + threadIdx.x * 8 : 0);
-    T* dbranch = static_cast<T*>(a.dbranch) + (a.dbranch ? row * a.ld_branch + threadIdx.x * 8 : 0);
-    T* dgate = static_cast<T*>(a.dgate) + (FULL && a.dgate ? row * a.ld_gate + threadIdx.x * 8 : 0);
+    T* dx = static_cast<T*>(a.dx) + (a.dx ? row * a.ld_x + threadIdx.x * kFirst : 0);
+    T* dbranch = static_cast<T*>(a.dbranch) + (a.dbranch ? row * a.ld_branch + threadIdx.x * kFirst : 0);
+    T* dgate = static_cast<T*>(a.dgate) + (FULL && a.dgate ? row * a.ld_gate + threadIdx.x * kFirst : 0);
     int turn = 0;
     for (unsigned at = 0; row < a.rows; row += stride, turn ^= 1) {
         fetch(at ? at - stage_bytes : ring_bytes - stage_bytes);
@@ -776,11 +800,9 @@ norm_backward_team_kernel(const NormArgs a) {
                 acc[1][i][j] = fma2(e, bh[j], acc[1][i][j]);
                 dh[j] = fma2(e, c[j], mul2(bh[j], nb));                          // dbranch (rb is 1 and rbm 0 without its norm)
             }
-            if (i < pieces) {
-                if (a.dx) team_put(dx + i * team_width<TEAM>() * 8, dy);
-                if (a.dbranch) team_put(dbranch + i * team_width<TEAM>() * 8, dh);
-                if (FULL && a.dgate) team_put(dgate + i * team_width<TEAM>() * 8, g);
-            }
+            if (a.dx) team_put<T, TEAM>(dx, i, chunks, dy);
+            if (a.dbranch) team_put<T, TEAM>(dbranch, i, chunks, dh);
+            if (FULL && a.dgate) team_put<T, TEAM>(dgate, i, chunks, g);
         }
         dx += stride * a.ld_x;
         dbranch += stride * a.ld_branch;
@@ -797,10 +819,12 @@ norm_backward_team_kernel(const NormArgs a) {
     for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-            if (i < pieces) {
-                const unsigned to = down + ((threadIdx.y * 2u + k) * (unsigned)a.cols + (unsigned)(i * team_width<TEAM>() + (int)threadIdx.x) * 8u) * 4u;
-                asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to), "f"(acc[k][i][0].x), "f"(acc[k][i][0].y), "f"(acc[k][i][1].x), "f"(acc[k][i][1].y) : "memory");
-                asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to + 16u), "f"(acc[k][i][2].x), "f"(acc[k][i][2].y), "f"(acc[k][i][3].x), "f"(acc[k][i][3].y) : "memory");
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int col = sizeof(T) == 2 ? (i * team_width<TEAM>() + (int)threadIdx.x) * 8 + 4 * h : ((2 * i + h) * team_width<TEAM>() + (int)threadIdx.x) * 4;
+                if (col < a.cols)
+                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(down + ((threadIdx.y * 2u + k) * (unsigned)a.cols + (unsigned)col) * 4u), "f"(acc[k][i][2 * h].x),
+                                 "f"(acc[k][i][2 * h].y), "f"(acc[k][i][2 * h + 1].x), "f"(acc[k][i][2 * h + 1].y) : "memory");
             }
     __syncthreads();
     float* part = a.part + (long long)blockIdx.x * 2 * a.cols;

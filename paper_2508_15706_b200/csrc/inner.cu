@@ -78,8 +78,14 @@ sl_status launch_adamw_bits(const sl_adamw* c, const AdamArgs& a, cudaStream_t s
 // ---- rotary
 template <class T, int VEC>
 sl_status launch_rotary(const RopeArgs& a, bool half, unsigned grid, size_t smem, cudaStream_t st) {
-    if (half) rotary_kernel<T, VEC, true><<<grid, kRopeThreads, smem, st>>>(a);
-    else rotary_kernel<T, VEC, false><<<grid, kRopeThreads, smem, st>>>(a);
+    constexpr bool kMayBeWide = VEC * sizeof(T) < 16;
+    if (kMayBeWide && a.copy != VEC && a.slots > a.rot_slots) {
+        if (half) rotary_kernel<T, VEC, true, kMayBeWide><<<grid, kRopeThreads, smem, st>>>(a);
+        else rotary_kernel<T, VEC, false, kMayBeWide><<<grid, kRopeThreads, smem, st>>>(a);
+    } else {
+        if (half) rotary_kernel<T, VEC, true, false><<<grid, kRopeThreads, smem, st>>>(a);
+        else rotary_kernel<T, VEC, false, false><<<grid, kRopeThreads, smem, st>>>(a);
+    }
     SL_CUDA(cudaGetLastError());
     return SL_OK;
 }
@@ -404,12 +410,10 @@ sl_status sl_rotary_apply(sl_rotary* c, const sl_rotary_desc* d, const sl_rotary
         return SL_ERR_TOO_LARGE;
     const int bytes = dtype_bytes(d->dtype), rot = c->cfg.rot_dim;
     const bool half = c->cfg.layout == SL_ROPE_HALF;
-    // the widest access that every offset of a turned or copied part is a multiple of
-    int vec = 16 / bytes;
-    const int64_t parts[] = {half ? rot / 2 : rot, d->head_dim - rot};
-    auto divides = [&](int v) {
-        for (int64_t p : parts)
-            if (p % v) return false;
+    // the widest accesses that every offset of the turned part, and of what is passed through, is a multiple of
+    int vec = 16 / bytes, copy = 16 / bytes;
+    auto divides = [&](int v, int64_t part, int64_t begin) {
+        if (part % v || begin % v) return false;
         for (const sl_rotary_heads* h : {q, k}) {
             if (!h->in) continue;
             for (int64_t st : {h->in_batch, h->in_token, h->in_head, h->out_batch, h->out_token, h->out_head})
@@ -418,7 +422,8 @@ sl_status sl_rotary_apply(sl_rotary* c, const sl_rotary_desc* d, const sl_rotary
         }
         return true;
     };
-    while (vec > 1 && !divides(vec)) vec /= 2;
+    while (copy > 1 && !divides(copy, d->head_dim - rot, rot)) copy /= 2;
+    while (vec > 1 && (vec > copy || !divides(vec, half ? rot / 2 : rot, 0))) vec /= 2;  // (never wider than the rest's)
     for (const sl_rotary_heads* h : {q, k})
         if (!fits(h->in, bytes) || !fits(h->out, bytes)) return SL_ERR_ALIGNMENT;
     if (positions && !fits(positions, d->position_bits / 8)) return SL_ERR_ALIGNMENT;
@@ -445,7 +450,8 @@ sl_status sl_rotary_apply(sl_rotary* c, const sl_rotary_desc* d, const sl_rotary
     a.magnitude = (float)c->cfg.magnitude;
     a.sign = d->inverse ? -1.0f : 1.0f;
     a.rot_slots = half ? rot / 2 / vec : (vec > 1 ? rot / vec : rot / 2);
-    a.slots = a.rot_slots + (int)(d->head_dim - rot) / vec;
+    a.copy = copy;
+    a.slots = a.rot_slots + (int)(d->head_dim - rot) / copy;
     if (a.rows == 0) return SL_OK;
     int n_sms = 0;
     sl_status s = sm_count(&n_sms);

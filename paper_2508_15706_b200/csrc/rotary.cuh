@@ -23,18 +23,27 @@ struct RopeArgs {
     long long pos_batch, pos_token, first, rows;  // rows = batch * seq
     int position_bits, seq, head_dim, rot, tokens;  // tokens per CTA
     int slots, rot_slots;                           // accesses per head, those of them that turn
+    int copy;                                       // values per access of the rest, which is passed through
     float magnitude, sign;
 };
 
 // One item: a slot of a head of a token.  VEC consecutive values per access.  Half layout: a turning slot is two accesses, rot / 2
 // apart; interleaved: one access of VEC / 2 pairs (one pair of single values where VEC is 1).  The slots behind them copy what is
-// passed through.
-template <class T, int VEC, bool HALF>
+// passed through; WIDE: by wider accesses than those that turn.
+template <class T, int VEC, bool HALF, bool WIDE>
 struct RopeItem {
     Pack<T, VEC> a, b;
+    uint4 c;  // WIDE: what is passed through
     __device__ __forceinline__ void load(const T* in, int slot, const RopeArgs& r) {
-        if (slot >= r.rot_slots) {
+        if (!WIDE && slot >= r.rot_slots) {
             a.load(in + r.rot + (slot - r.rot_slots) * VEC);
+        } else if (slot >= r.rot_slots) {
+            const T* p = in + r.rot + (slot - r.rot_slots) * r.copy;
+            const int bytes = r.copy * (int)sizeof(T);
+            if (bytes == 16) c = *reinterpret_cast<const uint4*>(p);
+            else if (bytes == 8) c.x = reinterpret_cast<const uint2*>(p)->x, c.y = reinterpret_cast<const uint2*>(p)->y;
+            else if (bytes == 4) c.x = *reinterpret_cast<const unsigned*>(p);
+            else c.x = *reinterpret_cast<const unsigned short*>(p);
         } else if (HALF) {
             a.load(in + slot * VEC);
             b.load(in + r.rot / 2 + slot * VEC);
@@ -49,7 +58,17 @@ struct RopeItem {
     // read neighbouring words)
     __device__ __forceinline__ void turn_store(T* out, int slot, const RopeArgs& r, const float2* cs, bool in_place) {
         if (slot >= r.rot_slots) {
-            if (!in_place) a.store(out + r.rot + (slot - r.rot_slots) * VEC);
+            if (in_place) return;
+            if (!WIDE) {
+                a.store(out + r.rot + (slot - r.rot_slots) * VEC);
+                return;
+            }
+            T* p = out + r.rot + (slot - r.rot_slots) * r.copy;
+            const int bytes = r.copy * (int)sizeof(T);
+            if (bytes == 16) *reinterpret_cast<uint4*>(p) = c;
+            else if (bytes == 8) *reinterpret_cast<uint2*>(p) = make_uint2(c.x, c.y);
+            else if (bytes == 4) *reinterpret_cast<unsigned*>(p) = c.x;
+            else *reinterpret_cast<unsigned short*>(p) = (unsigned short)c.x;
         } else if (HALF) {
             const int c = slot * VEC;
             float x[VEC], y[VEC];
@@ -94,7 +113,7 @@ struct RopeItem {
 
 // A thread keeps its slot and walks over the (token, head) pairs of the CTA, a few of them at a time, all loads before the
 // first use; the first batch is on its way while sines and cosines are computed.
-template <class T, int VEC, bool HALF>
+template <class T, int VEC, bool HALF, bool WIDE>
 __global__ void __launch_bounds__(kRopeThreads)
 rotary_kernel(const RopeArgs a) {
     constexpr int kBatch = HALF && VEC > 1 ? 2 : 4, kPairs = HALF ? VEC : (VEC > 1 ? VEC / 2 : 1);  // pairs of a slot
@@ -140,7 +159,7 @@ rotary_kernel(const RopeArgs a) {
 
     bool ready = false;
     for (int slot = threadIdx.x - group * span; slot < a.slots || !ready; slot += span) {
-        RopeItem<T, VEC, HALF> item[kBatch];
+        RopeItem<T, VEC, HALF, WIDE> item[kBatch];
         Place at;
         at.tok = group / heads;
         at.head = group - at.tok * heads;

@@ -228,7 +228,7 @@ loss_row_kernel(const LossArgs a, const T* logits, T* grad, int cluster) {
     extern __shared__ __align__(16) char ring[];  // [stages][NV * threads] vectors
     __shared__ __align__(8) unsigned long long landed[kLossStages];
     __shared__ float buf[2][3][32], xts[2];
-    __shared__ float mine[4];  // this CTA's maximum, sum of exponentials, sum: read by the cluster
+    __shared__ float mine[2][4];  // this CTA's maximum, sum of exponentials, sum of two rows in turn: read by the cluster
     const int tid = threadIdx.x, threads = blockDim.x;
     const unsigned teams = gridDim.x / (unsigned)cluster;
     long long row = blockIdx.x / (unsigned)cluster;
@@ -344,15 +344,14 @@ loss_row_kernel(const LossArgs a, const T* logits, T* grad, int cluster) {
         if (cluster > 1) {
             namespace cg = cooperative_groups;
             auto group = cg::this_cluster();
-            if (tid == 0) mine[0] = r.m, mine[1] = r.s, mine[2] = r.sum;
+            if (tid == 0) mine[turn][0] = r.m, mine[turn][1] = r.s, mine[turn][2] = r.sum;
             group.sync();
             for (int c = 0; c < cluster; ++c) {  // in the same order in every CTA
-                const float* other = group.map_shared_rank(mine, (unsigned)c);
+                const float* other = group.map_shared_rank(mine[turn], (unsigned)c);
                 const float m2 = other[0], s2 = other[1], x2 = other[2];
                 if (c == 0) r.m = m2, r.s = s2, r.sum = x2;
                 else join(r.m, r.s, m2, s2), r.sum += x2;
             }
-            group.sync();  // nobody leaves, or writes the next row's, while its values are read
         }
         r.finish();
         if (!weighed) {
@@ -404,6 +403,7 @@ loss_row_kernel(const LossArgs a, const T* logits, T* grad, int cluster) {
         if (stage == 0) phase ^= 1u;
         at = stage * stage_bytes;
     }
+    if (cluster > 1) cooperative_groups::this_cluster().sync();  // nobody leaves while its values are read
     if (!arrived && tid == 0)  // (a last bounded wait for what may still be on its way into this CTA's memory)
         for (int k = 0; k < kLossStages; ++k, stage = stage + 1 == kLossStages ? 0u : stage + 1, phase ^= stage == 0) bulk_wait(landed_at + stage * 8u, phase);
     add_rows(a, gridDim.x, w, valid);

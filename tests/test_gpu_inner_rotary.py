@@ -104,6 +104,21 @@ def test_strides_orders_and_positions(layout):
             assert torch.equal(again, q)
 
 
+@pytest.mark.parametrize("head_dim,rot,stride", [(70, 64, 72), (66, 64, 80), (72, 64, 72), (100, 24, 104), (128, 50, 128), (51, 34, 64), (96, 38, 96)])
+@pytest.mark.parametrize("act", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_rest_of_the_head_of_any_width(head_dim, rot, stride, act, layout):
+    """The part that turns and the part that is passed through divide into accesses of different widths; padded heads."""
+    from paper_2508_15706_b200.inner import Rotary
+    x = torch.randn(2, 9, 3, stride, device="cuda").to(act)
+    q = x[..., :head_dim]
+    out = torch.full((2, 9, 3, stride), 5.0, dtype=act, device="cuda")
+    Rotary(rot, layout=layout).apply(q, None, None, first=3, out_q=out[..., :head_dim])
+    pos = (torch.arange(9, device="cuda") + 3).expand(2, 9)
+    close(out[..., :head_dim], *turned(q.double(), pos, freqs(rot, 10000.0, "none", 1, 0, 0, 0), rot, layout, 1.0, False))
+    assert torch.equal(out[..., rot:head_dim], q[..., rot:]) and torch.all(out[..., head_dim:] == 5.0)
+
+
 @pytest.mark.parametrize("scaling", ["none", "linear", "base", "by_parts"])
 @pytest.mark.parametrize("rot", [4, 64, 128])
 def test_scalings_and_far_positions(scaling, rot):
