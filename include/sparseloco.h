@@ -528,6 +528,7 @@ sl_status sl_rotary_apply(sl_rotary* ctx, const sl_rotary_desc* d, const sl_rota
  * and loss +inf; NaN or +inf in a row give NaN.  A target outside [0, vocab) that is not ignore_index gives its row (and the
  * total) a NaN loss and a gradient of 0 (the row counts).
  * grad: NULL (loss only), or rows of `dtype` by ld_grad; grad may be logits itself (then ld_grad = ld_logits).
+ * The kernel's waits for its own copies are bounded; one that ran out would show as NaN losses from that row on.
  * row_loss (rows fp32) is required; lse, total may be NULL.  targets: int32 or int64 (target_bits).  rows = 0 is allowed.
  * workspace: sl_loss_workspace_bytes(), 16-byte aligned, contents need not be kept; calls that share it must not overlap.
  * Errors: INVALID_ARG, ALIGNMENT, UNSUPPORTED (dtype, target_bits), TOO_LARGE (vocab > 2^30), NOMEM, CUDA. */
