@@ -9,6 +9,7 @@ torch's autograd.
 from __future__ import annotations
 
 import ctypes as C
+import struct
 from typing import Optional, Sequence
 
 import torch
@@ -46,6 +47,12 @@ class _LossDesc(C.Structure):
     _fields_ = [("rows", I64), ("vocab", I64), ("dtype", I32), ("target_bits", I32), ("ld_logits", I64), ("ld_grad", I64), ("ignore_index", I64), ("smoothing", F32), ("z", F32), ("scale", F32), ("mean", I32)]
 
 
+# The descriptions of a call as bytes in the C layout: packing is several times faster than filling a ctypes structure.
+_norm_bytes = struct.Struct("@qqiiiffqqqqqqq").pack      # _NormDesc
+_heads_bytes = struct.Struct("@PPqqqqqqq").pack           # _RotaryHeads
+_rotary_bytes = struct.Struct("@iiiqqqqqq").pack          # _RotaryDesc
+_loss_bytes = struct.Struct("@qqiiqqqfffi").pack          # _LossDesc (without the padding at its end)
+
 _L.sl_adamw_create.argtypes = [P, P, P, I32, C.POINTER(P)]
 _L.sl_adamw_destroy.argtypes = [P]
 _L.sl_adamw_sizes.argtypes = [P, C.POINTER(I64), C.POINTER(I64)]
@@ -75,12 +82,8 @@ def _dtype(t: torch.dtype) -> int:
 
 # The checks below are made on every call of operators that may take a few microseconds, so they ask for each property once
 # and put a message together only when one fails.
-def _here() -> int:
-    return torch._C._cuda_getDevice()
-
-
-def _queue(dev: int) -> int:
-    return torch._C._cuda_getCurrentRawStream(dev)
+_here = torch._C._cuda_getDevice            # the current device
+_queue = torch._C._cuda_getCurrentRawStream  # its current stream
 
 
 def _ptr(t: Optional[torch.Tensor], dev: int, dtype, numel: int, what: str) -> Optional[int]:
@@ -189,7 +192,8 @@ def _gate(gate, dev, rows, cols, act, wt):
     return (3, *_rows(gate, dev, rows, cols, act, "element gate"))
 
 
-def _norm_desc(x, dev, weight, branch_weight, gate, alpha, eps):
+def _norm_case(x, dev, weight, branch_weight, gate):
+    """Rows, columns, types, and the gate's kind, address and stride."""
     if x.dim() != 2:
         _refuse("activations must be [rows, cols]")
     rows, cols = x.shape
@@ -201,14 +205,14 @@ def _norm_desc(x, dev, weight, branch_weight, gate, alpha, eps):
     else:
         wt = gate.dtype if gate is not None and gate.shape == (cols,) else torch.float32
     kind, g, ld = (0, None, 0) if gate is None else _gate(gate, dev, rows, cols, act, wt)
-    return _NormDesc(rows, cols, _dtype(act), _dtype(wt), kind, alpha, eps, 0, 0, ld), rows, cols, act, wt, g
+    return rows, cols, act, wt, kind, g, ld
 
 
 def norm_forward(x, weight=None, *, branch=None, branch_weight=None, gate=None, alpha: float = 1.0, eps: float = 1e-6, norm: bool = True, y=None, h=None, rstd=None, branch_rstd=None):
     """y = x + alpha * gate * norm(branch) (the norm only with `branch_weight`), h = norm(y) * weight (`norm=False`: no h).
     Returns (y, h, rstd, branch_rstd); y is x itself without a branch.  Outputs left out are allocated."""
     dev = _here()
-    d, rows, cols, act, wt, g = _norm_desc(x, dev, weight, branch_weight, gate, alpha, eps)
+    rows, cols, act, wt, kind, g, ld_g = _norm_case(x, dev, weight, branch_weight, gate)
     if branch is not None and y is None:
         y = torch.empty(rows, cols, dtype=act, device=x.device)
     if norm and h is None:
@@ -217,11 +221,12 @@ def norm_forward(x, weight=None, *, branch=None, branch_weight=None, gate=None, 
         rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
     if branch_weight is not None and branch_rstd is None:
         branch_rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
-    px, d.ld_x = _rows(x, dev, rows, cols, act, "x")
-    pb, d.ld_branch = _rows(branch, dev, rows, cols, act, "branch")
-    py, d.ld_y = _rows(y, dev, rows, cols, act, "y") if branch is not None else (None, 0)
-    ph, d.ld_h = _rows(h, dev, rows, cols, act, "h") if norm else (None, 0)
-    _check(_L.sl_norm_forward(C.byref(d), px, pb, _ptr(branch_weight, dev, wt, cols, "branch_weight"), g, _ptr(weight, dev, wt, cols, "weight"), py, ph,
+    px, ld_x = _rows(x, dev, rows, cols, act, "x")
+    pb, ld_b = _rows(branch, dev, rows, cols, act, "branch")
+    py, ld_y = _rows(y, dev, rows, cols, act, "y") if branch is not None else (None, 0)
+    ph, ld_h = _rows(h, dev, rows, cols, act, "h") if norm else (None, 0)
+    d = _norm_bytes(rows, cols, _dtype(act), _dtype(wt), kind, alpha, eps, ld_x, ld_b, ld_g, ld_y, ld_h, 0, 0)
+    _check(_L.sl_norm_forward(d, px, pb, _ptr(branch_weight, dev, wt, cols, "branch_weight"), g, _ptr(weight, dev, wt, cols, "weight"), py, ph,
                               _ptr(branch_rstd, dev, torch.float32, rows, "branch_rstd"), _ptr(rstd, dev, torch.float32, rows, "rstd"), _queue(dev)))
     return y if branch is not None else x, h, rstd, branch_rstd
 
@@ -238,13 +243,12 @@ def norm_backward(dy, dh, y, weight=None, *, rstd=None, branch=None, branch_weig
     """Gradients of `norm_forward`, written into the outputs that are given.  `y`, `rstd`, `branch_rstd` as the forward pass left them;
     dy (gradient that reaches y from elsewhere) or dh may be None."""
     dev = _here()
-    d, rows, cols, act, wt, g = _norm_desc(y if y is not None else dy, dev, weight, branch_weight, gate, alpha, 0.0)
-    pdy, d.ld_dy = _rows(dy, dev, rows, cols, act, "dy")
-    pdh, d.ld_dh = _rows(dh, dev, rows, cols, act, "dh")
-    py, d.ld_y = _rows(y, dev, rows, cols, act, "y")
+    rows, cols, act, wt, gate_kind, g, ld_g = _norm_case(y if y is not None else dy, dev, weight, branch_weight, gate)
+    pdy, ld_dy = _rows(dy, dev, rows, cols, act, "dy")
+    pdh, ld_dh = _rows(dh, dev, rows, cols, act, "dh")
+    py, ld_y = _rows(y, dev, rows, cols, act, "y")
     pb, ld_b = _rows(branch, dev, rows, cols, act, "branch")
-    d.ld_branch = ld_b
-    pdx, d.ld_x = _rows(dx, dev, rows, cols, act, "dx")
+    pdx, ld_x = _rows(dx, dev, rows, cols, act, "dx")
     pdb, ld = _rows(dbranch, dev, rows, cols, act, "dbranch")
     if dbranch is not None and ld != ld_b:
         _refuse("dbranch must have the row stride of branch")
@@ -253,11 +257,12 @@ def norm_backward(dy, dh, y, weight=None, *, rstd=None, branch=None, branch_weig
         if gate is None or dgate.shape != gate.shape:
             _refuse("dgate must have the shape of gate")
         kind, pdg, ld = _gate(dgate, dev, rows, cols, act, wt)
-        if ld != d.ld_gate:
+        if ld != ld_g:
             _refuse("dgate must have the strides of gate")
-    if workspace is None and (dweight is not None or dbranch_weight is not None or (dgate is not None and d.gate_kind == 1)):
+    if workspace is None and (dweight is not None or dbranch_weight is not None or (dgate is not None and gate_kind == 1)):
         workspace = norm_backward_workspace(rows, cols, dtype=act)
-    _check(_L.sl_norm_backward(C.byref(d), pdy, pdh, py, pb, _ptr(branch_weight, dev, wt, cols, "branch_weight"), g, _ptr(weight, dev, wt, cols, "weight"),
+    d = _norm_bytes(rows, cols, _dtype(act), _dtype(wt), gate_kind, alpha, 0.0, ld_x, ld_b, ld_g, ld_y, 0, ld_dy, ld_dh)
+    _check(_L.sl_norm_backward(d, pdy, pdh, py, pb, _ptr(branch_weight, dev, wt, cols, "branch_weight"), g, _ptr(weight, dev, wt, cols, "weight"),
                                _ptr(branch_rstd, dev, torch.float32, rows, "branch_rstd"), _ptr(rstd, dev, torch.float32, rows, "rstd"), pdx, pdb, _ptr(dweight, dev, wt, cols, "dweight"),
                                _ptr(dbranch_weight, dev, wt, cols, "dbranch_weight"), pdg, _ptr(workspace, dev, torch.uint8, 0, "workspace"),
                                0 if workspace is None else workspace.numel(), _queue(dev)))
@@ -343,8 +348,8 @@ class Rotary:
             pos, pos_token, pos_batch = positions.data_ptr(), st[-1], st[0] if len(st) == 2 else 0
         if batch * seq == 0:
             return
-        d = _RotaryDesc(_dtype(dtype), bits, inverse, batch, seq, head_dim, first, pos_batch, pos_token)
-        _check(_L.sl_rotary_apply(self._h, C.byref(d), C.byref(hq), None if hk is None else C.byref(hk), pos, _queue(dev)))
+        d = _rotary_bytes(_dtype(dtype), bits, inverse, batch, seq, head_dim, first, pos_batch, pos_token)
+        _check(_L.sl_rotary_apply(self._h, d, hq, hk, pos, _queue(dev)))
 
 
 def _heads(x, out, dev, batch, seq, head_dim, dtype, what):
@@ -352,7 +357,7 @@ def _heads(x, out, dev, batch, seq, head_dim, dtype, what):
     if (len(sh) != 4 or sh[0] != batch or sh[1] != seq or sh[3] != head_dim or out.shape != sh or x.get_device() != dev or out.get_device() != dev or x.dtype is not dtype or
             out.dtype is not dtype or (head_dim > 1 and (a[3] != 1 or b[3] != 1))):
         _refuse(f"{what} must be CUDA tensors [{batch}, {seq}, heads, {head_dim}] of {dtype} on device {dev} with a unit stride inside a head, got {tuple(sh)} {x.dtype}, {tuple(out.shape)} {out.dtype}")
-    return _RotaryHeads(x.data_ptr(), out.data_ptr(), sh[2], a[0], a[1], a[2], b[0], b[1], b[2])
+    return _heads_bytes(x.data_ptr(), out.data_ptr(), sh[2], a[0], a[1], a[2], b[0], b[1], b[2])
 
 
 class _Turn(torch.autograd.Function):
@@ -401,8 +406,8 @@ def token_loss(logits, targets, *, grad=None, ignore_index: int = -100, smoothin
     lse = torch.empty(rows, device=logits.device) if lse is None else lse
     total = torch.empty(1, device=logits.device) if total is None else total
     workspace = loss_workspace() if workspace is None else workspace
-    d = _LossDesc(rows, vocab, _dtype(act), bits, ld_x, ld_g, ignore_index, smoothing, z, scale, mean)
-    _check(_L.sl_token_loss(C.byref(d), px, pt, pg, _ptr(row_loss, dev, torch.float32, rows, "row_loss"), _ptr(lse, dev, torch.float32, rows, "lse"),
+    d = _loss_bytes(rows, vocab, _dtype(act), bits, ld_x, ld_g, ignore_index, smoothing, z, scale, mean)
+    _check(_L.sl_token_loss(d, px, pt, pg, _ptr(row_loss, dev, torch.float32, rows, "row_loss"), _ptr(lse, dev, torch.float32, rows, "lse"),
                             _ptr(total, dev, torch.float32, 1, "total"), _ptr(workspace, dev, torch.uint8, 0, "workspace"), workspace.numel(), _queue(dev)))
     return total, row_loss, lse
 
