@@ -14,6 +14,10 @@ from typing import Optional, Sequence
 
 import torch
 
+try:
+    from . import _checks
+except ImportError as e:
+    raise ImportError("the extension _checks.so is missing or was built for another torch: build it with `python -c 'import __graft_entry__ as g; g.build(force=True)'`") from e
 from .binding import SlError, SL_ERR_INVALID_ARG, _check, _L, _TensorDesc
 
 P, I32, I64, F32, F64 = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_double
@@ -35,10 +39,6 @@ class _RotaryConfig(C.Structure):
     _fields_ = [("rot_dim", I32), ("layout", I32), ("scaling", I32), ("base", F64), ("factor", F64), ("original_length", F64), ("low_turns", F64), ("high_turns", F64), ("magnitude", F64)]
 
 
-class _RotaryHeads(C.Structure):
-    _fields_ = [("inp", P), ("out", P), ("heads", I64), ("in_batch", I64), ("in_token", I64), ("in_head", I64), ("out_batch", I64), ("out_token", I64), ("out_head", I64)]
-
-
 class _RotaryDesc(C.Structure):
     _fields_ = [("dtype", I32), ("position_bits", I32), ("inverse", I32), ("batch", I64), ("seq", I64), ("head_dim", I64), ("first", I64), ("pos_batch", I64), ("pos_token", I64)]
 
@@ -49,7 +49,6 @@ class _LossDesc(C.Structure):
 
 # The descriptions of a call as bytes in the C layout: packing is several times faster than filling a ctypes structure.
 _norm_bytes = struct.Struct("@qqiiiffqqqqqqq").pack      # _NormDesc
-_heads_bytes = struct.Struct("@PPqqqqqqq").pack           # _RotaryHeads
 _rotary_bytes = struct.Struct("@iiiqqqqqq").pack          # _RotaryDesc
 _loss_bytes = struct.Struct("@qqiiqqqfffi").pack          # _LossDesc (without the padding at its end)
 
@@ -80,29 +79,22 @@ def _dtype(t: torch.dtype) -> int:
     return code
 
 
-# The checks below are made on every call of operators that may take a few microseconds, so they ask for each property once
-# and put a message together only when one fails.
 _here = torch._C._cuda_getDevice            # the current device
 _queue = torch._C._cuda_getCurrentRawStream  # its current stream
 
-
-def _ptr(t: Optional[torch.Tensor], dev: int, dtype, numel: int, what: str) -> Optional[int]:
-    """Address of a contiguous tensor of at least `numel` elements on device `dev`."""
-    if t is None:
-        return None
-    if t.get_device() != dev or t.dtype is not dtype or not t.is_contiguous() or t.numel() < numel:
-        _refuse(f"{what} must be a contiguous CUDA tensor of {dtype} on device {dev} with at least {numel} elements, got {t.dtype} {tuple(t.shape)} on {t.device}")
-    return t.data_ptr()
+# The checks of every tensor of a call, compiled (csrc/checks.cpp): in Python they took half of a small call.
+#   _ptr(t, device, numel, dtype, what)           address of a contiguous tensor of at least numel elements, None of None
+#   _rows(t, device, rows, cols, dtype, what)     (address, row stride) of a matrix with a unit column stride, (None, 0) of None
+#   _heads(x, out, device, batch, seq, head_dim, dtype, what)   a sl_rotary_heads as bytes
+_ptr, _rows, _heads = _checks.ptr, _checks.rows, _checks.heads
 
 
-def _rows(t: Optional[torch.Tensor], dev: int, rows: int, cols: int, dtype, what: str):
-    """(address, row stride) of a [rows, cols] matrix with a unit column stride."""
-    if t is None:
-        return None, 0
-    st = t.stride()
-    if t.get_device() != dev or t.dtype is not dtype or t.shape != (rows, cols) or (st[1] != 1 and cols != 1) or (rows > 1 and st[0] < cols):
-        _refuse(f"{what} must be a CUDA tensor [{rows}, {cols}] of {dtype} on device {dev} with unit column stride and rows apart, got {t.dtype} {tuple(t.shape)} strides {st} on {t.device}")
-    return t.data_ptr(), st[0] if rows > 1 else cols
+def _refuse_tensor(what, t, wanted):
+    got = f"{t.dtype} {tuple(t.shape)} strides {t.stride() if t.layout is torch.strided else t.layout} on {t.device}" if isinstance(t, torch.Tensor) else type(t).__name__
+    _refuse(f"{what} must be {wanted}, got {got}")
+
+
+_checks.set_refuse(_refuse_tensor)
 
 
 class AdamW:
@@ -153,7 +145,7 @@ class AdamW:
     def _state(self, dev, m, v, scales):
         if dev != self.device.index:
             _refuse(f"this AdamW was made on {self.device}, the current device is {dev}")
-        return (_ptr(m, dev, self._moment, self.flat_elems, "m"), _ptr(v, dev, self._moment, self.flat_elems, "v"), _ptr(scales, dev, torch.uint8, 2 * self.blocks, "scales"))
+        return (_ptr(m, dev, self.flat_elems, self._moment, "m"), _ptr(v, dev, self.flat_elems, self._moment, "v"), _ptr(scales, dev, 2 * self.blocks, torch.uint8, "scales"))
 
     def step(self, theta, grad, m, v, scales=None, *, step: int, lr: float, grad_scale: float = 1.0, seed: Optional[int] = None, copy=None, norm=None) -> None:
         """One step, in place.  `step` counts from 1; `grad_scale` multiplies the gradient (1 / accumulated micro-batches);
@@ -161,21 +153,21 @@ class AdamW:
         `seed` (default: the step) seeds the rounding of an 8-bit second moment."""
         dev, n = _here(), self.flat_elems
         pm, pv, ps = self._state(dev, m, v, scales)
-        _check(_L.sl_adamw_step(self._h, _ptr(theta, dev, self.param_dtype, n, "theta"), _ptr(grad, dev, self.grad_dtype, n, "grad"), pm, pv, ps,
-                                _ptr(copy, dev, torch.bfloat16, n, "copy"), _ptr(norm, dev, torch.float32, 1, "norm"), step, lr, grad_scale,
+        _check(_L.sl_adamw_step(self._h, _ptr(theta, dev, n, self.param_dtype, "theta"), _ptr(grad, dev, n, self.grad_dtype, "grad"), pm, pv, ps,
+                                _ptr(copy, dev, n, torch.bfloat16, "copy"), _ptr(norm, dev, 1, torch.float32, "norm"), step, lr, grad_scale,
                                 (step if seed is None else seed) & 0xFFFFFFFF, _queue(dev)))
 
     def read_state(self, m, v, scales, m_out, v_out) -> None:
         """8-bit moments as fp32 values, in flat buffers of the same layout."""
         dev, n = _here(), self.flat_elems
         pm, pv, ps = self._state(dev, m, v, scales)
-        _check(_L.sl_adamw_read_state(self._h, pm, pv, ps, _ptr(m_out, dev, torch.float32, n, "m_out"), _ptr(v_out, dev, torch.float32, n, "v_out"), _queue(dev)))
+        _check(_L.sl_adamw_read_state(self._h, pm, pv, ps, _ptr(m_out, dev, n, torch.float32, "m_out"), _ptr(v_out, dev, n, torch.float32, "v_out"), _queue(dev)))
 
     def write_state(self, m_in, v_in, m, v, scales, *, seed: int = 0) -> None:
         """fp32 moments into the 8-bit form, rounded as a step rounds them."""
         dev, n = _here(), self.flat_elems
         pm, pv, ps = self._state(dev, m, v, scales)
-        _check(_L.sl_adamw_write_state(self._h, _ptr(m_in, dev, torch.float32, n, "m_in"), _ptr(v_in, dev, torch.float32, n, "v_in"), pm, pv, ps, seed & 0xFFFFFFFF, _queue(dev)))
+        _check(_L.sl_adamw_write_state(self._h, _ptr(m_in, dev, n, torch.float32, "m_in"), _ptr(v_in, dev, n, torch.float32, "v_in"), pm, pv, ps, seed & 0xFFFFFFFF, _queue(dev)))
 
 
 # ------------------------------------------------------------------------------------------------------------- norms
@@ -183,7 +175,7 @@ def _gate(gate, dev, rows, cols, act, wt):
     """(kind, address, stride): [cols] = per column, [rows, 1] or (rows != cols) [rows] = per row, [rows, cols] = per element."""
     sh = gate.shape
     if len(sh) == 1 and sh[0] == cols:
-        return 1, _ptr(gate, dev, wt, cols, "column gate"), 0
+        return 1, _ptr(gate, dev, cols, wt, "column gate"), 0
     if sh == (rows,) or (sh == (rows, 1) and cols != 1):
         st = gate.stride(0)
         if gate.get_device() != dev or gate.dtype is not act or (rows > 1 and st < 1):
@@ -226,8 +218,8 @@ def norm_forward(x, weight=None, *, branch=None, branch_weight=None, gate=None, 
     py, ld_y = _rows(y, dev, rows, cols, act, "y") if branch is not None else (None, 0)
     ph, ld_h = _rows(h, dev, rows, cols, act, "h") if norm else (None, 0)
     d = _norm_bytes(rows, cols, _dtype(act), _dtype(wt), kind, alpha, eps, ld_x, ld_b, ld_g, ld_y, ld_h, 0, 0)
-    _check(_L.sl_norm_forward(d, px, pb, _ptr(branch_weight, dev, wt, cols, "branch_weight"), g, _ptr(weight, dev, wt, cols, "weight"), py, ph,
-                              _ptr(branch_rstd, dev, torch.float32, rows, "branch_rstd"), _ptr(rstd, dev, torch.float32, rows, "rstd"), _queue(dev)))
+    _check(_L.sl_norm_forward(d, px, pb, _ptr(branch_weight, dev, cols, wt, "branch_weight"), g, _ptr(weight, dev, cols, wt, "weight"), py, ph,
+                              _ptr(branch_rstd, dev, rows, torch.float32, "branch_rstd"), _ptr(rstd, dev, rows, torch.float32, "rstd"), _queue(dev)))
     return y if branch is not None else x, h, rstd, branch_rstd
 
 
@@ -262,9 +254,9 @@ def norm_backward(dy, dh, y, weight=None, *, rstd=None, branch=None, branch_weig
     if workspace is None and (dweight is not None or dbranch_weight is not None or (dgate is not None and gate_kind == 1)):
         workspace = norm_backward_workspace(rows, cols, dtype=act)
     d = _norm_bytes(rows, cols, _dtype(act), _dtype(wt), gate_kind, alpha, 0.0, ld_x, ld_b, ld_g, ld_y, 0, ld_dy, ld_dh)
-    _check(_L.sl_norm_backward(d, pdy, pdh, py, pb, _ptr(branch_weight, dev, wt, cols, "branch_weight"), g, _ptr(weight, dev, wt, cols, "weight"),
-                               _ptr(branch_rstd, dev, torch.float32, rows, "branch_rstd"), _ptr(rstd, dev, torch.float32, rows, "rstd"), pdx, pdb, _ptr(dweight, dev, wt, cols, "dweight"),
-                               _ptr(dbranch_weight, dev, wt, cols, "dbranch_weight"), pdg, _ptr(workspace, dev, torch.uint8, 0, "workspace"),
+    _check(_L.sl_norm_backward(d, pdy, pdh, py, pb, _ptr(branch_weight, dev, cols, wt, "branch_weight"), g, _ptr(weight, dev, cols, wt, "weight"),
+                               _ptr(branch_rstd, dev, rows, torch.float32, "branch_rstd"), _ptr(rstd, dev, rows, torch.float32, "rstd"), pdx, pdb, _ptr(dweight, dev, cols, wt, "dweight"),
+                               _ptr(dbranch_weight, dev, cols, wt, "dbranch_weight"), pdg, _ptr(workspace, dev, 0, torch.uint8, "workspace"),
                                0 if workspace is None else workspace.numel(), _queue(dev)))
 
 
@@ -352,14 +344,6 @@ class Rotary:
         _check(_L.sl_rotary_apply(self._h, d, hq, hk, pos, _queue(dev)))
 
 
-def _heads(x, out, dev, batch, seq, head_dim, dtype, what):
-    sh, a, b = x.shape, x.stride(), out.stride()
-    if (len(sh) != 4 or sh[0] != batch or sh[1] != seq or sh[3] != head_dim or out.shape != sh or x.get_device() != dev or out.get_device() != dev or x.dtype is not dtype or
-            out.dtype is not dtype or (head_dim > 1 and (a[3] != 1 or b[3] != 1))):
-        _refuse(f"{what} must be CUDA tensors [{batch}, {seq}, heads, {head_dim}] of {dtype} on device {dev} with a unit stride inside a head, got {tuple(sh)} {x.dtype}, {tuple(out.shape)} {out.dtype}")
-    return _heads_bytes(x.data_ptr(), out.data_ptr(), sh[2], a[0], a[1], a[2], b[0], b[1], b[2])
-
-
 class _Turn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, rope, positions, first):
@@ -399,7 +383,7 @@ def token_loss(logits, targets, *, grad=None, ignore_index: int = -100, smoothin
     bits = 64 if targets.dtype is torch.int64 else 32 if targets.dtype is torch.int32 else 0
     if not bits or targets.shape != (rows,):
         _refuse(f"targets must be [{rows}] of int32 or int64, got {targets.dtype} {tuple(targets.shape)}")
-    pt = _ptr(targets, dev, targets.dtype, rows, "targets")
+    pt = _ptr(targets, dev, rows, targets.dtype, "targets")
     px, ld_x = _rows(logits, dev, rows, vocab, act, "logits")
     pg, ld_g = _rows(grad, dev, rows, vocab, act, "grad")
     row_loss = torch.empty(rows, device=logits.device) if row_loss is None else row_loss
@@ -407,8 +391,8 @@ def token_loss(logits, targets, *, grad=None, ignore_index: int = -100, smoothin
     total = torch.empty(1, device=logits.device) if total is None else total
     workspace = loss_workspace() if workspace is None else workspace
     d = _loss_bytes(rows, vocab, _dtype(act), bits, ld_x, ld_g, ignore_index, smoothing, z, scale, mean)
-    _check(_L.sl_token_loss(d, px, pt, pg, _ptr(row_loss, dev, torch.float32, rows, "row_loss"), _ptr(lse, dev, torch.float32, rows, "lse"),
-                            _ptr(total, dev, torch.float32, 1, "total"), _ptr(workspace, dev, torch.uint8, 0, "workspace"), workspace.numel(), _queue(dev)))
+    _check(_L.sl_token_loss(d, px, pt, pg, _ptr(row_loss, dev, rows, torch.float32, "row_loss"), _ptr(lse, dev, rows, torch.float32, "lse"),
+                            _ptr(total, dev, 1, torch.float32, "total"), _ptr(workspace, dev, 0, torch.uint8, "workspace"), workspace.numel(), _queue(dev)))
     return total, row_loss, lse
 
 

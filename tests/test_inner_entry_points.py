@@ -92,3 +92,22 @@ def test_rotary_settings(lib):
     for bad in ({"rot_dim": 7}, {"rot_dim": 1026}, {"layout": 2}, {"scaling": 5}, {"base": 1.0}, {"magnitude": float("nan")}, {"scaling": 1, "factor": 0.0}, {"scaling": 2, "factor": 2.0, "rot_dim": 2},
                 {"scaling": 3, "factor": 2.0}, {"scaling": 3, "factor": 2.0, "original_length": 100.0, "high_turns": 1.0}):
         assert create(**bad) == B.SL_ERR_INVALID_ARG, bad
+
+
+def test_tensor_checks_refuse_with_a_message(lib):
+    """The compiled checks: None passes through, everything that is not a fitting CUDA tensor raises SlError, nothing aborts."""
+    import torch
+    from paper_2508_15706_b200 import binding as B, inner
+    f32 = torch.float32
+    assert inner._ptr(None, 0, 4, f32, "x") is None and inner._rows(None, 0, 2, 2, f32, "x") == (None, 0)
+    q = torch.zeros(1, 2, 3, 4)
+    for bad in (torch.zeros(2, 2), torch.zeros(2, 2).to_sparse(), torch.zeros(2, 2, device="meta"), 7, "x", [1.0]):
+        for call in (lambda: inner._ptr(bad, 0, 4, f32, "x"), lambda: inner._rows(bad, 0, 2, 2, f32, "x"), lambda: inner._heads(bad, q, 0, 1, 2, 4, f32, "x"),
+                     lambda: inner._ptr(bad, -1, 4, f32, "x"), lambda: inner._rows(bad, -1, 2, 2, f32, "x"), lambda: inner._ptr(bad, 0, 4, "float", "x")):
+            with pytest.raises(B.SlError) as e:
+                call()
+            assert e.value.status == B.SL_ERR_INVALID_ARG and "x must be a" in str(e.value)
+    with pytest.raises(TypeError):
+        inner._ptr(None, 0)
+    with pytest.raises(TypeError):
+        inner._rows(torch.zeros(2, 2), "0", 2, 2, f32, "x")
