@@ -257,6 +257,7 @@ norm_forward_kernel(const NormArgs a) {
     }
     T* y = static_cast<T*>(a.y) + (a.y ? row * a.ld_y + norm_column<VEC>(0) : 0);
     T* h = static_cast<T*>(a.h) + (a.h ? row * a.ld_h + norm_column<VEC>(0) : 0);
+    int turn = 0;  // of the exchanges, one or two in a row
     for (unsigned at = 0; row < a.rows; row += stride) {
         if (kFew) {
             fetch(at ? at - stage_bytes : ring_bytes - stage_bytes);
@@ -272,7 +273,8 @@ norm_forward_kernel(const NormArgs a) {
 #pragma unroll
                 for (int i = 0; i < P; ++i) q = fma2(z[i], z[i], q);
                 float s[1] = {q.x + q.y};
-                row_sums<1>(s, sums[0]);
+                row_sums<1>(s, sums[turn]);
+                turn ^= 1;
                 rb = reciprocal_root(fmaf(s[0], a.inv_cols, a.eps));
                 if (a.branch_rstd && threadIdx.x == 0) a.branch_rstd[row] = rb;
             }
@@ -296,7 +298,8 @@ norm_forward_kernel(const NormArgs a) {
 #pragma unroll
         for (int i = 0; i < P; ++i) q = fma2(v[i], v[i], q);  // (0 beyond the row's end)
         float s[1] = {q.x + q.y};
-        row_sums<1>(s, sums[1]);
+        row_sums<1>(s, sums[turn]);
+        turn ^= 1;
         const float r = reciprocal_root(fmaf(s[0], a.inv_cols, a.eps));
         if (a.rstd && threadIdx.x == 0) a.rstd[row] = r;
         if (!kFew) norm_weights<W, VEC, NV>(a.weight, nullptr, pieces, w);
@@ -626,6 +629,7 @@ norm_forward_team_kernel(const NormArgs a) {
     const unsigned mine = weights + threadIdx.x * 16u, plane = (unsigned)team_width<TEAM>() * 16u;  // this thread's weights: piece i at mine + 2 i plane
     T* y = static_cast<T*>(a.y) + (a.y ? row * a.ld_y + threadIdx.x * kFirst : 0);
     T* h = static_cast<T*>(a.h) + (a.h ? row * a.ld_h + threadIdx.x * kFirst : 0);
+    int turn = 0;  // of the exchanges, one or two in a row
     for (unsigned at = 0; row < a.rows; row += stride) {
         fetch(at ? at - stage_bytes : ring_bytes - stage_bytes);
         copy_wait(a.stages - 1);
@@ -641,7 +645,8 @@ norm_forward_team_kernel(const NormArgs a) {
                     for (int j = 0; j < 4; ++j) q = fma2(z[j], z[j], q);
                 }
                 float s[1] = {q.x + q.y};
-                team_sums<1, TEAM>(s, sums[0]);
+                team_sums<1, TEAM>(s, sums[turn]);
+                turn ^= 1;
                 rb = reciprocal_root(fmaf(s[0], a.inv_cols, a.eps));
                 if (a.branch_rstd && threadIdx.x == 0) a.branch_rstd[row] = rb;
                 q = both(0.0f);
@@ -674,7 +679,8 @@ norm_forward_team_kernel(const NormArgs a) {
         at = at + stage_bytes == ring_bytes ? 0u : at + stage_bytes;
         if (!a.h) continue;
         float s[1] = {q.x + q.y};
-        team_sums<1, TEAM>(s, sums[1]);
+        team_sums<1, TEAM>(s, sums[turn]);
+        turn ^= 1;
         const float r = reciprocal_root(fmaf(s[0], a.inv_cols, a.eps));
         if (a.rstd && threadIdx.x == 0) a.rstd[row] = r;
 #pragma unroll
