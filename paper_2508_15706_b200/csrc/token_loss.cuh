@@ -365,7 +365,9 @@ loss_row_kernel(const LossArgs a, const T* logits, T* grad, int cluster) {
         if (!grad) {
         } else if (r.has_gradient()) {
             const float k = r.factor(a, w), off = off_all, hit = w * (1.0f - a.smoothing);
-            const float2 k2 = both(k * exp2_fast(ref - r.m)), off2 = both(-off);             // (from the thread's maximum to the row's)
+            // from the thread's maximum to the row's, which is not below it; a thread of nothing but -inf has ref 0 in place of a
+            // maximum, and its exponentials, all 0, want a finite factor wherever the row's maximum lies
+            const float2 k2 = both(k * exp2_fast(fminf(ref - r.m, 0.0f))), off2 = both(-off);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 float2 q[VEC / 2];
