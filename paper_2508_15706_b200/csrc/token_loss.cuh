@@ -5,8 +5,10 @@
 // registers until the row's maximum and sum are known, and the gradient is those times one factor per thread: one exponential per
 // logit.  (Computed a second time instead, with the row's bits in registers, they bound the kernel: 318 us at 8192 x 32000.)
 // Exponentials are 2^(x log2 e - M), one fused multiply-add and one instruction: M stands for the maximum in that scale, and its
-// rounding moves nothing as long as it is the same M everywhere.  Where |x log2 e| could overflow (a row of the type's lowest
-// value) the factor is 1 instead: numbers of that size are equal or differ by more than any exponential can show.
+// rounding moves nothing as long as it is the same M everywhere and is small beside an exponential's range: up to 2^30, where it is
+// 64 at most.  Beyond (a mask of -1e10, a row of the type's lowest value) the factor is 1 instead: numbers of that size are equal
+// or 64 and more apart, and 2^-64 is nothing in a sum.  Maxima are compared as M / 2 and, beyond 2^30, as they are: an order that
+// is theirs on both sides of 2^30 and passes no number's range.
 // Rows that eight CTAs cannot hold, and gradients that sit elsewhere relative to 16 bytes than their logits, go through a kernel that
 // reads the row twice (the second time from L2).
 #pragma once
@@ -64,17 +66,22 @@ __device__ __forceinline__ float exp2_fast(float x) {  // 2^x, relative error 2^
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-__device__ __forceinline__ float loss_scale(float top) { return fabsf(top) < 1e30f ? kLog2e : 1.0f; }  // (1 for infinities)
+constexpr float kLossFar = 1073741824.0f;  // 2^30
+__device__ __forceinline__ float loss_scale(float top) { return fabsf(top) < kLossFar ? kLog2e : 1.0f; }  // (1 for infinities)
 __device__ __forceinline__ float loss_offset(float top) { return top == -INFINITY ? 0.0f : top * loss_scale(top); }
+// The rank of a maximum: half of its offset, or, beyond 2^30, the maximum itself.  `lift` is what sums relative to `from` are
+// multiplied with to be relative to `to`: 2 to the difference of the offsets.
+__device__ __forceinline__ float loss_rank(float top) { return fabsf(top) < kLossFar ? 0.5f * (top * kLog2e) : top; }
+__device__ __forceinline__ float lift(float from, float to) { return exp2_fast((from - to) + (from - to)); }
 
-// Scaled maximum and sum of exponentials relative to it; -inf with 0 = nothing seen, NaN and +inf end in the sum.
+// Rank of the maximum and sum of exponentials relative to it; -inf with 0 = nothing seen, NaN and +inf end in the sum.
 __device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
     const float top = fmaxf(m, m2);
     if (top == -INFINITY) {
         s += s2;
         return;
     }
-    s = s * exp2_fast(m - top) + s2 * exp2_fast(m2 - top);
+    s = s * lift(m, top) + s2 * lift(m2, top);
     m = top;
 }
 
@@ -83,21 +90,22 @@ __device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
 __device__ __forceinline__ void block_join(float& m, float& s, float& sum, bool with_sum, float (*buf)[32]) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     float top = warp_max(m);
-    s = top == -INFINITY ? warp_sum(s) : warp_sum(s * exp2_fast(m - top));
+    s = top == -INFINITY ? warp_sum(s) : warp_sum(s * lift(m, top));
     if (with_sum) sum = warp_sum(sum);
     if (lane == 0) buf[0][warp] = top, buf[1][warp] = s, buf[2][warp] = sum;
     __syncthreads();
     m = lane < warps ? buf[0][lane] : -INFINITY;
     s = lane < warps ? buf[1][lane] : 0.0f;
     top = warp_max(m);
-    s = top == -INFINITY ? warp_sum(s) : warp_sum(s * exp2_fast(m - top));
+    s = top == -INFINITY ? warp_sum(s) : warp_sum(s * lift(m, top));
     if (with_sum) sum = warp_sum(lane < warps ? buf[2][lane] : 0.0f);
     m = top;
 }
 
 // What a row comes to, from its maximum, sum and target.
 struct LossRow {
-    float m, s, sum, scale;
+    float m, s, sum;   // m: the maximum's rank
+    float scale, ref;  // exponentials are 2^(x scale - ref)
     long long target;
     bool counts, inside, empty;
     __device__ __forceinline__ bool has_gradient() const { return counts && inside && !empty; }
@@ -108,11 +116,12 @@ struct LossRow {
     }
     __device__ __forceinline__ void finish() {
         empty = m == -INFINITY && s == 0.0f;  // every logit is -inf
-        scale = fabsf(m) < 1e30f ? kLog2e : 1.0f;
+        scale = loss_scale(m);  // (the rank of a maximum below 2^30 is below 2^30)
+        ref = scale == 1.0f ? m : m + m;
     }
-    __device__ __forceinline__ float lse() const { return empty ? -INFINITY : scale == 1.0f ? m + logf(s) : (m + log2f(s)) * kLn2; }
+    __device__ __forceinline__ float lse() const { return empty ? -INFINITY : scale == 1.0f ? ref + logf(s) : (ref + log2f(s)) * kLn2; }
     // ... within 2^-21 of it or so: what the gradient's factor of p needs
-    __device__ __forceinline__ float near_lse() const { return scale == 1.0f ? m + __logf(s) : (m + __log2f(s)) * kLn2; }
+    __device__ __forceinline__ float near_lse() const { return scale == 1.0f ? ref + __logf(s) : (ref + __log2f(s)) * kLn2; }
     __device__ __forceinline__ float factor(const LossArgs& a, float w) const { return __fdividef(a.z == 0.0f ? w : w * fmaf(2.0f * a.z, near_lse(), 1.0f), s); }
 };
 // 1 / (rows that count), or 1, times the caller's scale; the count comes from the kernel before
@@ -277,7 +286,7 @@ loss_row_kernel(const LossArgs a, const T* logits, T* grad, int cluster) {
         const LossPart<T, VEC, RAGGED> part(a, x, rank, cluster);
         const int before = part.before(rank), behind = part.behind(a, rank, cluster);
         const bool last_too = (NV - 1) * threads + tid < part.vectors;
-        float m = -INFINITY, s, sum = 0.0f, ref;
+        float m = -INFINITY, s, sum = 0.0f, rank_own;
         float2 e[NV][VEC / 2];
         arrived = arrived && bulk_wait(landed_at + stage * 8u, phase);
         LossRow r;
@@ -306,8 +315,7 @@ loss_row_kernel(const LossArgs a, const T* logits, T* grad, int cluster) {
                     xts[turn] = widen(own);
                 }
             }
-            const float scale = loss_scale(m);
-            ref = loss_offset(m);
+            const float scale = loss_scale(m), ref = loss_offset(m);
             s = exp2_fast(fmaf(first, scale, -ref)) + exp2_fast(fmaf(last_one, scale, -ref));
             if (a.smoothing != 0.0f) {
                 sum = (before >= 0 ? first : 0.0f) + (behind >= 0 ? last_one : 0.0f);
@@ -334,7 +342,7 @@ loss_row_kernel(const LossArgs a, const T* logits, T* grad, int cluster) {
             }
             acc[0] = add2(acc[0], acc[1]);
             s += acc[0].x + acc[0].y;
-            m *= scale;
+            m = rank_own = loss_rank(m);
             if (!arrived) s = __int_as_float(0x7FC00000);
         }
         block_join(m, s, sum, a.smoothing != 0.0f, buf[turn]);
@@ -365,9 +373,8 @@ loss_row_kernel(const LossArgs a, const T* logits, T* grad, int cluster) {
         if (!grad) {
         } else if (r.has_gradient()) {
             const float k = r.factor(a, w), off = off_all, hit = w * (1.0f - a.smoothing);
-            // from the thread's maximum to the row's, which is not below it; a thread of nothing but -inf has ref 0 in place of a
-            // maximum, and its exponentials, all 0, want a finite factor wherever the row's maximum lies
-            const float2 k2 = both(k * exp2_fast(fminf(ref - r.m, 0.0f))), off2 = both(-off);
+            // from the thread's maximum to the row's, which is not below it (a thread of nothing but -inf: 0)
+            const float2 k2 = both(k * lift(rank_own, r.m)), off2 = both(-off);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 float2 q[VEC / 2];
@@ -388,7 +395,7 @@ loss_row_kernel(const LossArgs a, const T* logits, T* grad, int cluster) {
                 }
             }
             auto one = [&](int i) {
-                const float d = fmaf(k, exp2_fast(fmaf(widen(x[i]), r.scale, -r.m)), -off);
+                const float d = fmaf(k, exp2_fast(fmaf(widen(x[i]), r.scale, -r.ref)), -off);
                 g[i] = narrow<T>(i == (int)r.target ? d - hit : d);
             };
             if (before >= 0) one(before);
@@ -430,14 +437,13 @@ loss_stream_kernel(const LossArgs a, const T* logits, T* grad) {
     LossRow r;
     r.aim(a, target_of(a, row));
     float m = -INFINITY, s = 0.0f, sum = 0.0f;
-    float scale = kLog2e, ref = 0.0f;           // m in the scale of the exponentials
+    float scale = kLog2e, ref = 0.0f;           // of the exponentials
     auto rise = [&](float top) {                // the maximum so far goes up to top
         if (top > m) {
-            const float to = loss_offset(top);
-            s *= exp2_fast(m == -INFINITY ? m : ref - to);
+            s *= lift(loss_rank(m), loss_rank(top));
             m = top;
             scale = loss_scale(top);
-            ref = to;
+            ref = loss_offset(top);
         }
     };
     auto see = [&](float v) {
@@ -458,7 +464,7 @@ loss_stream_kernel(const LossArgs a, const T* logits, T* grad) {
         for (int j = 0; j < VEC; ++j) see(f[j]);
     }
     for (int i = rest + tid; i < a.vocab; i += kLossThreads) rise(widen(x[i])), see(widen(x[i]));
-    m = m == -INFINITY ? m : ref;
+    m = loss_rank(m);
     const float xt = r.counts && r.inside ? widen(x[r.target]) : 0.0f;  // (read before any thread writes a gradient in its place)
     block_join(m, s, sum, true, buf);
     r.m = m, r.s = s, r.sum = sum;
@@ -472,7 +478,7 @@ loss_stream_kernel(const LossArgs a, const T* logits, T* grad) {
         const float k = some ? r.factor(a, w) : 0.0f, off = w * a.smoothing / (float)a.vocab, hit = w * (1.0f - a.smoothing);
         auto of = [&](float v, int i) {
             if (!some) return 0.0f;
-            const float d = fmaf(k, exp2_fast(fmaf(v, r.scale, -r.m)), -off);
+            const float d = fmaf(k, exp2_fast(fmaf(v, r.scale, -r.ref)), -off);
             return i == (int)r.target ? d - hit : d;
         };
         for (int i = tid; i < head; i += kLossThreads) g[i] = narrow<T>(of(widen(x[i]), i));
