@@ -119,8 +119,15 @@ struct LossRow {
         scale = loss_scale(m);  // (the rank of a maximum below 2^30 is below 2^30)
         ref = scale == 1.0f ? m : m + m;
     }
-    __device__ __forceinline__ float lse() const { return empty ? -INFINITY : scale == 1.0f ? ref + logf(s) : (ref + log2f(s)) * kLn2; }
-    // ... within 2^-21 of it or so: what the gradient's factor of p needs
+    __device__ __forceinline__ float log_sum() const { return scale == 1.0f ? logf(s) : log2f(s); }
+    __device__ __forceinline__ float lse(float log_s) const { return empty ? -INFINITY : scale == 1.0f ? ref + log_s : (ref + log_s) * kLn2; }
+    // lse - x for a logit x (or their mean): from the parts, since lse is rounded at its own size, which may be any.  The rounding of
+    // ref is in s and in ref - x log2 e alike and goes out between them.  What is below 2^-21, twice the accuracy of an exponential, is 0.
+    __device__ __forceinline__ float above(float x, float log_s) const {
+        const float d = scale == 1.0f ? ref - x + log_s : fabsf(x) < kLossFar ? (log_s + fmaf(-x, scale, ref)) * kLn2 : lse(log_s) - x;
+        return d < 4.76837158203125e-7f ? 0.0f : d;  // (NaN stays)
+    }
+    // ... within 2^-21 of lse or so: what the gradient's factor of p needs
     __device__ __forceinline__ float near_lse() const { return scale == 1.0f ? ref + __logf(s) : (ref + __log2f(s)) * kLn2; }
     __device__ __forceinline__ float factor(const LossArgs& a, float w) const { return __fdividef(a.z == 0.0f ? w : w * fmaf(2.0f * a.z, near_lse(), 1.0f), s); }
 };
@@ -132,13 +139,14 @@ __device__ __forceinline__ float row_weight(const LossArgs& a, int& valid) {
 }
 __device__ __forceinline__ void write_row(const LossArgs& a, const LossRow& r, long long row, float xt) {
     float loss = 0.0f;
-    const float lse = r.lse();
+    const float log_s = r.log_sum(), lse = r.lse(log_s);
     if (r.counts) {
         if (!r.inside) loss = __int_as_float(0x7FC00000);
         else if (r.empty) loss = INFINITY;
         else {
-            loss = lse - (1.0f - a.smoothing) * xt + a.z * lse * lse;
-            if (a.smoothing != 0.0f) loss -= a.smoothing * (r.sum / (float)a.vocab);
+            loss = a.z == 0.0f ? 0.0f : a.z * lse * lse;
+            if (a.smoothing != 1.0f) loss += (1.0f - a.smoothing) * r.above(xt, log_s);
+            if (a.smoothing != 0.0f) loss += a.smoothing * r.above(r.sum / (float)a.vocab, log_s);
         }
     }
     a.row_loss[row] = loss;
@@ -436,7 +444,9 @@ loss_stream_kernel(const LossArgs a, const T* logits, T* grad) {
     const int rest = head + body * VEC;                     // scalars from here on
     LossRow r;
     r.aim(a, target_of(a, row));
-    float m = -INFINITY, s = 0.0f, sum = 0.0f;
+    const bool smoothed = a.smoothing != 0.0f;
+    float m = -INFINITY, s = 0.0f;
+    double logits_sum = 0.0;                    // (hundreds of terms a thread)
     float scale = kLog2e, ref = 0.0f;           // of the exponentials
     auto rise = [&](float top) {                // the maximum so far goes up to top
         if (top > m) {
@@ -447,10 +457,14 @@ loss_stream_kernel(const LossArgs a, const T* logits, T* grad) {
         }
     };
     auto see = [&](float v) {
-        sum += v;
         s += exp2_fast(fmaf(v, scale, -ref));   // (0 for -inf; NaN and +inf end here and stay in the sum)
     };
-    for (int i = tid; i < head; i += kLossThreads) rise(widen(x[i])), see(widen(x[i]));
+    auto one = [&](float v) {
+        rise(v);
+        see(v);
+        if (smoothed) logits_sum += v;
+    };
+    for (int i = tid; i < head; i += kLossThreads) one(widen(x[i]));
     for (int i = tid; i < body; i += kLossThreads) {
         Pack<T, VEC> p;
         p.load(x + head + i * VEC);
@@ -462,8 +476,15 @@ loss_stream_kernel(const LossArgs a, const T* logits, T* grad) {
         rise(top);
 #pragma unroll
         for (int j = 0; j < VEC; ++j) see(f[j]);
+        if (smoothed) {
+            float part = f[0];
+#pragma unroll
+            for (int j = 1; j < VEC; ++j) part += f[j];
+            logits_sum += part;
+        }
     }
-    for (int i = rest + tid; i < a.vocab; i += kLossThreads) rise(widen(x[i])), see(widen(x[i]));
+    for (int i = rest + tid; i < a.vocab; i += kLossThreads) one(widen(x[i]));
+    float sum = (float)logits_sum;
     m = loss_rank(m);
     const float xt = r.counts && r.inside ? widen(x[r.target]) : 0.0f;  // (read before any thread writes a gradient in its place)
     block_join(m, s, sum, true, buf);
