@@ -543,6 +543,11 @@ typedef struct {
 size_t sl_loss_workspace_bytes(void);
 sl_status sl_token_loss(const sl_loss_desc* d, const void* logits, const void* targets, void* grad, float* row_loss, float* lse,
                         float* total, void* workspace, size_t workspace_bytes, void* cuda_stream);
+/* The loss's backward pass under a framework that differentiates: out = upstream[0] * grad, n contiguous elements of `dtype`,
+ * products in fp32 rounded once.  upstream: one fp32 on the device.  out may be grad.  (A factor that is known beforehand belongs into
+ * `scale`, which acts before the gradient's only rounding.)
+ * Errors: INVALID_ARG, ALIGNMENT (a pointer off its element size), UNSUPPORTED (dtype), TOO_LARGE (n > 2^40), CUDA. */
+sl_status sl_token_loss_backward(int32_t dtype, int64_t n, const void* grad, const float* upstream, void* out, void* cuda_stream);
 
 const char* sl_strerror(sl_status s);
 const char* sl_last_cuda_error(void); /* text of the last CUDA error seen by this thread */

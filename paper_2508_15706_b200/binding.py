@@ -24,7 +24,7 @@ EXPORTS = (
     # the inner phase (wrapped in inner.py)
     "sl_adamw_create", "sl_adamw_destroy", "sl_adamw_sizes", "sl_adamw_step", "sl_adamw_read_state", "sl_adamw_write_state",
     "sl_norm_forward", "sl_norm_workspace_bytes", "sl_norm_backward", "sl_rotary_create", "sl_rotary_destroy", "sl_rotary_apply",
-    "sl_loss_workspace_bytes", "sl_token_loss",
+    "sl_loss_workspace_bytes", "sl_token_loss", "sl_token_loss_backward",
 )
 PROFILE_SLOTS = 9
 

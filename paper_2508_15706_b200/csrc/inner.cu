@@ -159,6 +159,18 @@ sl_status launch_loss(const LossArgs& a, const T* logits, T* grad, bool same, in
     return ragged ? launch_loss_nv<T, true>(a, logits, grad, nv, threads, cluster, n_sms, st) : launch_loss_nv<T, false>(a, logits, grad, nv, threads, cluster, n_sms, st);
 }
 
+template <class T>
+sl_status launch_loss_backward(const T* grad, const float* upstream, T* out, long long n, cudaStream_t st) {
+    constexpr int V = 16 / (int)sizeof(T);
+    const bool whole = fits(grad, 16) && fits(out, 16);
+    const long long items = whole ? std::max(1ll, n / V) : n, per = (long long)kUpThreads * kUpVectors;
+    const unsigned grid = (unsigned)((items + per - 1) / per);
+    if (whole) loss_backward_kernel<T, V><<<grid, kUpThreads, 0, st>>>(grad, upstream, out, n);
+    else loss_backward_kernel<T, 1><<<grid, kUpThreads, 0, st>>>(grad, upstream, out, n);
+    SL_CUDA(cudaGetLastError());
+    return SL_OK;
+}
+
 bool overlaps_no(const sl_tensor_desc* tensors, int n) {
     std::vector<std::pair<long long, long long>> span((size_t)n);
     for (int j = 0; j < n; ++j) span[(size_t)j] = {(long long)tensors[j].offset, (long long)tensors[j].offset + tensors[j].rows * tensors[j].cols};
@@ -510,6 +522,17 @@ sl_status sl_token_loss(const sl_loss_desc* d, const void* logits, const void* t
     sl_status s = sm_count(&n_sms);
     if (s != SL_OK) return s;
     return d->dtype == SL_F32 ? launch_loss<float>(a, (const float*)logits, (float*)grad, same, n_sms, st) : launch_loss<bf16>(a, (const bf16*)logits, (bf16*)grad, same, n_sms, st);
+}
+
+sl_status sl_token_loss_backward(int32_t dtype, int64_t n, const void* grad, const float* upstream, void* out, void* stream) {
+    if (n < 0 || (n > 0 && (!grad || !upstream || !out))) return SL_ERR_INVALID_ARG;
+    if (!known_dtype(dtype)) return SL_ERR_UNSUPPORTED;
+    if (n > (1ll << 40)) return SL_ERR_TOO_LARGE;
+    const int bytes = dtype_bytes(dtype);
+    if (!fits(grad, bytes) || !fits(out, bytes) || !fits(upstream, 4)) return SL_ERR_ALIGNMENT;
+    if (n == 0) return SL_OK;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return dtype == SL_F32 ? launch_loss_backward<float>((const float*)grad, upstream, (float*)out, n, st) : launch_loss_backward<bf16>((const bf16*)grad, upstream, (bf16*)out, n, st);
 }
 
 }  // extern "C"

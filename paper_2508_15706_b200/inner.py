@@ -66,6 +66,7 @@ _L.sl_rotary_destroy.argtypes = [P]
 _L.sl_rotary_apply.argtypes = [P, P, P, P, P, P]
 _L.sl_loss_workspace_bytes.restype = C.c_size_t
 _L.sl_token_loss.argtypes = [P] * 8 + [C.c_size_t, P]
+_L.sl_token_loss_backward.argtypes = [I32, I64, P, P, P, P]
 
 
 def _refuse(what: str):
@@ -398,18 +399,22 @@ def token_loss(logits, targets, *, grad=None, ignore_index: int = -100, smoothin
 
 class _NextTokenLoss(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, logits, targets, ignore_index, smoothing, z):
+    def forward(ctx, logits, targets, ignore_index, smoothing, z, scale):
         grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device) if ctx.needs_input_grad[0] else None
-        total, _, _ = token_loss(logits, targets, grad=grad, ignore_index=ignore_index, smoothing=smoothing, z=z)
+        total, _, _ = token_loss(logits, targets, grad=grad, ignore_index=ignore_index, smoothing=smoothing, z=z, scale=scale)
         ctx.save_for_backward(grad)
         return total.view(())
 
     @staticmethod
     def backward(ctx, d):
         (grad,) = ctx.saved_tensors
-        return grad * d.to(grad.dtype), None, None, None, None
+        dev, out = _here(), torch.empty_like(grad)
+        _check(_L.sl_token_loss_backward(_dtype(grad.dtype), grad.numel(), grad.data_ptr(), _ptr(d, dev, 1, torch.float32, "the loss's gradient"), out.data_ptr(), _queue(dev)))
+        return out, None, None, None, None, None
 
 
-def next_token_loss(logits, targets, *, ignore_index: int = -100, smoothing: float = 0.0, z: float = 0.0):
-    """Mean loss over the rows that count, under autograd; the gradient is formed in the forward pass."""
-    return _NextTokenLoss.apply(logits.reshape(-1, logits.shape[-1]), targets.reshape(-1), ignore_index, smoothing, z)
+def next_token_loss(logits, targets, *, ignore_index: int = -100, smoothing: float = 0.0, z: float = 0.0, scale: float = 1.0):
+    """Mean loss over the rows that count, times `scale`, under autograd; the gradient is formed in the forward pass.  A factor known
+    beforehand (1 / accumulated micro-batches) belongs into `scale`: a bfloat16 gradient is then rounded once, by
+    `(loss * factor).backward()` twice."""
+    return _NextTokenLoss.apply(logits.reshape(-1, logits.shape[-1]), targets.reshape(-1), ignore_index, smoothing, z, scale)
