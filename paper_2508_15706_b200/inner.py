@@ -4,7 +4,7 @@ positions and the next-token loss.  Wrappers over libsparseloco's C entry points
 Two layers.  `AdamW`, `Rotary`, `norm_forward` / `norm_backward` and `token_loss` marshal arguments only: buffers are the
 caller's (allocated here where an output is left out), work goes on torch's current stream, nothing synchronises.
 `block_norm`, `rotary` and `next_token_loss` are the same operators as autograd functions, for a model that runs under
-torch's autograd.
+torch's autograd.  Their backward passes are kernels without derivatives of their own: a second derivative raises.
 """
 from __future__ import annotations
 
@@ -13,6 +13,7 @@ import struct
 from typing import Optional, Sequence
 
 import torch
+from torch.autograd.function import once_differentiable
 
 try:
     from . import _checks
@@ -272,6 +273,7 @@ class _BlockNorm(torch.autograd.Function):
         return y, h
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy, dh):
         y, branch, weight, branch_weight, gate, rstd, brstd = ctx.saved_tensors
         need = ctx.needs_input_grad
@@ -355,6 +357,7 @@ class _Turn(torch.autograd.Function):
         return out_q, out_k
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dq, dk):
         out_q, out_k = torch.empty(dq.shape, dtype=dq.dtype, device=dq.device), torch.empty(dk.shape, dtype=dk.dtype, device=dk.device)
         dq, dk = (t if t.stride(-1) == 1 else t.contiguous() for t in (dq, dk))
@@ -406,6 +409,7 @@ class _NextTokenLoss(torch.autograd.Function):
         return total.view(())
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, d):
         (grad,) = ctx.saved_tensors
         dev, out = _here(), torch.empty_like(grad)
