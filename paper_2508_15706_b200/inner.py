@@ -352,21 +352,21 @@ class _Turn(torch.autograd.Function):
     def forward(ctx, q, k, rope, positions, first):
         ctx.rope, ctx.first = rope, first
         ctx.save_for_backward(positions)
-        out_q, out_k = torch.empty(q.shape, dtype=q.dtype, device=q.device), torch.empty(k.shape, dtype=k.dtype, device=k.device)
-        rope.apply(q, k, positions, first=first, out_q=out_q, out_k=out_k)
-        return out_q, out_k
+        out = [None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k)]
+        rope.apply(q, k, positions, first=first, out_q=out[0], out_k=out[1])
+        return tuple(out)
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dq, dk):
-        out_q, out_k = torch.empty(dq.shape, dtype=dq.dtype, device=dq.device), torch.empty(dk.shape, dtype=dk.dtype, device=dk.device)
-        dq, dk = (t if t.stride(-1) == 1 else t.contiguous() for t in (dq, dk))
-        ctx.rope.apply(dq, dk, ctx.saved_tensors[0], first=ctx.first, inverse=True, out_q=out_q, out_k=out_k)
-        return out_q, out_k, None, None, None
+        out = [None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (dq, dk)]
+        dq, dk = (t if t is None or t.stride(-1) == 1 else t.contiguous() for t in (dq, dk))
+        ctx.rope.apply(dq, dk, ctx.saved_tensors[0], first=ctx.first, inverse=True, out_q=out[0], out_k=out[1])
+        return (*out, None, None, None)
 
 
-def rotary(rope: Rotary, q, k, positions=None, *, first: int = 0):
-    """`rope.apply` under autograd: new q and k."""
+def rotary(rope: Rotary, q, k=None, positions=None, *, first: int = 0):
+    """`rope.apply` under autograd: new q and k (None without k)."""
     return _Turn.apply(q, k, rope, positions, first)
 
 
