@@ -172,6 +172,13 @@ class AdamW:
         _check(_L.sl_adamw_write_state(self._h, _ptr(m_in, dev, n, torch.float32, "m_in"), _ptr(v_in, dev, n, torch.float32, "v_in"), pm, pv, ps, seed & 0xFFFFFFFF, _queue(dev)))
 
 
+def _laid_out(t):
+    """A matrix as the kernels take it, unit column stride and rows apart: itself, or (transposed, expanded) a copy."""
+    if t is None or ((t.shape[1] <= 1 or t.stride(1) == 1) and (t.shape[0] <= 1 or t.stride(0) >= t.shape[1])):
+        return t
+    return t.contiguous()
+
+
 # ------------------------------------------------------------------------------------------------------------- norms
 def _gate(gate, dev, rows, cols, act, wt):
     """(kind, address, stride): [cols] = per column, [rows, 1] or (rows != cols) [rows] = per row, [rows, cols] = per element."""
@@ -291,12 +298,13 @@ class _BlockNorm(torch.autograd.Function):
 
 
 def block_norm(x, weight=None, *, branch=None, branch_weight=None, gate=None, alpha: float = 1.0, eps: float = 1e-6):
-    """(y, h) of `norm_forward` under autograd, on [..., cols] activations; a gate is [cols], [..., 1] or [..., cols]."""
+    """(y, h) of `norm_forward` under autograd, on [..., cols] activations of any strides; a gate is [cols], [..., 1] or [..., cols]."""
     shape = x.shape
-    flat = [None if t is None else t.reshape(-1, shape[-1]) for t in (x, branch)]
-    if gate is not None and gate.dim() > 1:
-        gate = gate.reshape(-1, gate.shape[-1])
-    y, h = _BlockNorm.apply(flat[0], flat[1], weight, branch_weight, gate, alpha, eps)
+    flat = [None if t is None else _laid_out(t.reshape(-1, shape[-1])) for t in (x, branch)]
+    if gate is not None:
+        gate = gate.contiguous() if gate.dim() < 2 else _laid_out(gate.reshape(-1, gate.shape[-1]))
+    vectors = [None if t is None else t.contiguous() for t in (weight, branch_weight)]
+    y, h = _BlockNorm.apply(flat[0], flat[1], vectors[0], vectors[1], gate, alpha, eps)
     return y.view(shape), h.view(shape)
 
 
@@ -366,7 +374,8 @@ class _Turn(torch.autograd.Function):
 
 
 def rotary(rope: Rotary, q, k=None, positions=None, *, first: int = 0):
-    """`rope.apply` under autograd: new q and k (None without k)."""
+    """`rope.apply` under autograd, for any strides: new q and k (None without k)."""
+    q, k = (t if t is None or t.stride(-1) == 1 else t.contiguous() for t in (q, k))
     return _Turn.apply(q, k, rope, positions, first)
 
 
@@ -421,4 +430,4 @@ def next_token_loss(logits, targets, *, ignore_index: int = -100, smoothing: flo
     """Mean loss over the rows that count, times `scale`, under autograd; the gradient is formed in the forward pass.  A factor known
     beforehand (1 / accumulated micro-batches) belongs into `scale`: a bfloat16 gradient is then rounded once, by
     `(loss * factor).backward()` twice."""
-    return _NextTokenLoss.apply(logits.reshape(-1, logits.shape[-1]), targets.reshape(-1), ignore_index, smoothing, z, scale)
+    return _NextTokenLoss.apply(_laid_out(logits.reshape(-1, logits.shape[-1])), targets.reshape(-1).contiguous(), ignore_index, smoothing, z, scale)
