@@ -399,9 +399,9 @@ def token_loss(logits, targets, *, grad=None, ignore_index: int = -100, smoothin
     pt = _ptr(targets, dev, rows, targets.dtype, "targets")
     px, ld_x = _rows(logits, dev, rows, vocab, act, "logits")
     pg, ld_g = _rows(grad, dev, rows, vocab, act, "grad")
-    row_loss = torch.empty(rows, device=logits.device) if row_loss is None else row_loss
-    lse = torch.empty(rows, device=logits.device) if lse is None else lse
-    total = torch.empty(1, device=logits.device) if total is None else total
+    row_loss = torch.empty(rows, dtype=torch.float32, device=logits.device) if row_loss is None else row_loss
+    lse = torch.empty(rows, dtype=torch.float32, device=logits.device) if lse is None else lse
+    total = torch.empty(1, dtype=torch.float32, device=logits.device) if total is None else total
     workspace = loss_workspace() if workspace is None else workspace
     d = _loss_bytes(rows, vocab, _dtype(act), bits, ld_x, ld_g, ignore_index, smoothing, z, scale, mean)
     _check(_L.sl_token_loss(d, px, pt, pg, _ptr(row_loss, dev, rows, torch.float32, "row_loss"), _ptr(lse, dev, rows, torch.float32, "lse"),
