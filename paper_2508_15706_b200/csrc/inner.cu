@@ -420,6 +420,11 @@ sl_status sl_rotary_apply(sl_rotary* c, const sl_rotary_desc* d, const sl_rotary
     if (d->head_dim > 65536 || d->seq > 0x7FFFFFFFll || d->batch > 0x7FFFFFFFll || d->batch * d->seq > 0x7FFFFFFFll || q->heads > 65536 ||
         k->heads > 65536 || (q->heads + k->heads) * d->head_dim > (1ll << 27))
         return SL_ERR_TOO_LARGE;
+    for (const sl_rotary_heads* h : {q, k}) {  // in place means the very same elements: dimensions of one element may have any stride
+        const int64_t extent[] = {d->batch, d->seq, h->heads}, in[] = {h->in_batch, h->in_token, h->in_head}, out[] = {h->out_batch, h->out_token, h->out_head};
+        for (int i = 0; i < 3; ++i)
+            if (h->in && h->in == h->out && extent[i] > 1 && in[i] != out[i]) return SL_ERR_INVALID_ARG;
+    }
     const int bytes = dtype_bytes(d->dtype), rot = c->cfg.rot_dim;
     const bool half = c->cfg.layout == SL_ROPE_HALF;
     // the widest accesses that every offset of the turned part, and of what is passed through, is a multiple of
