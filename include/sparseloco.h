@@ -493,7 +493,7 @@ sl_status sl_norm_backward(const sl_norm_desc* d, const void* dy, const void* dh
  * inverse != 0 turns by the negative angle: the backward pass (gradients of q and k in, gradients of their inputs out).
  * q and k (k.in NULL: none) are [batch, seq, heads, head_dim] with strides in elements for batch, token and head and a
  * unit stride inside a head; `out` may equal `in` with equal strides (in place; other strides are INVALID_ARG), else the two must
- * not overlap.
+ * not overlap.  An input may be shared along a dimension (stride 0), an output may not (INVALID_ARG), in place neither.
  * positions: int32 or int64 (position_bits 32 / 64) by batch and token stride (a stride of 0 shares one row), or NULL: first + token.
  * Errors: INVALID_ARG, ALIGNMENT (a pointer off its element size), UNSUPPORTED (dtype), TOO_LARGE, CUDA. */
 enum { SL_ROPE_HALF = 0, SL_ROPE_INTERLEAVED = 1 };

@@ -423,7 +423,7 @@ sl_status sl_rotary_apply(sl_rotary* c, const sl_rotary_desc* d, const sl_rotary
     for (const sl_rotary_heads* h : {q, k}) {  // in place means the very same elements: dimensions of one element may have any stride
         const int64_t extent[] = {d->batch, d->seq, h->heads}, in[] = {h->in_batch, h->in_token, h->in_head}, out[] = {h->out_batch, h->out_token, h->out_head};
         for (int i = 0; i < 3; ++i)
-            if (h->in && h->in == h->out && extent[i] > 1 && in[i] != out[i]) return SL_ERR_INVALID_ARG;
+            if (h->in && extent[i] > 1 && ((h->in == h->out && in[i] != out[i]) || out[i] == 0)) return SL_ERR_INVALID_ARG;
     }
     const int bytes = dtype_bytes(d->dtype), rot = c->cfg.rot_dim;
     const bool half = c->cfg.layout == SL_ROPE_HALF;

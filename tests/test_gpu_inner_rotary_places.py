@@ -40,3 +40,22 @@ def test_strides_of_single_elements_do_not_count():
     rope.apply(one, first=3, out_q=(w := torch.empty_like(one)))
     rope.apply(one, first=3, out_q=one.as_strided((1, 1, 1, 16), (1, 2, 3, 1)))
     assert torch.equal(one, w)
+
+
+@pytest.mark.parametrize("dim", [0, 1, 2])
+def test_outputs_shared_along_a_dimension_are_refused(dim):
+    """A key head expanded over the query heads, one token over a sequence: fine as an input, not as what is written."""
+    from paper_2508_15706_b200.inner import Rotary
+    rope = Rotary(16)
+    shape = [2, 5, 4, 16]
+    shape[dim] = 1
+    one = torch.randn(shape, device="cuda")
+    shared, before = one.expand(2, 5, 4, 16), one.clone()
+    refused(rope.apply, shared)
+    refused(rope.apply, shared.contiguous(), shared)
+    refused(rope.apply, shared.contiguous(), out_q=shared)
+    assert torch.equal(one, before)
+    out, want = torch.empty(2, 5, 4, 16, device="cuda"), shared.contiguous()
+    rope.apply(shared, out_q=out)
+    rope.apply(want)
+    assert torch.equal(out, want)
