@@ -453,7 +453,8 @@ sl_status sl_adamw_write_state(sl_adamw* ctx, const float* m_in, const float* v_
  * h is formed from y before y is rounded.  gate: none, one value per column, per row, or per element.
  * x, branch, y, h, their gradients and a row or element gate are `dtype`; the weights, a column gate and their gradients
  * `weight_dtype` (fp32, or bfloat16 with bfloat16 activations).  Every matrix has its own row stride in elements (>= cols;
- * 0 means cols); a row gate is one value per row, its stride 1 (0) or more.  y may be x and h may be branch.
+ * 0 means cols); a row gate is one value per row, its stride 1 (0) or more.  y may be x and h may be branch
+ * (with one row stride: an output at an input's address with another one is INVALID_ARG, here and in the backward pass).
  * Backward, from dy (gradient of y from elsewhere, NULL: none) and dh (NULL: none), with the forward pass's y, rstd (needed with dh)
  * and branch_rstd:
  *     dx = dy + r (dh weight - yhat mean(dh weight yhat)),  yhat = y r

@@ -6,6 +6,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <initializer_list>
 
 #include "sparseloco.h"
 
@@ -211,6 +212,18 @@ struct NormAlign {
     }
 };
 
+// A matrix that is written where another one is read has to be the very same rows: others would be written before they are read.
+struct NormPlace {
+    const void* p;
+    long long ld;
+};
+bool in_place_by_rows(long long rows, std::initializer_list<NormPlace> read, std::initializer_list<NormPlace> written) {
+    for (const NormPlace& w : written)
+        for (const NormPlace& r : read)
+            if (rows > 1 && w.p && w.p == r.p && w.ld != r.ld) return false;
+    return true;
+}
+
 }  // namespace
 
 extern "C" {
@@ -232,6 +245,8 @@ sl_status sl_norm_forward(const sl_norm_desc* d, const void* x, const void* bran
     a.h = h;
     a.branch_rstd = branch_rstd;
     a.rstd = rstd;
+    const bool full = d->gate_kind == SL_GATE_FULL;
+    if (!in_place_by_rows(d->rows, {{x, a.ld_x}, {branch, a.ld_branch}, {full ? gate : nullptr, a.ld_gate}}, {{y, a.ld_y}, {h, a.ld_h}})) return SL_ERR_INVALID_ARG;
     const int wb = dtype_bytes(d->weight_dtype);
     NormAlign al(d);
     al.matrix(x, a.ld_x);
@@ -295,6 +310,10 @@ sl_status sl_norm_backward(const sl_norm_desc* d, const void* dy, const void* dh
     a.dx = dx;
     a.dbranch = dbranch;
     a.dgate = d->gate_kind == SL_GATE_COLUMN ? nullptr : dgate;
+    const bool full = d->gate_kind == SL_GATE_FULL;
+    if (!in_place_by_rows(d->rows, {{dy, a.ld_dy}, {dh, a.ld_dh}, {y, a.ld_y}, {branch, a.ld_branch}, {full ? gate : nullptr, a.ld_gate}},
+                          {{dx, a.ld_x}, {dbranch, a.ld_branch}, {full ? dgate : nullptr, a.ld_gate}}))
+        return SL_ERR_INVALID_ARG;
     const int wb = dtype_bytes(d->weight_dtype);
     NormAlign al(d);
     al.matrix(dy, a.ld_dy);
