@@ -1,6 +1,6 @@
 // The checks that inner.py makes of every tensor it hands to the library, compiled: in Python they cost as much as the rest of a
-// small call.  A Python extension module over torch's C++ tensors; what is wrong is
-// reported through a Python function (`refuse`) that puts the message together.
+// small call.  A Python extension module over torch's C++ tensors; what is wrong is reported through a Python function (`refuse`) that
+// puts the message together.  It reads the objects of one torch and one Python: `built_for` names them, and the package refuses others.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <torch/csrc/Dtype.h>
@@ -143,4 +143,12 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_checks", nullptr, -1, methods, nu
 
 }  // namespace
 
-extern "C" PyObject* PyInit__checks() { return PyModule_Create(&module); }
+#ifndef BUILT_FOR
+#error "BUILT_FOR names the torch and the Python that this is compiled for"
+#endif
+
+extern "C" PyObject* PyInit__checks() {
+    PyObject* m = PyModule_Create(&module);
+    if (m && PyModule_AddStringConstant(m, "built_for", BUILT_FOR) < 0) Py_CLEAR(m);
+    return m;
+}

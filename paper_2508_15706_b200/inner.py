@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import struct
+import sys
 from typing import Optional, Sequence
 
 import torch
@@ -17,8 +18,10 @@ from torch.autograd.function import once_differentiable
 
 try:
     from . import _checks
-except ImportError as e:
-    raise ImportError("the extension _checks.so is missing or was built for another torch: build it with `python -c 'import __graft_entry__ as g; g.build(force=True)'`") from e
+    if _checks.built_for != f"built for torch {torch.__version__} {sys.implementation.cache_tag}":
+        raise ImportError(f"it was {_checks.built_for}")
+except (ImportError, AttributeError) as e:
+    raise ImportError("the extension _checks.so is missing or was built for another torch: build it with `python -c 'import __graft_entry__ as g; g.build()'`") from e
 from .binding import SlError, SL_ERR_INVALID_ARG, _check, _L, _TensorDesc
 
 P, I32, I64, F32, F64 = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_double
