@@ -342,8 +342,10 @@ struct AdamArgs {
     long long blocks;
     float coef, beta1, omb1, beta2, omb2, eps, inv_sqrt_bc2, step_size, lr;
     unsigned seed;
-    int skip;
+    int skip, flush;
 };
+// What counting a denormal v as 0 leaves out of the denominator, up to 2^-63 / sqrt(1 - beta2^t), is below 2^-23 of eps.
+inline bool adamw_may_flush(float eps, float inv_sqrt_bc2) { return eps >= 9.094947017729282e-13f * inv_sqrt_bc2; }  // 2^-40
 
 // The moments are formed by single-rounded operations in the order of the formula, so that the 8-bit codes do not depend
 // on how a compiler contracts them.  (Not by the paired ones: their products and sums are contracted, explicit rounding or not.)
@@ -359,7 +361,7 @@ __device__ __forceinline__ void adamw_element(float& p, float g, float& m, float
     asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
     p = fmaf(-a.step_size, __fdividef(m, fmaf(r, a.inv_sqrt_bc2, a.eps)), fmaf(-decay, p, p));
 }
-// ... for eps >= 1e-15, which hides a sqrt(v) below 2^-63: denormal operands of sqrt and reciprocal may count as 0.
+// ... where eps hides a denormal v, which the root here takes for 0 (AdamArgs::flush).
 __device__ __forceinline__ void adamw_pair(float2& p, float2 g, float2& m, float2& v, const AdamArgs& a, float c, float2 decay) {
     adamw_moments(g.x, m.x, v.x, a, c);
     adamw_moments(g.y, m.y, v.y, a, c);
@@ -434,7 +436,7 @@ adamw_step_kernel(const AdamTile* __restrict__ tiles, const float* __restrict__ 
         x.moments(m, v);
 #pragma unroll
         for (int j = 0; j < kAdamVec; ++j) p[j] = x.p[j];
-        if (a.eps >= 1e-15f) {
+        if (a.flush) {
 #pragma unroll
             for (int j = 0; j < kAdamVec; j += 2) {
                 float2 pp = make_float2(p[j], p[j + 1]), mm = make_float2(m[j], m[j + 1]), vv = make_float2(v[j], v[j + 1]);

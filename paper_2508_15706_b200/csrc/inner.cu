@@ -310,6 +310,7 @@ sl_status sl_adamw_step(sl_adamw* c, void* theta, const void* grad, void* m, voi
     a.omb2 = (float)(1.0 - c->cfg.beta2);
     a.eps = (float)c->cfg.eps;
     a.inv_sqrt_bc2 = (float)(1.0 / sqrt(1.0 - pow(c->cfg.beta2, (double)step)));
+    a.flush = adamw_may_flush(a.eps, a.inv_sqrt_bc2);
     a.step_size = (float)(lr / (1.0 - pow(c->cfg.beta1, (double)step)));
     a.lr = (float)lr;
     a.seed = seed;
