@@ -181,10 +181,17 @@ rotary_kernel(const RopeArgs a) {
                         const long long w = b * a.pos_batch + s * a.pos_token;
                         pos = a.position_bits == 64 ? static_cast<const long long*>(a.positions)[w] : (long long)static_cast<const int*>(a.positions)[w];
                     }
-                    // position * frequency in turns, modulo 1 by the 64-bit product; as half turns in [-1, 1)
-                    const long long phase = (long long)((unsigned long long)pos * a.turns[f]);
+                    // position * frequency in turns, modulo 1 by the 64-bit product; the nearest quarter turn is taken off before
+                    // what is left is rounded to fp32, as half turns in [-1/4, 1/4): sine and cosine stay accurate where they are small
+                    const unsigned long long phase = (unsigned long long)pos * a.turns[f], quarter = (phase + (1ull << 61)) >> 62;
                     float sn, cs;
-                    sincospif((float)phase * 1.0842021724855044e-19f, &sn, &cs);  // 2^-63
+                    sincospif((float)(long long)(phase - (quarter << 62)) * 1.0842021724855044e-19f, &sn, &cs);  // 2^-63
+                    if (quarter & 1) {
+                        const float s0 = sn;
+                        sn = cs;
+                        cs = -s0;
+                    }
+                    if (quarter & 2) sn = -sn, cs = -cs;
                     turn[t * half + (f % kPairs) * a.rot_slots + f / kPairs] = make_float2(cs * a.magnitude, sn * a.sign * a.magnitude);
                 }
                 __syncthreads();
