@@ -112,8 +112,12 @@ class AdamW:
     def __init__(self, shapes: Sequence[Sequence[int]], offsets: Optional[Sequence[int]] = None, *, weight_decay=0.1, betas=(0.9, 0.95),
                  eps: float = 1e-8, max_norm: float = 1.0, state_bits: int = 32, param_dtype=torch.float32, grad_dtype=torch.float32, skip_nonfinite: bool = True):
         n = len(shapes)
+        if offsets is not None and len(offsets) != n:
+            _refuse(f"{len(offsets)} offsets for {n} tensors")
         descs, pos = (_TensorDesc * n)(), 0
         for j, sh in enumerate(shapes):
+            if len(sh) not in (1, 2):
+                _refuse(f"tensor {j} must be [rows, cols] or a vector, got {tuple(sh)}")
             rows, cols = (1, sh[0]) if len(sh) == 1 else (sh[0], sh[1])
             off = offsets[j] if offsets is not None else (pos + 3) // 4 * 4
             descs[j] = _TensorDesc(rows, cols, off)
