@@ -528,7 +528,8 @@ sl_status sl_rotary_apply(sl_rotary* ctx, const sl_rotary_desc* d, const sl_rota
  * is still written).  total = w * sum of the losses; 0 when no row counts.  A logit of -inf has p = 0 (a masked vocabulary
  * entry; with smoothing > 0 it makes the loss infinite, as the formula says); a row of nothing but -inf has lse = -inf, gradient 0
  * and loss +inf; NaN or +inf in a row give NaN.  A target outside [0, vocab) that is not ignore_index gives its row (and the
- * total) a NaN loss and a gradient of 0 (the row counts).
+ * total) a NaN loss and a gradient of 0 (the row counts).  A row's loss is formed from the differences of lse to the logits, as accurate
+ * for logits near 1000 as near 0; a difference below 2^-21 counts as 0.
  * grad: NULL (loss only), or rows of `dtype` by ld_grad; grad may be logits itself (then ld_grad = ld_logits).
  * The kernel's waits for its own copies are bounded; one that ran out would show as NaN losses from that row on.
  * row_loss (rows fp32) is required; lse, total may be NULL.  targets: int32 or int64 (target_bits).  rows = 0 is allowed.

@@ -1,4 +1,4 @@
-// Residual update and norms around a block, forward and backward, row by row.  Part of libsparseloco (inner.cu).
+// Residual update and norms around a block, forward and backward, row by row.  Part of libsparseloco (block_norm.cu).
 //
 // Bound: HBM.  Forward reads x and branch and writes y and h; backward reads dy, dh, y, branch and writes dx, dbranch:
 // every matrix once.  A row lives in the registers of its threads between its sums and its outputs (a warp for narrow
@@ -9,6 +9,10 @@
 #include "inner_common.cuh"
 
 namespace {
+
+// Not tuned: rows wider than the team kernels' shared memory allows in the backward pass (from 4104 columns in fp32, 8200 in bfloat16),
+// and rows of many single values a thread: the general backward kernels keep 32 columns of six arrays a thread and spill 1700 to 3900 bytes.
+// The one-warp backward teams of up to 512 columns spill 90 to 720 bytes.
 
 constexpr int kNormMaxCols = 16384;
 constexpr int kNormMaxThreads = 512;

@@ -129,6 +129,7 @@ struct LossRow {
     }
     // ... within 2^-21 of lse or so: what the gradient's factor of p needs
     __device__ __forceinline__ float near_lse() const { return scale == 1.0f ? ref + __logf(s) : (ref + __log2f(s)) * kLn2; }
+    // (the quotient within 2 ulp: s is at most 2^95, far below where the fast division gives up, and at least 2^-65)
     __device__ __forceinline__ float factor(const LossArgs& a, float w) const { return __fdividef(a.z == 0.0f ? w : w * fmaf(2.0f * a.z, near_lse(), 1.0f), s); }
 };
 // 1 / (rows that count), or 1, times the caller's scale; the count comes from the kernel before

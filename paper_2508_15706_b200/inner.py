@@ -107,7 +107,9 @@ class AdamW:
 
     Parameters, gradients and moments are flat buffers of one layout: let every parameter's `.grad` be a view of the flat
     gradient, and theta_local[r] of the outer step is the very buffer that `step` updates.  `state_bits=8` keeps the moments
-    in 8-bit codes with one power-of-two scale per 128 elements: 2 bytes per parameter in place of 8."""
+    in 8-bit codes with one power-of-two scale per 128 elements: 2 bytes per parameter in place of 8.
+
+    One object holds scratch memory for the gradient's norm: its steps must not overlap on the device (two streams want two objects)."""
 
     def __init__(self, shapes: Sequence[Sequence[int]], offsets: Optional[Sequence[int]] = None, *, weight_decay=0.1, betas=(0.9, 0.95),
                  eps: float = 1e-8, max_norm: float = 1.0, state_bits: int = 32, param_dtype=torch.float32, grad_dtype=torch.float32, skip_nonfinite: bool = True):
