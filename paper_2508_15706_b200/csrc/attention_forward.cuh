@@ -254,7 +254,6 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_forward_kernel(const
 #pragma unroll
                 for (int i = 0; i < 4; ++i) tmem_loaded(s[i]);
                 const int k0 = t * 128;
-                const bool some = k0 < mine.z || k0 + 128 > mine.w;
                 if (k0 < mine.z) {
                     const int lo = see.x - k0;
 #pragma unroll
@@ -298,11 +297,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attention_forward_kernel(const
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
                         const float2 e = fma2(make_float2(s[i][2 * j], s[i][2 * j + 1]), c2, from2);
-                        float2 p = exp2_pair<kFwdPoly>(e, j);
-                        if (some) {  // (nothing of a masked score)
-                            p.x = e.x == -INFINITY ? 0.0f : p.x;
-                            p.y = e.y == -INFINITY ? 0.0f : p.y;
-                        }
+                        const float2 p = exp2_pair<kFwdPoly>(e, j);  // (0 of -inf, and NaN stays: a row with one is found by its sums)
                         sum2 = add2(sum2, p);
                         w[j] = narrow2(p);
                     }

@@ -191,19 +191,27 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// The larger of two, NaN where either is.
+__device__ __forceinline__ float max_nan(float x, float y) {
+    float z;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(z) : "f"(x), "f"(y));
+    return z;
+}
 // The same of two values by multiply-adds, for part of a tile's exponentials (the instruction above takes 8 cycles a warp): x = n + f with n the
 // nearest integer, 2^f on [-1/2, 1/2] by the polynomial of degree 5 with the smallest relative error that is 1 at 0 (1.1e-7, a linear
-// programme over 4001 points), n added to the exponent.  Below -126 it stays at 2^-126.
+// programme over 4001 points), times 2^n.  What is added to round x leaves n + 127 in the lowest bits, the exponent of 2^n.  x may be up to 127; below -126.5
+// (-inf too) the factor's exponent is 0 and the result 0, as the instruction's is, and NaN goes through every step.
 __device__ __forceinline__ float2 exp2_poly(float2 x) {
-    x.x = fmaxf(x.x, -126.0f);
-    x.y = fmaxf(x.y, -126.0f);
-    const float2 t = add2(x, both(12582912.0f)), n = add2(t, both(-12582912.0f)), f = fma2(n, both(-1.0f), x);
+    constexpr float kRound = 12582912.0f + 127.0f;  // 3 * 2^22
+    x.x = max_nan(x.x, -127.0f);
+    x.y = max_nan(x.y, -127.0f);
+    const float2 t = add2(x, both(kRound)), n = add2(t, both(-kRound)), f = fma2(n, both(-1.0f), x);
     float2 p = fma2(both(0.001326465280726552f), f, both(0.009671511128544807f));
     p = fma2(p, f, both(0.05550733953714371f));
     p = fma2(p, f, both(0.24022242426872253f));
     p = fma2(p, f, both(0.6931470036506653f));
     p = fma2(p, f, both(1.0f));
-    return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)), __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
+    return mul2(p, make_float2(__int_as_float(__float_as_int(t.x) << 23), __int_as_float(__float_as_int(t.y) << 23)));
 }
 // pair i of a row: which of the two ways
 template <int OF8>
