@@ -291,7 +291,8 @@ __device__ __noinline__ void plain_forward_tile(const AttnArgs& a, int q0, int h
     }
 }
 
-// p of queries against keys, kept in registers: rows are queries (ty R + r), columns keys (tx + 16 c); `own` is which of the two the ranges are of
+// p of queries against keys, kept in registers: rows are queries (ty R + r), columns keys (tx + 16 c); KEYS is which of the two the ranges are of.
+// Masked ones are -0, which no exponential is, so that plain_ds knows them.
 template <int R, int C, bool KEYS>
 __device__ __forceinline__ void plain_p(const AttnArgs& a, float (&p)[R][C], const int2* range, const float* lse, int q0, int k0, bool some, int tx, int ty) {
 #pragma unroll
@@ -303,17 +304,17 @@ __device__ __forceinline__ void plain_p(const AttnArgs& a, float (&p)[R][C], con
             const int col = tx + 16 * c, j = k0 + col;
             const int2 see = KEYS ? range[row] : range[col];
             const bool in = !some || (KEYS ? j >= see.x && j < see.y : i >= see.x && i < see.y);
-            p[r][c] = in ? exp2f(fmaf(p[r][c], a.c, l)) : 0.0f;
+            p[r][c] = in ? exp2f(fmaf(p[r][c], a.c, l)) : -0.0f;
         }
     }
 }
-// ds = p (dp - delta); 0 where p is, whatever dp
+// ds = p (dp - delta); 0 where masked, whatever dp.  (Not wherever p is 0: a weight that vanishes passes a NaN on all the same.)
 template <int R, int C>
 __device__ __forceinline__ void plain_ds(float (&dp)[R][C], const float (&p)[R][C], const float* delta, int ty) {
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int c = 0; c < C; ++c) dp[r][c] = p[r][c] == 0.0f ? 0.0f : p[r][c] * (dp[r][c] + delta[ty * R + r]);
+        for (int c = 0; c < C; ++c) dp[r][c] = __float_as_uint(p[r][c]) == 0x80000000u ? 0.0f : p[r][c] * (dp[r][c] + delta[ty * R + r]);
 }
 template <int R, int C>
 __device__ __forceinline__ void plain_keep(float* to, const float (&x)[R][C], int pitch, int tx, int ty) {
