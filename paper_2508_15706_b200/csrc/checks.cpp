@@ -174,13 +174,14 @@ PyObject* empties(PyObject* const* args, Py_ssize_t n) {
             return nullptr;
         }
         if (!integers(a + 1, 2, v[i])) return nullptr;
-        if (v[i][0] < 0 || v[i][0] > (1ll << 40) || v[i][1] > (1ll << 20)) {
+        types[i] = reinterpret_cast<THPDtype*>(a[0])->scalar_type;
+        const int64_t most = (1ll << 50) / (int64_t)c10::elementSize(types[i]), across = v[i][1] < 0 ? 1 : v[i][1];  // (2^50 bytes a tensor: their sum stays within 64 bits)
+        if (v[i][0] < 0 || (across > 0 && v[i][0] > most / across)) {
             PyErr_SetString(PyExc_ValueError, "empties: sizes out of range");
             return nullptr;
         }
-        types[i] = reinterpret_cast<THPDtype*>(a[0])->scalar_type;
         at_byte[i] = bytes;
-        bytes += (v[i][0] * (v[i][1] < 0 ? 1 : v[i][1]) * (int64_t)c10::elementSize(types[i]) + 255) / 256 * 256;
+        bytes += (v[i][0] * across * (int64_t)c10::elementSize(types[i]) + 255) / 256 * 256;
     }
     const at::Tensor all = at::empty({bytes}, at::TensorOptions().dtype(at::kByte).device(at::kCUDA, (at::DeviceIndex)dev));
     PyObject* out = PyTuple_New(count);
