@@ -28,11 +28,18 @@ PyObject* refused(PyObject* what, PyObject* tensor, PyObject* wanted) {
 
 bool is_dtype(const at::Tensor& x, PyObject* dtype) { return THPDtype_Check(dtype) && reinterpret_cast<THPDtype*>(dtype)->scalar_type == x.scalar_type(); }
 
-// The entry as Python calls it: a C++ exception (a tensor without strides or storage, say) becomes a RuntimeError here.
+// The entry as Python calls it: a C++ exception (a tensor without strides or storage, say) becomes a RuntimeError here, memory that is not there torch's
+// own error for it.
 template <PyObject* (*F)(PyObject* const*, Py_ssize_t)>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
     try {
         return F(args, n);
+    } catch (const c10::OutOfMemoryError& e) {
+        PyObject* torch = PyImport_ImportModule("torch");
+        PyObject* type = torch ? PyObject_GetAttrString(torch, "OutOfMemoryError") : nullptr;
+        if (type) PyErr_SetString(type, e.what_without_backtrace());  // (else the error of the lookup stands)
+        Py_XDECREF(type);
+        Py_XDECREF(torch);
     } catch (const std::exception& e) {
         PyErr_SetString(PyExc_RuntimeError, e.what());
     } catch (...) {
