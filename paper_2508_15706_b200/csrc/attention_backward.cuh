@@ -218,13 +218,16 @@ __global__ void __launch_bounds__(kBwdThreads, BwdShape<D>::kCtas) attention_dkv
     const int round0 = share.x, rounds = share.y - share.x;
 
     if (warp >= 8) {
-        if (warp == 9 && rounds > 0 && elected()) {
-            bar_expect(shared_address(&sh.own_full), 2 * kOwn);
-            for (int p = 0; p < D / 64; ++p)
-                for (int r = 0; r < 128; r += R) {
-                    tile_load(sk + p * 16384 + r * 128, &mk, swapped >> 1 & 1, p * 64, kv, k0 + r, shared_address(&sh.own_full));
-                    tile_load(sv + p * 16384 + r * 128, &mv, swapped >> 2 & 1, p * 64, kv, k0 + r, shared_address(&sh.own_full));
-                }
+        if (warp == 9 && elected()) {
+            if (rounds > 0) {
+                bar_expect(shared_address(&sh.own_full), 2 * kOwn);
+                for (int p = 0; p < D / 64; ++p)
+                    for (int r = 0; r < 128; r += R) {
+                        tile_load(sk + p * 16384 + r * 128, &mk, swapped >> 1 & 1, p * 64, kv, k0 + r, shared_address(&sh.own_full));
+                        tile_load(sv + p * 16384 + r * 128, &mv, swapped >> 2 & 1, p * 64, kv, k0 + r, shared_address(&sh.own_full));
+                    }
+            }
+            // (A CTA without rounds waits too: that this kernel has ended has to mean that the one in front of it has, since dq waits for this one alone.)
             earlier_done();    // the statistics are there, for the loads below and for dq,
             next_may_begin();  // which may begin when every CTA has come as far
             bool ok = true;
@@ -510,7 +513,7 @@ __global__ void __launch_bounds__(kBwdThreads, BwdShape<D>::kCtas) attention_dq_
         const int4 mine = sh.ranges[warp & 3];
         const bool in = see.y > 0;
         const long long at = (long long)head * a.pitch + i;  // (the statistics are padded to whole tiles)
-        const float2 c2 = both(a.c), l2 = both(a.nlse2[at]), d2 = both(a.ndelta[at]);
+        const float2 c2 = both(a.c), l2 = both(__ldcg(&a.nlse2[at])), d2 = both(__ldcg(&a.ndelta[at]));  // (from L2: written by a kernel that this one has not waited for itself)
         bool ok = true;
         for (int round = 0; round < rounds; ++round) {
             const int j0 = (first + round) * R + H * half;
@@ -558,7 +561,7 @@ __global__ void __launch_bounds__(kBwdThreads, BwdShape<D>::kCtas) attention_dq_
         tmem_fence_after();
         tmem_free(tmem, Shape::kColumns);
     }
-    // (the last CTA, which has the least to do, ends after dk and dv have: what follows in the stream waits for this kernel alone)
+    // (the last CTA, which has the least to do, ends after dk and dv have, and with them the statistics: what follows in the stream waits for this kernel alone)
     if (tid == 0 && blockIdx.x + 1 == gridDim.x && blockIdx.y + 1 == gridDim.y) earlier_done();
     if (sh.failed || !sh.again || tid >= 256) return;
     constexpr int kSteps = R / plain_step_of(D);  // of the fp32 code to a round

@@ -328,8 +328,8 @@ template <int ROWS>
 __device__ __forceinline__ void plain_stats(float* lse, float* delta, const AttnArgs& a, int head, int q0, int tid) {
     if (tid < ROWS) {
         const long long at = (long long)head * a.pitch + q0 + tid;  // (padded to whole tiles)
-        lse[tid] = a.nlse2[at];
-        delta[tid] = a.ndelta[at];
+        lse[tid] = __ldcg(&a.nlse2[at]);  // (from L2, for the kernels that begin before the one that wrote them is waited for)
+        delta[tid] = __ldcg(&a.ndelta[at]);
     }
 }
 
