@@ -184,10 +184,12 @@ __device__ __forceinline__ X lanes16_sum(X x) {
 }
 
 // The ranges of a tile's rows into shared memory, and over all of them: the first and the last token seen, and the largest
-// beginning and smallest end (steps of tokens between those are full for every row).  All threads get the four numbers.
+// beginning and smallest end (steps of tokens between those are full for every row).  All threads get the four numbers.  The note of values that
+// are not finite is cleared between the two barriers: a thread still in the last round of a tile before this one reads that tile's.
 template <int TILE, bool KEYS>
-__device__ __forceinline__ int4 plain_ranges(const AttnArgs& a, int first, int2* range, int tid) {
+__device__ __forceinline__ int4 plain_ranges(const AttnArgs& a, int first, int2* range, volatile int* odd, int tid) {
     plain_sync();
+    if (tid == 0) *odd = 0;
     if (tid < TILE) range[tid] = KEYS ? keys_of(a, first + tid) : queries_of(a, first + tid);
     plain_sync();
     int4 all = make_int4(0x7FFFFFFF, 0, 0, 0x7FFFFFFF);
@@ -227,8 +229,7 @@ __device__ __noinline__ void plain_forward_tile(const AttnArgs& a, int q0, int h
     volatile int* odd = reinterpret_cast<int*>(range + TILE);
     int unused = 0;  // (q and k meet masked scores only before they are masked)
     const int tx = tid & 15, ty = tid >> 4;
-    if (tid == 0) *odd = 0;
-    const int4 all = plain_ranges<TILE, true>(a, q0, range, tid);
+    const int4 all = plain_ranges<TILE, true>(a, q0, range, odd, tid);
     plain_load<T, DMAX, TILE>(sq, a.q, a.sq, head, q0, a, tid, &unused);
     float acc[R][DMAX / 64][4], top[R], sum[R];
     plain_zero(acc);
@@ -345,8 +346,7 @@ __device__ __noinline__ void plain_dkv_tile(const AttnArgs& a, int k0, int kv, i
     volatile int* odd = reinterpret_cast<int*>(delta + STEP);
     int unused = 0;
     const int tx = tid & 15, ty = tid >> 4;
-    if (tid == 0) *odd = 0;
-    const int4 all = plain_ranges<TILE, false>(a, k0, range, tid);
+    const int4 all = plain_ranges<TILE, false>(a, k0, range, odd, tid);
     plain_load<T, DMAX, TILE>(sk, a.k, a.sk, kv, k0, a, tid, &unused);
     plain_load<T, DMAX, TILE>(sv, a.v, a.sv, kv, k0, a, tid, &unused);
     float gk[R][DMAX / 64][4], gv[R][DMAX / 64][4];
@@ -403,8 +403,7 @@ __device__ __noinline__ void plain_dq_tile(const AttnArgs& a, int q0, int head, 
     volatile int* odd = reinterpret_cast<int*>(delta + TILE);
     int unused = 0;
     const int tx = tid & 15, ty = tid >> 4;
-    if (tid == 0) *odd = 0;
-    const int4 all = plain_ranges<TILE, true>(a, q0, range, tid);
+    const int4 all = plain_ranges<TILE, true>(a, q0, range, odd, tid);
     plain_load<T, DMAX, TILE>(sq, a.q, a.sq, head, q0, a, tid, &unused);
     plain_load<T, DMAX, TILE>(sdo, a.dout, a.sdo, head, q0, a, tid, &unused);
     plain_stats<TILE>(lse, delta, a, head, q0, tid);
