@@ -438,14 +438,17 @@ def attention_forward(q, k, v, offsets=None, *, causal: bool = True, scale: Opti
     """Attention over packed sequences: q [tokens, heads, head_dim], k and v with heads that divide q's, sequence s being the tokens
     offsets[s] .. offsets[s + 1] - 1 (int32 on the device; None: one sequence); or [batch, seq, heads, head_dim] without offsets.
     Strides are free outside a head.  `scale` defaults to head_dim ** -0.5.  Returns (out, lse), lse fp32 [heads, tokens].  Rows of tokens in no sequence: 0
-    in an `out` allocated here, left as they were in one that is given."""
+    in an `out` allocated here and -inf in such an `lse`, left as they were in one that is given."""
     dev = _here()
     tokens, heads, kv, dim, act, sequences, seq, table, scale = _attention_case(q, k, v, offsets, dev, scale)
-    fill = out is None
-    if fill:
-        out = torch.empty(q.shape, dtype=act, device=q.device)
+    fill = out is None and lse is None
+    apart = not fill and table is not None  # (the kernels fill the rest of both or of neither: of one alone it is set beforehand)
+    if out is None:
+        out = (torch.zeros if apart else torch.empty)(q.shape, dtype=act, device=q.device)
     if lse is None:
         (lse,) = _empties(dev, torch.float32, heads, tokens)
+        if apart:
+            lse.fill_(float("-inf"))
     pq, pk, pv = _tokens(q, dev, tokens, heads, dim, act, "q"), _tokens(k, dev, tokens, kv, dim, act, "k"), _tokens(v, dev, tokens, kv, dim, act, "v")
     po = _tokens(out, dev, tokens, heads, dim, act, "out")
     d = _attention_bytes(tokens, sequences, seq, heads, kv, dim, _dtype(act), causal, fill, scale, *pq[1:], *pk[1:], *pv[1:], *po[1:], 0, 0, 0, 0, 0, 0, 0, 0)
@@ -466,12 +469,13 @@ def attention_workspace(q, k, offsets=None, *, causal: bool = True) -> torch.Ten
 
 
 def attention_backward(dout, q, k, v, out, lse, offsets=None, *, causal: bool = True, scale: Optional[float] = None, dq=None, dk=None, dv=None, workspace=None):
-    """Gradients of `attention_forward`, from its out and lse: (dq, dk, dv).  Those left out are allocated; rows of tokens in no
-    sequence are 0 when all three are, and left as they were otherwise."""
+    """Gradients of `attention_forward`, from its out and lse: (dq, dk, dv).  Those left out are allocated.  Rows of tokens in no
+    sequence: 0 in those allocated here, left as they were in those given."""
     dev = _here()
     tokens, heads, kv, dim, act, sequences, seq, table, scale = _attention_case(q, k, v, offsets, dev, scale)
     fill = dq is None and dk is None and dv is None
-    dq, dk, dv = (torch.empty(x.shape, dtype=act, device=x.device) if g is None else g for g, x in ((dq, q), (dk, k), (dv, v)))
+    make = torch.empty if fill or table is None else torch.zeros  # (the kernels fill the rest of all three or of none)
+    dq, dk, dv = (make(x.shape, dtype=act, device=x.device) if g is None else g for g, x in ((dq, q), (dk, k), (dv, v)))
     pq, pk, pv = _tokens(q, dev, tokens, heads, dim, act, "q"), _tokens(k, dev, tokens, kv, dim, act, "k"), _tokens(v, dev, tokens, kv, dim, act, "v")
     po, pd = _tokens(out, dev, tokens, heads, dim, act, "out"), _tokens(dout, dev, tokens, heads, dim, act, "dout")
     gq, gk, gv = _tokens(dq, dev, tokens, heads, dim, act, "dq"), _tokens(dk, dev, tokens, kv, dim, act, "dk"), _tokens(dv, dev, tokens, kv, dim, act, "dv")
