@@ -540,7 +540,8 @@ def route_workspace(rows: int, experts: int, k: int) -> torch.Tensor:
 
 def route_forward(logits, k: int, *, mask=None, renormalize: bool = True, workspace=None) -> Routing:
     """The k experts of every row of [tokens, experts] logits with their weights (softmax, over the chosen alone with `renormalize`), places in
-    expert order, counts, balance loss and z loss.  `mask`: bool [tokens], False for tokens that do not count."""
+    expert order, counts, balance loss and z loss.  `mask`: bool [tokens], False for tokens that do not count.  The results lie in one piece of memory: it lives as
+    long as any of them."""
     if logits.dim() != 2:
         _refuse("logits must be [tokens, experts]")
     dev = _here()
@@ -551,10 +552,12 @@ def route_forward(logits, k: int, *, mask=None, renormalize: bool = True, worksp
         _refuse(f"mask must be bool [{rows}], got {mask.dtype} {tuple(mask.shape)}")
     pm = _ptr(mask, dev, rows, torch.bool, "mask")
     i32, f32 = torch.int32, torch.float32
-    scratch = _route_workspace_bytes(rows, E, k)
+    scratch = _route_workspace_bytes(rows, E, k) if workspace is None else 0
+    # (scratch of up to 16 KB lies with the results, which saves a visit to the allocator; more of it would live as long as they do)
     weights, experts, slots, counts, offsets, balance, z, lse, spare = r = _empties(dev, f32, rows, k, i32, rows, k, i32, rows, k, i32, E, -1, i32, E + 1, -1, f32, 1, -1, f32, 1, -1, f32, rows, -1,
-                                                                                    torch.uint8, scratch if workspace is None else 0, -1)
-    workspace = spare if workspace is None else workspace
+                                                                                    torch.uint8, scratch if scratch <= 16384 else 0, -1)
+    if workspace is None:
+        workspace = spare if scratch <= 16384 else _empties(dev, torch.uint8, scratch, -1)[0]
     _check(_L.sl_route_forward(_route_bytes(rows, E, k, _dtype(act), renormalize, ld, 0), px, pm, weights.data_ptr(), experts.data_ptr(), slots.data_ptr(), counts.data_ptr(),
                                offsets.data_ptr(), lse.data_ptr(), balance.data_ptr(), z.data_ptr(), _ptr(workspace, dev, 0, torch.uint8, "workspace"), workspace.numel(), _queue(dev)))
     return Routing(*r[:8])
