@@ -213,7 +213,7 @@ class AdamW:
 
 def _laid_out(t):
     """A matrix as the kernels take it, unit column stride and rows apart: itself, or (transposed, expanded) a copy."""
-    if t is None or ((t.shape[1] <= 1 or t.stride(1) == 1) and (t.shape[0] <= 1 or t.stride(0) >= t.shape[1])):
+    if t is None or t.dim() != 2 or ((t.shape[1] <= 1 or t.stride(1) == 1) and (t.shape[0] <= 1 or t.stride(0) >= t.shape[1])):
         return t
     return t.contiguous()
 
@@ -488,8 +488,8 @@ def attention_backward(dout, q, k, v, out, lse, offsets=None, *, causal: bool = 
 
 def _in_tokens(t):
     """A tensor as the attention kernels take it, a unit stride inside a head and sequences one behind the other: itself or a copy."""
-    if (t.shape[-1] <= 1 or t.stride(-1) == 1) and (t.dim() == 3 or t.shape[0] <= 1 or t.shape[1] <= 1 or t.stride(0) == t.shape[1] * t.stride(1)):
-        return t
+    if t.dim() < 3 or ((t.shape[-1] <= 1 or t.stride(-1) == 1) and (t.dim() == 3 or t.shape[0] <= 1 or t.shape[1] <= 1 or t.stride(0) == t.shape[1] * t.stride(1))):
+        return t  # (of fewer dimensions: refused by the call)
     return t.contiguous()
 
 
