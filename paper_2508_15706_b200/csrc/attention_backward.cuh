@@ -115,7 +115,7 @@ __device__ __forceinline__ bool store_part(unsigned at, bool any, bool in, bool 
         }
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
-            o[j] = !any || !in ? 0.0f : ok ? o[j] : NAN;
+            o[j] = !in ? 0.0f : !ok ? NAN : any ? o[j] : 0.0f;
             fine = fine && fabsf(o[j]) <= 3.4e38f;
         }
 #pragma unroll
@@ -124,6 +124,10 @@ __device__ __forceinline__ bool store_part(unsigned at, bool any, bool in, bool 
     }
     return fine;
 }
+
+// The tiles' swizzle counts from multiples of 1024 bytes.  The kernels have no static shared memory, so that the dynamic one begins on such an address, as its
+// declaration asks; with D = 128 it is too full for rounding up.  Should it ever lie elsewhere, nothing is copied and the results are NaN.
+__device__ __forceinline__ bool swizzle_placed(unsigned at) { return (at & 1023u) == 0u; }
 
 __device__ __forceinline__ void bwd_init(BwdShared& sh) {
     sh.failed = sh.again = 0;
@@ -215,7 +219,8 @@ __global__ void __launch_bounds__(kBwdThreads, BwdShape<D>::kCtas) attention_dkv
     const int4 all = tile_ranges(sh.ranges);
     const int first = all.y > 0 ? all.x / R : 0, tiles = (all.y + R - 1) / R - first;
     const int2 share = share_of(tiles * a.group, part, a.parts_kv);  // of the heads' tiles one after the other
-    const int round0 = share.x, rounds = share.y - share.x;
+    const bool placed = swizzle_placed(sk);
+    const int round0 = share.x, rounds = placed ? share.y - share.x : 0;
 
     if (warp >= 8) {
         if (warp == 9 && elected()) {
@@ -328,7 +333,7 @@ __global__ void __launch_bounds__(kBwdThreads, BwdShape<D>::kCtas) attention_dkv
         const unsigned lanes = (unsigned)(warp & 3) << 21, s_t = s_at + lanes + H * half, dp_t = dp_at + lanes + H * half;
         const int4 mine = sh.ranges[warp & 3];
         const float2 c2 = both(a.c);
-        bool ok = true;
+        bool ok = placed;
         for (int round = 0; round < rounds; ++round) {
             const int q0 = (first + (round0 + round) % tiles) * R + H * half;
             // (after a failure the rest of the waits end at once)
@@ -424,7 +429,8 @@ __global__ void __launch_bounds__(kBwdThreads, BwdShape<D>::kCtas) attention_dq_
     const unsigned tmem = sh.tmem, dp_at = tmem + 2 * R, dq_at = tmem + 3 * R;  // scores of even and odd rounds in front
     const int4 all = tile_ranges(sh.ranges);
     const int2 share = all.y > 0 ? share_of((all.y + R - 1) / R - all.x / R, part, a.parts_q) : make_int2(0, 0);
-    const int first = (all.y > 0 ? all.x / R : 0) + share.x, rounds = share.y - share.x;
+    const bool placed = swizzle_placed(sq);
+    const int first = (all.y > 0 ? all.x / R : 0) + share.x, rounds = placed ? share.y - share.x : 0;
 
     if (warp >= 8) {
         if (warp == 9 && rounds > 0 && elected()) {
@@ -514,7 +520,7 @@ __global__ void __launch_bounds__(kBwdThreads, BwdShape<D>::kCtas) attention_dq_
         const bool in = see.y > 0;
         const long long at = (long long)head * a.pitch + i;  // (the statistics are padded to whole tiles)
         const float2 c2 = both(a.c), l2 = both(__ldcg(&a.nlse2[at])), d2 = both(__ldcg(&a.ndelta[at]));  // (from L2: written by a kernel that this one has not waited for itself)
-        bool ok = true;
+        bool ok = placed;
         for (int round = 0; round < rounds; ++round) {
             const int j0 = (first + round) * R + H * half;
             const unsigned s_t = tmem + R * (round & 1) + lanes + H * half, dp_t = dp_at + lanes + H * half;
