@@ -288,7 +288,7 @@ __device__ __noinline__ void plain_forward_tile(const AttnArgs& a, int q0, int h
         const bool in = range[ty * R + r].y > 0;
         if (i >= a.tokens || (!in && !a.fill)) continue;
         plain_store<T, DMAX, R>(acc, r, a.o, a.so, head, i, in ? 1.0f / sum[r] : 0.0f, a, tx);
-        if (tx == 0) a.lse[(long long)head * a.tokens + i] = in ? top[r] * a.scale + logf(sum[r]) : -INFINITY;
+        if (tx == 0) a.lse[(long long)head * a.tokens + i] = !in ? -INFINITY : top[r] == INFINITY ? INFINITY : top[r] * a.scale + logf(sum[r]);  // (the sum is NaN beside a score of inf)
     }
 }
 
