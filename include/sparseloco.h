@@ -565,17 +565,18 @@ sl_status sl_token_loss_backward(int32_t dtype, int64_t n, const void* grad, con
  * sequence s is the tokens offsets[s] .. offsets[s + 1] - 1, possibly none.  Entries outside 0 .. tokens are taken as those limits (a
  * table that falls gives wrong results, but touches no memory outside the tensors).  Tokens in no sequence, behind the last one above
  * all, are not read into any result; of the outputs their rows are left as they were, or with fill_rest set to 0 (lse: -inf).
+ * What a query sees reaches it: a NaN score makes its out and lse NaN, one of +inf its out NaN and its lse +inf.
  * What a query must not see does not reach it, whatever it holds: rows in no sequence change no bit of a result, and infinities or
  * NaN at masked tokens of a sequence change no more than roundings (the tensor-core kernels have the tiles beside them formed in fp32).
- * Scores, softmax statistics and sums are fp32.  bfloat16 heads of up to 128 values whose strides and addresses are multiples of 16
- * bytes run on the tensor cores, p and ds rounded to bfloat16 as operands of a product; all else in fp32 multiply-adds.  Sums are formed in a fixed order
+ * Scores, softmax statistics and sums are fp32.  bfloat16 heads of up to 128 values whose addresses and strides are multiples of 16
+ * bytes, the strides above 0, run on the tensor cores, p and ds rounded to bfloat16 as operands of a product; all else in fp32 multiply-adds.  Sums are formed in a fixed order
  * (results repeat bit for bit).  The waits of the former kernels for their own copies and products are bounded; one that ran out
  * would show as NaN rows.
  * tokens = 0 is allowed.  workspace: sl_attention_workspace_bytes(), 16-byte aligned, contents need not be kept; calls that
  * share it must not overlap.
  * Errors: INVALID_ARG (NULL, sizes, heads that do not divide, strides, a scale that is not positive and finite, an output at
  * another tensor's address), ALIGNMENT (a pointer off its element size), UNSUPPORTED (dtype), TOO_LARGE (head_dim > 256, tokens > 2^30,
- * 65536 heads or more), NOMEM (workspace), CUDA. */
+ * 65536 heads or more, tokens / 32 times q_heads beyond 2^31), NOMEM (workspace), CUDA. */
 typedef struct {
     int64_t tokens, sequences, seq;
     int32_t q_heads, kv_heads, head_dim;

@@ -12,8 +12,8 @@
 //
 // dq needs nothing of dk and dv: its kernel begins as soon as the other's last CTAs have begun, and fills the SMs that run out of tiles of keys.
 //
-// Measured, bfloat16, causal, with the statistics: 4 x 4096 tokens, 16 heads of 128 on 4, 825 us from a graph (833 TFLOP/s counting the 5 products, 1166
-// with the 7 that run), 935 to 960 in a loop; 6007 tokens in 23 sequences, 12 heads of 64, 80 us.  A round of dk, dv takes 3200 cycles, of dq 2400, with the
+// Measured, bfloat16, causal, with the statistics: 4 x 4096 tokens, 16 heads of 128 on 4, 807 us from a graph (852 TFLOP/s counting the 5 products, 1193
+// with the 7 that run), 915 to 960 in a loop; 6007 tokens in 23 sequences, 12 heads of 64, 80 us (two CTAs an SM leave 80 registers a thread: dk, dv spills 84 bytes, dq 60).  A round of dk, dv takes 3200 cycles, of dq 2400, with the
 // tensor cores at work 63 % of them.  What was tried: two streams of 64-row items with a warpgroup each (4190 and 3390 cycles: a wait costs the
 // issuing thread 200 cycles even when there is nothing to wait for, and there were twice as many); four warpgroups to a round in place of two (the same
 // within 3 %); `lane == 0` in place of elect.sync (3990 and 3080).  Of 8 exponentials 1 goes by multiply-adds (0: 2 % slower, 3: 3 % with heads of 64).

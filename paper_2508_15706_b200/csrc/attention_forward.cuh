@@ -5,16 +5,17 @@
 // third group of warps feeds them: one thread issues every product, one every copy (K and V tiles through a ring), one warp clears rows.  While one
 // tile's S is with its warpgroup, the tensor cores work on the other's, so the two take turns, and K and V are read once for 256 queries.  With
 // D = 128 a tile pair costs 2048 cycles of products and 2 x 16384 exponentials, 2048 cycles at 16 a cycle: both bound.  So part of the exponentials are
-// formed by multiply-adds (1 of 8: 32768 tokens 3.75 -> 3.60 ms in a short run, 4 x 4096 with heads of 64 280 -> 247 us; 2 of 8 3.77 ms, 4 of 8 3.99), and m, the row's reference, follows the
+// formed by multiply-adds (1 of 8: 32768 tokens 3.75 -> 3.60 ms in a short run; 2 of 8 3.77 ms, 4 of 8 3.99), and m, the row's reference, follows the
 // maximum only when that has moved by more than 2^8 (P may be as large as that; sums and O are fp32), which spares O's rescaling.
-// P is rounded to bfloat16 as an operand: 2^-9 of its size at most on either side, beside the output's own rounding.
+// P is rounded to bfloat16 as an operand: 2^-8 of its size at most on either side, beside the output's own rounding.
 //
-// Measured, 16 heads of 128 on 4, bfloat16, causal: 32768 tokens 3.89 ms from a graph (1131 TFLOP/s, 69 % of what a library product reaches in a
-// burst, 82 % of what it holds), 4.23 ms in a loop at the power limit; 4 x 4096 tokens 299 us; 12 heads of 64 206 us.  37 tokens 7.9 us: one CTA's way from
-// the launch through offsets, copies, two products and the store.  Steps: issuing behind elect.sync 4.39 -> 4.04 ms.  V of a round and K of the next behind one
-// barrier made no difference.
+// Measured, 16 heads of 128 on 4, bfloat16, causal: 32768 tokens 3.50 ms from a graph (1258 TFLOP/s, 77 % of what a library product reaches in a
+// burst, 91 % of what it holds), 4.0 ms in a loop at the power limit; 4 x 4096 tokens 275 to 340 us with the clock, 12 heads of 64 190 to 225 us.  37 tokens 7.4 us: one
+// CTA's way from the launch through offsets, copies, two products and the store.  Steps: issuing behind elect.sync 4.39 -> 4.04 ms; no select for masked exponentials
+// 3.62 -> 3.48.  V of a round and K of the next behind one barrier made no difference.  The compiler fits 168 registers, those of the launch, and spills 144
+// bytes a thread, though the split leaves 216.
 //
-// Masked scores become -inf.  Their P is 0, but 0 times an infinity or NaN in V is not.  Rows of V outside every sequence (padding may hold
+// Masked scores become -inf.  Their P is 0, but 0 times an infinity or NaN in V is not.  (A NaN score stays NaN on either way to an exponential, so that the row's sums show it.)  Rows of V outside every sequence (padding may hold
 // anything) are set to 0 in shared memory; for the rest, a row whose output is not finite is taken again, with its whole tile, by the
 // fp32 code, which passes over what is masked.
 #pragma once

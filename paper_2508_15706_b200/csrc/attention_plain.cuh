@@ -6,7 +6,8 @@
 // conflicts), and of the sums R of the own rows, 4 neighbouring values every 64.  Bound: fp32 multiply-adds, two to an instruction, fed by one shared access of
 // 16 bytes for every 4 to 8 of them.  STEP is 32 for heads of 128 so that two CTAs fit an SM: one alone left most cycles without an instruction.
 // Measured, gradients in fp32 without a mask: 4096 tokens, 16 heads of 128 17.4 ms (20 TFLOP/s counting 5 products, 28 with the 7 that run, of 74);
-// 1501 tokens in 4 sequences, 10 heads on 5, 0.78 ms: tiles that only part of their rows see, and shared memory 59 % busy.
+// 1501 tokens in 4 sequences, 10 heads on 5, 0.78 ms: tiles that only part of their rows see, and shared memory 59 % busy.  Causal, 4096 tokens, 16 heads of 128: forward 2.4 ms
+// (29 TFLOP/s), gradients 7.8 ms (22, counting 5 products); heads of 64 1.24 and 3.7 ms.
 //
 // Masked scores have p = 0, which passes over finite values.  Whether all values loaded so far are finite is noted on the way into shared
 // memory; once one is not, the products of steps that are not full take each row's own range: what stands in a masked row, NaN or

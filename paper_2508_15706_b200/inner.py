@@ -596,7 +596,7 @@ def _used_of(offsets, dev):
 
 def dispatch_rows(x, slots, offsets=None, *, out=None):
     """Rows of x [tokens, cols] to the places of their choices: out [tokens * k, cols].  With the router's `offsets`, rows behind the last
-    place are set to 0."""
+    place are set to 0; without, they stay as they are, in an `out` allocated here whatever stood in that memory."""
     if x.dim() != 2:
         _refuse("x must be [tokens, cols]")
     dev = _here()
@@ -632,7 +632,7 @@ def combine_rows(y, slots, *, weights=None, residual=None, out=None):
 
 def combine_backward(dout, y, slots, weights=None, offsets=None, *, need_rows: bool = True, need_weights: bool = True, dy=None, dweights=None):
     """Gradients of `combine_rows`: (dy [tokens * k, cols], dweights fp32 [tokens, k]), None for one that is not needed.  With the router's
-    `offsets`, rows of dy behind the last place are set to 0."""
+    `offsets`, rows of dy behind the last place are set to 0; without, they stay as they are, as in `dispatch_rows`."""
     if dout.dim() != 2:
         _refuse("dout must be [tokens, cols]")
     dev = _here()
